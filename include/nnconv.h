@@ -94,7 +94,8 @@ typedef enum {
 } nnconv_status;
 
 typedef enum { NNCONV_NCHW = 0, NNCONV_NHWC = 1 } nnconv_layout;
-typedef enum { NNCONV_F16 = 0, NNCONV_BF16 = 1, NNCONV_F32 = 2 } nnconv_dtype;
+/* NNCONV_F8: the 8-bit moments of nnconv_adamw_update only. */
+typedef enum { NNCONV_F16 = 0, NNCONV_BF16 = 1, NNCONV_F32 = 2, NNCONV_F8 = 3 } nnconv_dtype;
 typedef enum { NNCONV_FWD = 0, NNCONV_DGRAD = 1, NNCONV_WGRAD = 2 } nnconv_pass;
 
 /* Convolution geometry (the parameters of the paper's convolution call plus
@@ -352,6 +353,211 @@ nnconv_status nnconv_sgd_update(int64_t count, float *master, float *momentum, v
                                 const nnconv_loss_scaler *state, const int32_t *overflow_flag,
                                 float lr, float momentum_coef, float weight_decay,
                                 void *hip_stream);
+
+/* Operators of a gated sequence block on channel-last tokens.
+ *
+ * A sequence of t tokens with c channels is an NHWC image of height 1 and
+ * width t, and a projection of its channels is a 1x1 convolution, so that
+ * nnconv_fwd, nnconv_dgrad and nnconv_wgrad are the block's matrix products.
+ * The calls below are what stands between them, and the solver that such
+ * blocks are trained with.  They follow the conventions above: caller-owned
+ * buffers, kernel launches only, gradients that carry the loss scale, and
+ * parameter gradients in fp32 with inv_loss_scale, accumulate and
+ * overflow_flag as nnconv_wgrad has them.  Sums, statistics and states are
+ * fp32; every 16-bit output is rounded once, to nearest even.  Results are
+ * bitwise reproducible for given sizes and inputs. */
+
+/* Root-mean-square norm over the channels of each row, with the residual's
+ * addition in front:
+ *   r     = x + residual, rounded to dtype  (x itself without a residual)
+ *   rstd  = 1 / sqrt(mean over c of r^2 + eps)
+ *   y     = gain * r * rstd
+ * The norm reads r as it is stored, so that the backward pass, which reads
+ * the stored r, is the gradient of what was computed.  Rows are dense: [rows][c]. */
+typedef struct {
+    int64_t rows;   /* >= 0: N*H*W of a channel-last activation, or tokens; 0 is a no-op */
+    int32_t c;      /* channels, >= 1 */
+    int32_t dtype;  /* F16 or BF16: x, residual, sum, y, dy, dsum, dx */
+    int32_t group;  /* nnconv_rmsnorm_fwd_q8: channels with one scale, 32, 64 or 128;
+                       0: one scale per row.  Others ignore it. */
+    float eps;      /* finite, >= 0 */
+} nnconv_rmsnorm_desc;
+
+/* Forward: y and, where the pointers are not NULL, sum (= r) and rstd
+ * (fp32, [rows], for the backward pass).  residual: NULL or [rows][c].
+ * gain: fp32, [c].  sum may be x or residual itself (updated in place);
+ * nothing else may overlap an output.  A row of zeros with eps = 0 gives NaN,
+ * as the formula does.  Any alignment of at least one element; 16-byte aligned
+ * rows are the fast ones.
+ * INVALID_ARG: rows < 0, c < 1, bad dtype, eps negative or not finite, null x,
+ * gain or y.  UNSUPPORTED: dtype F32.  MISALIGNED: pointers below their
+ * element size. */
+nnconv_status nnconv_rmsnorm_fwd(const nnconv_rmsnorm_desc *desc, const void *x,
+                                 const void *residual, const float *gain, void *sum, void *y,
+                                 float *rstd, void *hip_stream);
+
+/* Forward with y in 8 bits (e4m3: 4 exponent bits, 3 mantissa bits, largest
+ * value 448, no infinities) and fp32 scales:
+ *   scale = max |y| / 448 over the row, or over each group of `group` channels
+ *           (the last group of a row may be short); 0 where that is below 2^-126
+ *   q     = e4m3(y / scale), to nearest even, y unrounded; 0 where scale is 0
+ * so that q * scale stands for y.  q: [rows][c] bytes; scales:
+ * [rows][ceil(c / group)], or [rows].  The maximum passes over NaN; a NaN y has
+ * a NaN code, and an infinite y an infinite scale and a NaN code.  Otherwise as
+ * nnconv_rmsnorm_fwd; INVALID_ARG too for another group and null scales. */
+nnconv_status nnconv_rmsnorm_fwd_q8(const nnconv_rmsnorm_desc *desc, const void *x,
+                                    const void *residual, const float *gain, void *sum, void *q,
+                                    float *scales, float *rstd, void *hip_stream);
+
+/* Bytes of workspace of nnconv_rmsnorm_bwd. */
+nnconv_status nnconv_rmsnorm_workspace_size(const nnconv_rmsnorm_desc *desc, size_t *bytes);
+
+/* Backward, with xh = r * rstd:
+ *   dx    = dsum + rstd * (dy * gain - xh * mean over c of (dy * gain * xh))
+ *   dgain = (accumulate ? dgain : 0) + inv_loss_scale * sum over rows of dy * xh
+ * sum and rstd are the forward's (sum is x without a residual).  dsum: NULL
+ * (taken as 0) or the gradient that reaches r along the residual stream.
+ * dx is the gradient of r, hence of x and of residual alike; it may be dy or
+ * dsum itself.  dgain (fp32, [c]) may be NULL: then it is left out.  ws needs
+ * 4-byte alignment.
+ * Errors as nnconv_rmsnorm_fwd's, and as nnconv_wgrad's for accumulate and ws. */
+nnconv_status nnconv_rmsnorm_bwd(const nnconv_rmsnorm_desc *desc, const void *sum, const void *dy,
+                                 const void *dsum, const float *gain, const float *rstd, void *dx,
+                                 float *dgain, float inv_loss_scale, int32_t accumulate,
+                                 int32_t *overflow_flag, void *ws, size_t ws_bytes,
+                                 void *hip_stream);
+
+/* Gated linear recurrence over the tokens of each sequence, channel by channel:
+ *   z_t = f_t + bias, limited to [-80, 80];  a_t = 1 / (1 + exp(-z_t))
+ *   h_t = a_t * h_(t-1) + (1 - a_t) * x_t,   h_0 = h0
+ *   y_t = h_t * g_t / (1 + exp(-g_t))        (y_t = h_t without g)
+ * The limit keeps both a and 1 - a above 0, so that a gate never makes a NaN
+ * of an infinite state; a NaN passes through. */
+typedef struct {
+    int32_t n;      /* sequences, >= 0 */
+    int32_t t;      /* tokens of each, >= 0 */
+    int32_t c;      /* channels, >= 1 */
+    int32_t dtype;  /* F16 or BF16: x, f, g, y and their gradients */
+    int64_t ld;     /* elements from a token to the next in x, f, g, dx, df, dg, >= c:
+                       3 * c where they are thirds of one projection's output */
+    int64_t ldy;    /* the same in y and dy, >= c */
+} nnconv_recurrence_desc;
+
+/* Tokens between two states that the forward pass saves for the backward. */
+#define NNCONV_RECURRENCE_SAVE 64
+
+/* Bytes of `saved`: fp32 [n][ceil(t / NNCONV_RECURRENCE_SAVE)][c]. */
+nnconv_status nnconv_recurrence_saved_size(const nnconv_recurrence_desc *desc, size_t *bytes);
+
+/* Bytes of workspace of nnconv_recurrence_fwd (NNCONV_FWD) or
+ * nnconv_recurrence_bwd (NNCONV_DGRAD). */
+nnconv_status nnconv_recurrence_workspace_size(const nnconv_recurrence_desc *desc,
+                                               nnconv_pass pass, size_t *bytes);
+
+/* Forward.  x, f, g (may be NULL): token j of sequence i starts at element
+ * (i * t + j) * ld; y with ldy.  bias: fp32, [c], or NULL.  lengths: NULL or
+ * device int32 [n], taken into 0..t: tokens from the length on leave the
+ * state as it is and have y = 0 (their x, f and g may hold anything).
+ * h0: fp32 [n][c], NULL for zeros.  ht: NULL or fp32 [n][c], the state after
+ * the last token; it may be h0 itself: with t = 1 a call is one step of
+ * serving.  saved: NULL or what nnconv_recurrence_bwd needs.  No other output
+ * may overlap anything.  ws: 8-byte aligned; calls that may overlap in time
+ * need workspaces of their own.
+ * INVALID_ARG: sizes below the limits above, bad dtype, null x, f or y;
+ * UNSUPPORTED: dtype F32; WORKSPACE; MISALIGNED: pointers below their element
+ * size (ws: below 8). */
+nnconv_status nnconv_recurrence_fwd(const nnconv_recurrence_desc *desc, const void *x,
+                                    const void *f, const float *bias, const void *g,
+                                    const int32_t *lengths, const float *h0, void *y, float *ht,
+                                    float *saved, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Backward.  saved is the forward's.  dy: the gradient of y; dht: NULL or that
+ * of the last state.  With dh_t the gradient of h_t (its own y's and the next
+ * state's):
+ *   dx_t = (1 - a_t) dh_t,  df_t = a_t (1 - a_t) (h_(t-1) - x_t) dh_t,
+ *   dg_t = dy_t h_t d(g sigma(g))/dg,  dh0 = a_1 dh_1,
+ *   dbias = (accumulate ? dbias : 0) + inv_loss_scale * sum over tokens of df
+ * (df unrounded in the sum; the limit of z counts as the identity).  Tokens
+ * from the length on have zero gradients.  dx, df and, where g is given, dg
+ * are written; dh0 (fp32 [n][c], may be dht itself) and dbias (fp32 [c]) may be
+ * NULL.  Errors as the forward's and as nnconv_wgrad's for accumulate; null
+ * saved, dy, dx, df, or dg where g is given: INVALID_ARG. */
+nnconv_status nnconv_recurrence_bwd(const nnconv_recurrence_desc *desc, const void *x,
+                                    const void *f, const float *bias, const void *g,
+                                    const int32_t *lengths, const float *saved, const void *dy,
+                                    const float *dht, void *dx, void *df, void *dg, float *dh0,
+                                    float *dbias, float inv_loss_scale, int32_t accumulate,
+                                    int32_t *overflow_flag, void *ws, size_t ws_bytes,
+                                    void *hip_stream);
+
+/* AdamW over many tensors in one launch, in place of nnconv_sgd_update in the
+ * step above (and like it before nnconv_loss_scaler_update): with t the
+ * number of steps taken including this one and S the loss scale,
+ *   g = grad / S,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
+ *   master -= lr (m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps)
+ *                 + weight_decay * master)
+ *   w16 = round-to-nearest-even(master)
+ * in fp32, with m and v unrounded in the master's update.
+ *
+ * state_dtype F32: m and v are fp32 arrays.  F8: m is e4m3 (largest 448) and
+ * v e5m2 (largest 57344) codes, with one power of two for every
+ * NNCONV_ADAMW_BLOCK elements (m_scale, v_scale: bytes e that stand for
+ * 2^(e - 127), ceil(count / NNCONV_ADAMW_BLOCK) of them): the smallest one
+ * that brings the block's largest finite magnitude within range (0 for a block of
+ * zeros).  A change of v by 0.1 % is far below a code's spacing, and rounding to nearest
+ * would lose it in every step; codes are therefore rounded up or down at
+ * random, up with the probability of the part lost, so that they are right on
+ * average.  The random numbers are a hash of (seed, t, index of the tensor in the list,
+ * element), so a step can be repeated.  A v above 0 keeps a code above 0.
+ * A power of two as the scale keeps the codes' grid in place from step to
+ * step.  A value that is not finite has a NaN code. */
+#define NNCONV_ADAMW_BLOCK 64
+typedef struct {
+    float *master;        /* fp32, [count] */
+    const void *grad;     /* [count] of grad_dtype, loss-scaled */
+    void *w16;            /* NULL or [count] of w16_dtype: the working copy */
+    void *m, *v;          /* [count] of state_dtype */
+    uint8_t *m_scale, *v_scale; /* state_dtype F8 only */
+    int64_t count;        /* >= 0 */
+    float weight_decay;   /* finite */
+    int32_t grad_dtype;   /* F32, F16 or BF16 */
+    int32_t w16_dtype;    /* F16 or BF16 (ignored without w16) */
+    int32_t state_dtype;  /* F32 or F8 */
+} nnconv_adamw_tensor;
+
+/* A list of tensors laid out for nnconv_adamw_update.  Filled by
+ * nnconv_adamw_plan_init; holds no memory of its own. */
+typedef struct {
+    void *table;       /* the caller's device buffer */
+    int64_t chunks;
+    int32_t tensors;
+    int32_t reserved;
+} nnconv_adamw_plan;
+
+/* Bytes of device memory for the plan of `n` tensors. */
+nnconv_status nnconv_adamw_plan_size(const nnconv_adamw_tensor *tensors, int32_t n, size_t *bytes);
+
+/* Checks the list (a host array, not needed after the call), fills *plan and
+ * queues kernels that write the list to `table`, which has to
+ * live as long as the plan is used.  Once per set of tensors.
+ * INVALID_ARG: n < 0, null or negative members, bad dtypes, weight decay not
+ * finite; MISALIGNED: members below their element size, table below 16;
+ * WORKSPACE: table_bytes too small. */
+nnconv_status nnconv_adamw_plan_init(const nnconv_adamw_tensor *tensors, int32_t n, void *table,
+                                     size_t table_bytes, nnconv_adamw_plan *plan,
+                                     void *hip_stream);
+
+/* One step.  step: device int32, the number of steps taken so far (0 at
+ * first); the call adds 1.  state: the loss scaler's, or NULL (S = 1).
+ * overflow_flag: NULL or the step's device flag; where it is set the call
+ * changes nothing, step included.  Calls that may overlap in time need plans
+ * of their own.
+ * INVALID_ARG: null plan or step, lr or eps negative or not finite, betas outside
+ * [0, 1). */
+nnconv_status nnconv_adamw_update(const nnconv_adamw_plan *plan, int32_t *step, float lr,
+                                  float beta1, float beta2, float eps, uint32_t seed,
+                                  const nnconv_loss_scaler *state, const int32_t *overflow_flag,
+                                  void *hip_stream);
 
 #ifdef __cplusplus
 }

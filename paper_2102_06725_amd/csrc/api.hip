@@ -1931,3 +1931,308 @@ NNCONV_API nnconv_status nnconv_sgd_update(int64_t count, float *master, float *
                                         overflow_flag, lr, momentum_coef, weight_decay,
                                         (hipStream_t)hip_stream));
 }
+
+// ---------------------------------------------------------------------------
+// operators of a gated sequence block
+// ---------------------------------------------------------------------------
+
+static nnconv_status half_dtype(int32_t dtype) {
+    if (dtype == NNCONV_F16 || dtype == NNCONV_BF16) return NNCONV_OK;
+    return dtype == NNCONV_F32 || dtype == NNCONV_F8 ? NNCONV_ERR_UNSUPPORTED
+                                                     : NNCONV_ERR_INVALID_ARG;
+}
+
+static nnconv_status norm_check(const nnconv_rmsnorm_desc *d) {
+    if (!d || d->rows < 0 || d->c < 1) return NNCONV_ERR_INVALID_ARG;
+    if (!(d->eps >= 0.0f) || !__builtin_isfinite(d->eps)) return NNCONV_ERR_INVALID_ARG;
+    if (d->rows > MAX_ELEMS / d->c) return NNCONV_ERR_INVALID_ARG;
+    return half_dtype(d->dtype);
+}
+
+static nnconv_status norm_fwd(const nnconv_rmsnorm_desc *d, const void *x, const void *residual,
+                              const float *gain, void *sum, void *y, float *scales, float *rstd,
+                              bool q8, void *hip_stream) {
+    const nnconv_status st = norm_check(d);
+    if (st != NNCONV_OK) return st;
+    if (!x || !gain || !y) return NNCONV_ERR_INVALID_ARG;
+    if (!aligned(x, 2) || (residual && !aligned(residual, 2)) || !aligned(gain, 4) ||
+        (sum && !aligned(sum, 2)) || (rstd && !aligned(rstd, 4)) || !aligned(y, q8 ? 1 : 2) ||
+        (q8 && !aligned(scales, 4)))
+        return NNCONV_ERR_MISALIGNED;
+    if (d->rows == 0) return NNCONV_OK;
+    NormParams p;
+    p.rows = d->rows;
+    p.c = d->c;
+    p.group = q8 && d->group ? d->group : d->c;
+    p.groups = (int32_t)(((int64_t)d->c + p.group - 1) / p.group);
+    p.eps = d->eps;
+    p.x = x;
+    p.residual = residual;
+    p.gain = gain;
+    p.sum = sum;
+    p.y = y;
+    p.scales = scales;
+    p.rstd = rstd;
+    clear_stale_error();
+    return hip_status(launch_rmsnorm_fwd(d->dtype, p, q8, (hipStream_t)hip_stream));
+}
+
+NNCONV_API nnconv_status nnconv_rmsnorm_fwd(const nnconv_rmsnorm_desc *desc, const void *x,
+                                            const void *residual, const float *gain, void *sum,
+                                            void *y, float *rstd, void *hip_stream) {
+    return norm_fwd(desc, x, residual, gain, sum, y, nullptr, rstd, false, hip_stream);
+}
+
+NNCONV_API nnconv_status nnconv_rmsnorm_fwd_q8(const nnconv_rmsnorm_desc *desc, const void *x,
+                                               const void *residual, const float *gain, void *sum,
+                                               void *q, float *scales, float *rstd,
+                                               void *hip_stream) {
+    const nnconv_status st = norm_check(desc);
+    if (st != NNCONV_OK) return st;
+    if (!scales || (desc->group != 0 && desc->group != 32 && desc->group != 64 && desc->group != 128))
+        return NNCONV_ERR_INVALID_ARG;
+    return norm_fwd(desc, x, residual, gain, sum, q, scales, rstd, true, hip_stream);
+}
+
+static size_t norm_bwd_ws(const nnconv_rmsnorm_desc *d) {
+    const int64_t parts = rmsnorm_bwd_parts(d->rows, d->c);
+    return sizeof(float) * (size_t)((parts + colsum_extra(parts)) * d->c);
+}
+
+NNCONV_API nnconv_status nnconv_rmsnorm_workspace_size(const nnconv_rmsnorm_desc *desc,
+                                                       size_t *bytes) {
+    const nnconv_status st = norm_check(desc);
+    if (st != NNCONV_OK) return st;
+    if (!bytes) return NNCONV_ERR_INVALID_ARG;
+    *bytes = norm_bwd_ws(desc);
+    return NNCONV_OK;
+}
+
+NNCONV_API nnconv_status nnconv_rmsnorm_bwd(const nnconv_rmsnorm_desc *desc, const void *sum,
+                                            const void *dy, const void *dsum, const float *gain,
+                                            const float *rstd, void *dx, float *dgain,
+                                            float inv_loss_scale, int32_t accumulate,
+                                            int32_t *overflow_flag, void *ws, size_t ws_bytes,
+                                            void *hip_stream) {
+    const nnconv_status st = norm_check(desc);
+    if (st != NNCONV_OK) return st;
+    if (!sum || !dy || !gain || !rstd || !dx) return NNCONV_ERR_INVALID_ARG;
+    if (accumulate != 0 && accumulate != 1) return NNCONV_ERR_INVALID_ARG;
+    if (!aligned(sum, 2) || !aligned(dy, 2) || (dsum && !aligned(dsum, 2)) || !aligned(gain, 4) ||
+        !aligned(rstd, 4) || !aligned(dx, 2) || (dgain && !aligned(dgain, 4)) ||
+        (overflow_flag && !aligned(overflow_flag, 4)))
+        return NNCONV_ERR_MISALIGNED;
+    if (dgain) {
+        const size_t need = norm_bwd_ws(desc);
+        if (need > 0 && !ws) return NNCONV_ERR_INVALID_ARG;
+        if (ws_bytes < need) return NNCONV_ERR_WORKSPACE;
+        if (!aligned(ws, 4)) return NNCONV_ERR_MISALIGNED;
+    }
+    NormBwdParams p;
+    p.rows = desc->rows;
+    p.c = desc->c;
+    p.parts = rmsnorm_bwd_parts(desc->rows, desc->c);
+    p.sum = sum;
+    p.dy = dy;
+    p.dsum = dsum;
+    p.gain = gain;
+    p.rstd = rstd;
+    p.dx = dx;
+    p.part = dgain ? (float *)ws : nullptr;
+    hipStream_t s = (hipStream_t)hip_stream;
+    clear_stale_error();
+    TRY_HIP(launch_rmsnorm_bwd(desc->dtype, p, s));
+    if (!dgain) return NNCONV_OK;
+    return hip_status(launch_colsum(p.part, p.parts, p.c, p.part + (int64_t)p.parts * p.c, dgain,
+                                    inv_loss_scale, accumulate, overflow_flag, s));
+}
+
+static nnconv_status rec_check(const nnconv_recurrence_desc *d, RecParams *p) {
+    if (!d || d->n < 0 || d->t < 0 || d->c < 1 || d->ld < d->c || d->ldy < d->c)
+        return NNCONV_ERR_INVALID_ARG;
+    const int64_t ld = d->ld > d->ldy ? d->ld : d->ldy;
+    const int64_t tokens = (int64_t)d->n * d->t;
+    if (ld > MAX_ELEMS || tokens > MAX_ELEMS / ld) return NNCONV_ERR_INVALID_ARG;
+    if ((int64_t)d->n * d->c > MAX_ELEMS) return NNCONV_ERR_INVALID_ARG;
+    memset(p, 0, sizeof(*p));
+    p->n = d->n;
+    p->t = d->t;
+    p->c = d->c;
+    p->ld = d->ld;
+    p->ldy = d->ldy;
+    return half_dtype(d->dtype);
+}
+
+NNCONV_API nnconv_status nnconv_recurrence_saved_size(const nnconv_recurrence_desc *desc,
+                                                      size_t *bytes) {
+    RecParams p;
+    const nnconv_status st = rec_check(desc, &p);
+    if (st != NNCONV_OK) return st;
+    if (!bytes) return NNCONV_ERR_INVALID_ARG;
+    const int64_t chunks = ((int64_t)p.t + NNCONV_RECURRENCE_SAVE - 1) / NNCONV_RECURRENCE_SAVE;
+    *bytes = sizeof(float) * (size_t)(p.n * chunks * p.c);
+    return NNCONV_OK;
+}
+
+NNCONV_API nnconv_status nnconv_recurrence_workspace_size(const nnconv_recurrence_desc *desc,
+                                                          nnconv_pass pass, size_t *bytes) {
+    RecParams p;
+    const nnconv_status st = rec_check(desc, &p);
+    if (st != NNCONV_OK) return st;
+    if (!bytes || (pass != NNCONV_FWD && pass != NNCONV_DGRAD)) return NNCONV_ERR_INVALID_ARG;
+    *bytes = recurrence_ws(p, pass == NNCONV_DGRAD);
+    return NNCONV_OK;
+}
+
+static nnconv_status rec_workspace(const RecParams &p, bool backward, void *ws, size_t ws_bytes) {
+    const size_t need = recurrence_ws(p, backward);
+    if (need == 0) return NNCONV_OK;
+    if (!ws) return NNCONV_ERR_INVALID_ARG;
+    if (ws_bytes < need) return NNCONV_ERR_WORKSPACE;
+    return aligned(ws, 8) ? NNCONV_OK : NNCONV_ERR_MISALIGNED;
+}
+
+NNCONV_API nnconv_status nnconv_recurrence_fwd(const nnconv_recurrence_desc *desc, const void *x,
+                                               const void *f, const float *bias, const void *g,
+                                               const int32_t *lengths, const float *h0, void *y,
+                                               float *ht, float *saved, void *ws, size_t ws_bytes,
+                                               void *hip_stream) {
+    RecParams p;
+    nnconv_status st = rec_check(desc, &p);
+    if (st != NNCONV_OK) return st;
+    if (!x || !f || !y) return NNCONV_ERR_INVALID_ARG;
+    if (!aligned(x, 2) || !aligned(f, 2) || (g && !aligned(g, 2)) || !aligned(y, 2) ||
+        (bias && !aligned(bias, 4)) || (lengths && !aligned(lengths, 4)) ||
+        (h0 && !aligned(h0, 4)) || (ht && !aligned(ht, 4)) || (saved && !aligned(saved, 4)))
+        return NNCONV_ERR_MISALIGNED;
+    st = rec_workspace(p, false, ws, ws_bytes);
+    if (st != NNCONV_OK) return st;
+    p.x = x;
+    p.f = f;
+    p.g = g;
+    p.bias = bias;
+    p.lengths = lengths;
+    p.h0 = h0;
+    p.y = y;
+    p.ht = ht;
+    p.saved = saved;
+    p.ws = ws;
+    clear_stale_error();
+    return hip_status(launch_recurrence_fwd(desc->dtype, p, (hipStream_t)hip_stream));
+}
+
+NNCONV_API nnconv_status nnconv_recurrence_bwd(
+    const nnconv_recurrence_desc *desc, const void *x, const void *f, const float *bias,
+    const void *g, const int32_t *lengths, const float *saved, const void *dy, const float *dht,
+    void *dx, void *df, void *dg, float *dh0, float *dbias, float inv_loss_scale,
+    int32_t accumulate, int32_t *overflow_flag, void *ws, size_t ws_bytes, void *hip_stream) {
+    RecParams p;
+    nnconv_status st = rec_check(desc, &p);
+    if (st != NNCONV_OK) return st;
+    if (!x || !f || !saved || !dy || !dx || !df || (g && !dg)) return NNCONV_ERR_INVALID_ARG;
+    if (accumulate != 0 && accumulate != 1) return NNCONV_ERR_INVALID_ARG;
+    if (!aligned(x, 2) || !aligned(f, 2) || (g && (!aligned(g, 2) || !aligned(dg, 2))) ||
+        !aligned(dy, 2) || !aligned(dx, 2) || !aligned(df, 2) || (bias && !aligned(bias, 4)) ||
+        (lengths && !aligned(lengths, 4)) || !aligned(saved, 4) || (dht && !aligned(dht, 4)) ||
+        (dh0 && !aligned(dh0, 4)) || (dbias && !aligned(dbias, 4)) ||
+        (overflow_flag && !aligned(overflow_flag, 4)))
+        return NNCONV_ERR_MISALIGNED;
+    st = rec_workspace(p, true, ws, ws_bytes);
+    if (st != NNCONV_OK) return st;
+    p.x = x;
+    p.f = f;
+    p.g = g;
+    p.bias = bias;
+    p.lengths = lengths;
+    p.saved = const_cast<float *>(saved);
+    p.dy = dy;
+    p.dht = dht;
+    p.dx = dx;
+    p.df = df;
+    p.dg = dg;
+    p.dh0 = dh0;
+    p.ws = ws;
+    const int64_t parts = recurrence_bwd_parts(p);
+    p.part = dbias ? (float *)ws : nullptr;
+    hipStream_t s = (hipStream_t)hip_stream;
+    clear_stale_error();
+    TRY_HIP(launch_recurrence_bwd(desc->dtype, p, s));
+    if (!dbias) return NNCONV_OK;
+    return hip_status(launch_colsum(p.part, parts, p.c, p.part + parts * p.c, dbias,
+                                    inv_loss_scale, accumulate, overflow_flag, s));
+}
+
+static nnconv_status adamw_check(const nnconv_adamw_tensor *t, int32_t n, int64_t *chunks) {
+    if (n < 0 || (n > 0 && !t)) return NNCONV_ERR_INVALID_ARG;
+    *chunks = 0;
+    for (int32_t i = 0; i < n; ++i) {
+        const nnconv_adamw_tensor &e = t[i];
+        if (e.count < 0 || e.count > MAX_ELEMS) return NNCONV_ERR_INVALID_ARG;
+        if (!__builtin_isfinite(e.weight_decay)) return NNCONV_ERR_INVALID_ARG;
+        if (e.state_dtype != NNCONV_F32 && e.state_dtype != NNCONV_F8) return NNCONV_ERR_INVALID_ARG;
+        if (e.grad_dtype != NNCONV_F32 && e.grad_dtype != NNCONV_F16 && e.grad_dtype != NNCONV_BF16)
+            return NNCONV_ERR_INVALID_ARG;
+        if (e.w16 && e.w16_dtype != NNCONV_F16 && e.w16_dtype != NNCONV_BF16)
+            return NNCONV_ERR_INVALID_ARG;
+        if (e.count == 0) continue;
+        const bool f8 = e.state_dtype == NNCONV_F8;
+        if (!e.master || !e.grad || !e.m || !e.v || (f8 && (!e.m_scale || !e.v_scale)))
+            return NNCONV_ERR_INVALID_ARG;
+        if (!aligned(e.master, 4) || !aligned(e.grad, e.grad_dtype == NNCONV_F32 ? 4 : 2) ||
+            (e.w16 && !aligned(e.w16, 2)) || (!f8 && (!aligned(e.m, 4) || !aligned(e.v, 4))))
+            return NNCONV_ERR_MISALIGNED;
+        *chunks += (e.count + ADAMW_CHUNK - 1) / ADAMW_CHUNK;
+    }
+    return *chunks > 0x7FFFFFFF ? NNCONV_ERR_INVALID_ARG : NNCONV_OK;
+}
+
+static size_t adamw_bytes(int32_t n, int64_t chunks) {
+    return (size_t)n * sizeof(nnconv_adamw_tensor) + (size_t)chunks * sizeof(AdamwChunk);
+}
+
+NNCONV_API nnconv_status nnconv_adamw_plan_size(const nnconv_adamw_tensor *tensors, int32_t n,
+                                                size_t *bytes) {
+    int64_t chunks;
+    const nnconv_status st = adamw_check(tensors, n, &chunks);
+    if (st != NNCONV_OK) return st;
+    if (!bytes) return NNCONV_ERR_INVALID_ARG;
+    *bytes = adamw_bytes(n, chunks);
+    return NNCONV_OK;
+}
+
+NNCONV_API nnconv_status nnconv_adamw_plan_init(const nnconv_adamw_tensor *tensors, int32_t n,
+                                                void *table, size_t table_bytes,
+                                                nnconv_adamw_plan *plan, void *hip_stream) {
+    int64_t chunks;
+    const nnconv_status st = adamw_check(tensors, n, &chunks);
+    if (st != NNCONV_OK) return st;
+    const size_t need = adamw_bytes(n, chunks);
+    if (!plan || (need > 0 && !table)) return NNCONV_ERR_INVALID_ARG;
+    if (table_bytes < need) return NNCONV_ERR_WORKSPACE;
+    if (!aligned(table, 16)) return NNCONV_ERR_MISALIGNED;
+    clear_stale_error();
+    TRY_HIP(launch_adamw_plan(tensors, n, adamw_table(table, n), (hipStream_t)hip_stream));
+    plan->table = table;
+    plan->chunks = chunks;
+    plan->tensors = n;
+    plan->reserved = 0;
+    return NNCONV_OK;
+}
+
+NNCONV_API nnconv_status nnconv_adamw_update(const nnconv_adamw_plan *plan, int32_t *step, float lr,
+                                             float beta1, float beta2, float eps, uint32_t seed,
+                                             const nnconv_loss_scaler *state,
+                                             const int32_t *overflow_flag, void *hip_stream) {
+    if (!plan || !step || plan->tensors < 0 || plan->chunks < 0 || (plan->chunks > 0 && !plan->table))
+        return NNCONV_ERR_INVALID_ARG;
+    if (!(lr >= 0.0f) || !__builtin_isfinite(lr) || !(eps >= 0.0f) || !__builtin_isfinite(eps) ||
+        !(beta1 >= 0.0f && beta1 < 1.0f) || !(beta2 >= 0.0f && beta2 < 1.0f))
+        return NNCONV_ERR_INVALID_ARG;
+    if (!aligned(step, 4) || (state && !aligned(state, 4)) ||
+        (overflow_flag && !aligned(overflow_flag, 4)) || !aligned(plan->table, 16))
+        return NNCONV_ERR_MISALIGNED;
+    clear_stale_error();
+    return hip_status(launch_adamw(adamw_table(plan->table, plan->tensors), plan->chunks, step, lr,
+                                   beta1, beta2, eps, seed, state, overflow_flag,
+                                   (hipStream_t)hip_stream));
+}

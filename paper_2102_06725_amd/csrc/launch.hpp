@@ -418,4 +418,72 @@ hipError_t launch_sgd_update(int64_t count, float *master, float *mom, void *w16
                              const float *grad, const nnconv_loss_scaler *state,
                              const int32_t *flag, float lr, float mu, float wd, hipStream_t st);
 
+// --- operators of a gated sequence block ------------------------------------
+
+// Root-mean-square norm of dense rows [rows][c].
+struct NormParams {
+    int64_t rows;
+    int32_t c;
+    int32_t group, groups;  // 8-bit output: channels with one scale (c for a whole row), scales per row
+    float eps;
+    const void *x, *residual;
+    const float *gain;
+    void *sum, *y;
+    float *scales, *rstd;
+};
+struct NormBwdParams {
+    int64_t rows;
+    int32_t c, parts;
+    const void *sum, *dy, *dsum;
+    const float *gain, *rstd;
+    void *dx;
+    float *part;  // dgain partials [parts][c], or null
+};
+int32_t rmsnorm_bwd_parts(int64_t rows, int32_t c);
+hipError_t launch_rmsnorm_fwd(int dtype, const NormParams &p, bool q8, hipStream_t st);
+hipError_t launch_rmsnorm_bwd(int dtype, const NormBwdParams &p, hipStream_t st);
+
+// out = (accumulate ? out : 0) + inv_scale * column sums of part[parts][c] in
+// a fixed order; extra: colsum_extra(parts) * c floats of scratch.
+int64_t colsum_extra(int64_t parts);
+hipError_t launch_colsum(const float *part, int64_t parts, int32_t c, float *extra, float *out,
+                         float inv_scale, int accumulate, int32_t *flag, hipStream_t st);
+
+// Gated linear recurrence.
+struct RecParams {
+    int32_t n, t, c;
+    int64_t ld, ldy;
+    const void *x, *f, *g;
+    const float *bias;
+    const int32_t *lengths;
+    const float *h0;          // forward
+    void *y;
+    float *ht, *saved;
+    const void *dy;           // backward
+    const float *dht;
+    void *dx, *df, *dg;
+    float *dh0, *part;        // part: dbias partials, or null
+    void *ws;
+};
+int64_t recurrence_bwd_parts(const RecParams &p);
+size_t recurrence_ws(const RecParams &p, bool backward);
+hipError_t launch_recurrence_fwd(int dtype, const RecParams &p, hipStream_t st);
+hipError_t launch_recurrence_bwd(int dtype, const RecParams &p, hipStream_t st);
+
+// AdamW over a list of tensors, cut into chunks of ADAMW_CHUNK elements.
+constexpr int64_t ADAMW_CHUNK = 4096;
+struct AdamwChunk {
+    int32_t tensor, index;
+};
+struct AdamwTable {
+    nnconv_adamw_tensor *tensors;
+    AdamwChunk *chunks;
+};
+AdamwTable adamw_table(void *buffer, int32_t tensors);
+hipError_t launch_adamw_plan(const nnconv_adamw_tensor *tensors, int32_t n, const AdamwTable &tab,
+                             hipStream_t st);
+hipError_t launch_adamw(const AdamwTable &tab, int64_t chunks, int32_t *step, float lr, float beta1,
+                        float beta2, float eps, uint32_t seed, const nnconv_loss_scaler *state,
+                        const int32_t *flag, hipStream_t st);
+
 }  // namespace nnconv

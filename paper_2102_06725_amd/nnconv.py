@@ -29,10 +29,13 @@ NNCONV_NHWC = 1
 NNCONV_F16 = 0
 NNCONV_BF16 = 1
 NNCONV_F32 = 2
+NNCONV_F8 = 3
 NNCONV_FWD = 0
 NNCONV_DGRAD = 1
 NNCONV_WGRAD = 2
 NNCONV_NOALLOC_WS_BYTES = 64 * 1024 * 1024
+NNCONV_RECURRENCE_SAVE = 64
+NNCONV_ADAMW_BLOCK = 64
 # nnconv_tile: tiles of the implicit-GEMM forward / backward-data kernel
 NNCONV_TILE_256x256_8W = 0
 NNCONV_TILE_128x128_2S = 1
@@ -71,7 +74,11 @@ EXPORTS = ("nnconv_version", "nnconv_last_hip_error", "nnconv_status_string", "n
            "nnconv_dgrad_tile", "nnconv_wgrad", "nnconv_wgrad_noalloc",
            "nnconv_nchw_to_nhwc", "nnconv_nhwc_to_nchw", "nnconv_pad_channels",
            "nnconv_weight_kcrs_to_krsc", "nnconv_weight_krsc_to_kcrs",
-           "nnconv_loss_scaler_init", "nnconv_loss_scaler_update", "nnconv_sgd_update")
+           "nnconv_loss_scaler_init", "nnconv_loss_scaler_update", "nnconv_sgd_update",
+           "nnconv_rmsnorm_fwd", "nnconv_rmsnorm_fwd_q8", "nnconv_rmsnorm_workspace_size",
+           "nnconv_rmsnorm_bwd", "nnconv_recurrence_saved_size",
+           "nnconv_recurrence_workspace_size", "nnconv_recurrence_fwd", "nnconv_recurrence_bwd",
+           "nnconv_adamw_plan_size", "nnconv_adamw_plan_init", "nnconv_adamw_update")
 
 
 class nnconv_desc(ctypes.Structure):
@@ -85,6 +92,29 @@ class nnconv_loss_scaler(ctypes.Structure):
     _fields_ = [("scale", ctypes.c_float), ("factor", ctypes.c_float),
                 ("interval", ctypes.c_int32), ("counter", ctypes.c_int32),
                 ("skipped", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class nnconv_rmsnorm_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("c", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("group", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class nnconv_recurrence_desc(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("t", ctypes.c_int32), ("c", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("ld", ctypes.c_int64), ("ldy", ctypes.c_int64)]
+
+
+class nnconv_adamw_tensor(ctypes.Structure):
+    _fields_ = [("master", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("w16", ctypes.c_void_p),
+                ("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("count", ctypes.c_int64),
+                ("weight_decay", ctypes.c_float), ("grad_dtype", ctypes.c_int32),
+                ("w16_dtype", ctypes.c_int32), ("state_dtype", ctypes.c_int32)]
+
+
+class nnconv_adamw_plan(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("chunks", ctypes.c_int64),
+                ("tensors", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class NNConvError(RuntimeError):
@@ -148,6 +178,21 @@ def load(path: str | None = None):
     lib.nnconv_loss_scaler_update.argtypes = [_VP, _VP, _VP]
     lib.nnconv_sgd_update.argtypes = [_I64, _VP, _VP, _VP, _I32, _VP, _VP, _VP, ctypes.c_float,
                                       ctypes.c_float, ctypes.c_float, _VP]
+    _F32, _SZ, _SZP = ctypes.c_float, ctypes.c_size_t, ctypes.POINTER(ctypes.c_size_t)
+    norm, rec = ctypes.POINTER(nnconv_rmsnorm_desc), ctypes.POINTER(nnconv_recurrence_desc)
+    tens, plan = ctypes.POINTER(nnconv_adamw_tensor), ctypes.POINTER(nnconv_adamw_plan)
+    lib.nnconv_rmsnorm_fwd.argtypes = [norm] + [_VP] * 7
+    lib.nnconv_rmsnorm_fwd_q8.argtypes = [norm] + [_VP] * 8
+    lib.nnconv_rmsnorm_workspace_size.argtypes = [norm, _SZP]
+    lib.nnconv_rmsnorm_bwd.argtypes = [norm] + [_VP] * 7 + [_F32, _I32, _VP, _VP, _SZ, _VP]
+    lib.nnconv_recurrence_saved_size.argtypes = [rec, _SZP]
+    lib.nnconv_recurrence_workspace_size.argtypes = [rec, ctypes.c_int, _SZP]
+    lib.nnconv_recurrence_fwd.argtypes = [rec] + [_VP] * 10 + [_SZ, _VP]
+    lib.nnconv_recurrence_bwd.argtypes = [rec] + [_VP] * 13 + [_F32, _I32, _VP, _VP, _SZ, _VP]
+    lib.nnconv_adamw_plan_size.argtypes = [tens, _I32, _SZP]
+    lib.nnconv_adamw_plan_init.argtypes = [tens, _I32, _VP, _SZ, plan, _VP]
+    lib.nnconv_adamw_update.argtypes = [plan, _VP, _F32, _F32, _F32, _F32, ctypes.c_uint32, _VP,
+                                        _VP, _VP]
     for f in EXPORTS[3:]:
         getattr(lib, f).restype = ctypes.c_int
     if path is None:
@@ -261,6 +306,72 @@ def nnconv_sgd_update(count, master, momentum, w16, w16_dtype, grad, state, over
                                     float(weight_decay), stream)
 
 
+def nnconv_rmsnorm_fwd(desc, x, residual, gain, sum, y, rstd, stream) -> int:
+    return load().nnconv_rmsnorm_fwd(ctypes.byref(desc), x, residual, gain, sum, y, rstd, stream)
+
+
+def nnconv_rmsnorm_fwd_q8(desc, x, residual, gain, sum, q, scales, rstd, stream) -> int:
+    return load().nnconv_rmsnorm_fwd_q8(ctypes.byref(desc), x, residual, gain, sum, q, scales,
+                                        rstd, stream)
+
+
+def nnconv_rmsnorm_workspace_size(desc):
+    b = ctypes.c_size_t()
+    st = load().nnconv_rmsnorm_workspace_size(ctypes.byref(desc), ctypes.byref(b))
+    return st, b.value
+
+
+def nnconv_rmsnorm_bwd(desc, sum, dy, dsum, gain, rstd, dx, dgain, inv_loss_scale, accumulate,
+                       overflow_flag, ws, ws_bytes, stream) -> int:
+    return load().nnconv_rmsnorm_bwd(ctypes.byref(desc), sum, dy, dsum, gain, rstd, dx, dgain,
+                                     float(inv_loss_scale), int(accumulate), overflow_flag, ws,
+                                     ws_bytes, stream)
+
+
+def nnconv_recurrence_saved_size(desc):
+    b = ctypes.c_size_t()
+    st = load().nnconv_recurrence_saved_size(ctypes.byref(desc), ctypes.byref(b))
+    return st, b.value
+
+
+def nnconv_recurrence_workspace_size(desc, pass_: int):
+    b = ctypes.c_size_t()
+    st = load().nnconv_recurrence_workspace_size(ctypes.byref(desc), int(pass_), ctypes.byref(b))
+    return st, b.value
+
+
+def nnconv_recurrence_fwd(desc, x, f, bias, g, lengths, h0, y, ht, saved, ws, ws_bytes,
+                          stream) -> int:
+    return load().nnconv_recurrence_fwd(ctypes.byref(desc), x, f, bias, g, lengths, h0, y, ht,
+                                        saved, ws, ws_bytes, stream)
+
+
+def nnconv_recurrence_bwd(desc, x, f, bias, g, lengths, saved, dy, dht, dx, df, dg, dh0, dbias,
+                          inv_loss_scale, accumulate, overflow_flag, ws, ws_bytes, stream) -> int:
+    return load().nnconv_recurrence_bwd(ctypes.byref(desc), x, f, bias, g, lengths, saved, dy, dht,
+                                        dx, df, dg, dh0, dbias, float(inv_loss_scale),
+                                        int(accumulate), overflow_flag, ws, ws_bytes, stream)
+
+
+def nnconv_adamw_plan_size(tensors, n):
+    """tensors: a ctypes array of nnconv_adamw_tensor (None for n = 0)."""
+    b = ctypes.c_size_t()
+    st = load().nnconv_adamw_plan_size(tensors, int(n), ctypes.byref(b))
+    return st, b.value
+
+
+def nnconv_adamw_plan_init(tensors, n, table, table_bytes, plan, stream) -> int:
+    return load().nnconv_adamw_plan_init(tensors, int(n), table, table_bytes, ctypes.byref(plan),
+                                         stream)
+
+
+def nnconv_adamw_update(plan, step, lr, beta1, beta2, eps, seed, state, overflow_flag,
+                        stream) -> int:
+    return load().nnconv_adamw_update(ctypes.byref(plan), step, float(lr), float(beta1),
+                                      float(beta2), float(eps), int(seed), state, overflow_flag,
+                                      stream)
+
+
 def check(status: int, what: str = "") -> None:
     if status != NNCONV_OK:
         raise NNConvError(status, what)
@@ -329,3 +440,168 @@ class Conv2d:
         check(nnconv_wgrad(self.desc, x.data_ptr(), dy.data_ptr(), dw.data_ptr(), dw_dtype,
                            inv_loss_scale, accumulate, flag, ws.data_ptr(), nb,
                            self._stream(stream)), "nnconv_wgrad")
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+class _Workspaces:
+    """Workspaces of a handle, one per stream and kind, so that calls on several streams
+    do not share one.  A torch tensor each, allocated on first use."""
+
+    def __init__(self):
+        self._held = {}
+
+    def get(self, kind, stream, nbytes, device):
+        t = self._held.get((kind, stream))
+        if t is None or t.numel() < nbytes:
+            import torch
+            t = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=device)
+            self._held[kind, stream] = t
+        return t
+
+
+class RMSNorm:
+    """Root-mean-square norm of [rows][c] torch tensors (dense, on the current device), with
+    the residual's addition: nnconv_rmsnorm_*.  `rows` may be changed between calls (a serving
+    program's batch)."""
+
+    def __init__(self, rows, c, dtype=NNCONV_F16, eps=1e-6, group=0):
+        self.desc = nnconv_rmsnorm_desc(rows, c, dtype, group, eps)
+        self._ws = _Workspaces()
+
+    @property
+    def rows(self):
+        return self.desc.rows
+
+    @rows.setter
+    def rows(self, rows):
+        self.desc.rows = rows
+
+    def fwd(self, x, gain, y, residual=None, sum=None, rstd=None, stream=None):
+        check(nnconv_rmsnorm_fwd(self.desc, x.data_ptr(), _ptr(residual), gain.data_ptr(),
+                                 _ptr(sum), y.data_ptr(), _ptr(rstd),
+                                 Conv2d._stream(stream)), "nnconv_rmsnorm_fwd")
+
+    def fwd_q8(self, x, gain, q, scales, residual=None, sum=None, rstd=None, stream=None):
+        check(nnconv_rmsnorm_fwd_q8(self.desc, x.data_ptr(), _ptr(residual), gain.data_ptr(),
+                                    _ptr(sum), q.data_ptr(), scales.data_ptr(), _ptr(rstd),
+                                    Conv2d._stream(stream)), "nnconv_rmsnorm_fwd_q8")
+
+    def bwd(self, sum, dy, gain, rstd, dx, dgain=None, dsum=None, inv_loss_scale=1.0,
+            accumulate=0, overflow_flag=None, stream=None):
+        stream = Conv2d._stream(stream)
+        ws, nb = None, 0
+        if dgain is not None:
+            st, nb = nnconv_rmsnorm_workspace_size(self.desc)
+            check(st, "nnconv_rmsnorm_workspace_size")
+            ws = self._ws.get("bwd", stream, nb, sum.device)
+        check(nnconv_rmsnorm_bwd(self.desc, sum.data_ptr(), dy.data_ptr(), _ptr(dsum),
+                                 gain.data_ptr(), rstd.data_ptr(), dx.data_ptr(), _ptr(dgain),
+                                 inv_loss_scale, accumulate, _ptr(overflow_flag), _ptr(ws), nb,
+                                 stream), "nnconv_rmsnorm_bwd")
+
+
+class GatedRecurrence:
+    """Gated linear recurrence over n sequences of t tokens with c channels:
+    nnconv_recurrence_*.  ld and ldy: elements between the tokens of x, f, g (3 * c for the
+    thirds of one projection's output, passed as views) and of y.  `n` and `t` may be changed
+    between calls."""
+
+    def __init__(self, n, t, c, ld=None, ldy=None, dtype=NNCONV_F16):
+        self.desc = nnconv_recurrence_desc(n, t, c, dtype, c if ld is None else ld,
+                                           c if ldy is None else ldy)
+        self._ws = _Workspaces()
+
+    @property
+    def n(self):
+        return self.desc.n
+
+    @n.setter
+    def n(self, n):
+        self.desc.n = n
+
+    @property
+    def t(self):
+        return self.desc.t
+
+    @t.setter
+    def t(self, t):
+        self.desc.t = t
+
+    def saved(self, device="cuda"):
+        """A tensor for the states that fwd saves for bwd."""
+        import torch
+        st, nb = nnconv_recurrence_saved_size(self.desc)
+        check(st, "nnconv_recurrence_saved_size")
+        return torch.empty(max(nb // 4, 1), dtype=torch.float32, device=device)
+
+    def _workspace(self, pass_, stream, device):
+        st, nb = nnconv_recurrence_workspace_size(self.desc, pass_)
+        check(st, "nnconv_recurrence_workspace_size")
+        return (None, 0) if nb == 0 else (self._ws.get(pass_, stream, nb, device).data_ptr(), nb)
+
+    def fwd(self, x, f, bias, y, g=None, lengths=None, h0=None, ht=None, saved=None, stream=None):
+        stream = Conv2d._stream(stream)
+        ws, nb = self._workspace(NNCONV_FWD, stream, x.device)
+        check(nnconv_recurrence_fwd(self.desc, x.data_ptr(), f.data_ptr(), _ptr(bias), _ptr(g),
+                                    _ptr(lengths), _ptr(h0), y.data_ptr(), _ptr(ht), _ptr(saved),
+                                    ws, nb, stream), "nnconv_recurrence_fwd")
+
+    def bwd(self, x, f, bias, saved, dy, dx, df, g=None, dg=None, lengths=None, dht=None, dh0=None,
+            dbias=None, inv_loss_scale=1.0, accumulate=0, overflow_flag=None, stream=None):
+        stream = Conv2d._stream(stream)
+        ws, nb = self._workspace(NNCONV_DGRAD, stream, x.device)
+        check(nnconv_recurrence_bwd(self.desc, x.data_ptr(), f.data_ptr(), _ptr(bias), _ptr(g),
+                                    _ptr(lengths), saved.data_ptr(), dy.data_ptr(), _ptr(dht),
+                                    dx.data_ptr(), df.data_ptr(), _ptr(dg), _ptr(dh0),
+                                    _ptr(dbias), inv_loss_scale, accumulate, _ptr(overflow_flag),
+                                    ws, nb, stream), "nnconv_recurrence_bwd")
+
+
+class AdamW:
+    """AdamW over a list of tensors: nnconv_adamw_*.
+
+    Each entry of `tensors` is a dict with master, grad, m, v (and w16; m_scale and v_scale with
+    8-bit moments) as dense torch tensors on one device, and weight_decay.  Moments in 8 bits are
+    torch.float8_e4m3fn (m) and torch.float8_e5m2 (v), or uint8, with a byte of scale for every
+    NNCONV_ADAMW_BLOCK elements.  The tensors are kept: the list holds their addresses."""
+
+    def __init__(self, tensors, seed=0, stream=None):
+        import torch
+        codes = {torch.float32: NNCONV_F32, torch.float16: NNCONV_F16, torch.bfloat16: NNCONV_BF16}
+        self.tensors, self.seed = list(tensors), seed
+        n = len(self.tensors)
+        arr = (nnconv_adamw_tensor * max(n, 1))()
+        for a, t in zip(arr, self.tensors):
+            every = {k: t.get(k) for k in ("master", "grad", "w16", "m", "v", "m_scale", "v_scale")}
+            count = every["master"].numel()
+            f8 = every["m_scale"] is not None
+            blocks = -(-count // NNCONV_ADAMW_BLOCK)
+            for k, v in every.items():
+                if v is None:
+                    continue
+                if not v.is_contiguous() or v.numel() != (blocks if k.endswith("_scale") else count):
+                    raise ValueError("AdamW: %s has another size than the master, or is not dense" % k)
+                if v.element_size() != (1 if f8 and k[0] in "mv" and k != "master" else
+                                        2 if k == "w16" else v.element_size() if k == "grad" else 4):
+                    raise ValueError("AdamW: %s has type %s" % (k, v.dtype))
+                setattr(a, k, v.data_ptr())
+            a.count, a.weight_decay = count, float(t.get("weight_decay", 0.0))
+            a.grad_dtype = codes.get(every["grad"].dtype, -1)
+            a.w16_dtype = NNCONV_F16 if every["w16"] is None else codes.get(every["w16"].dtype, -1)
+            a.state_dtype = NNCONV_F8 if f8 else NNCONV_F32
+        st, nb = nnconv_adamw_plan_size(arr, n)
+        check(st, "nnconv_adamw_plan_size")
+        device = self.tensors[0]["master"].device if n else "cuda"
+        self._table = torch.empty(max(nb, 1), dtype=torch.uint8, device=device)
+        self.plan = nnconv_adamw_plan()
+        check(nnconv_adamw_plan_init(arr, n, self._table.data_ptr(), nb, self.plan,
+                                     Conv2d._stream(stream)), "nnconv_adamw_plan_init")
+
+    def step(self, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, state=None, overflow_flag=None,
+             stream=None):
+        check(nnconv_adamw_update(self.plan, step.data_ptr(), lr, beta1, beta2, eps, self.seed,
+                                  _ptr(state), _ptr(overflow_flag), Conv2d._stream(stream)),
+              "nnconv_adamw_update")

@@ -1,0 +1,150 @@
+"""Refusals and sizes of the sequence block's operators: every call here fails
+its checks (or has nothing to do) before anything is queued."""
+import ctypes
+
+import pytest
+
+from paper_2102_06725_amd import nnconv as nc
+
+FAKE = 0x100000  # never dereferenced
+INV, UNS = nc.NNCONV_ERR_INVALID_ARG, nc.NNCONV_ERR_UNSUPPORTED
+MIS, WSP, OK = nc.NNCONV_ERR_MISALIGNED, nc.NNCONV_ERR_WORKSPACE, nc.NNCONV_OK
+
+
+def test_struct_sizes():
+    assert ctypes.sizeof(nc.nnconv_rmsnorm_desc) == 24
+    assert ctypes.sizeof(nc.nnconv_recurrence_desc) == 32
+    assert ctypes.sizeof(nc.nnconv_adamw_tensor) == 80
+    assert ctypes.sizeof(nc.nnconv_adamw_plan) == 24
+
+
+def norm(rows=4, c=16, dtype=nc.NNCONV_F16, group=0, eps=1e-6):
+    return nc.nnconv_rmsnorm_desc(rows, c, dtype, group, eps)
+
+
+def fwd(d, x=FAKE, res=None, gain=FAKE, s=None, y=FAKE, rstd=None):
+    return nc.nnconv_rmsnorm_fwd(d, x, res, gain, s, y, rstd, None)
+
+
+def q8(d, q=FAKE, scales=FAKE, x=FAKE):
+    return nc.nnconv_rmsnorm_fwd_q8(d, x, None, FAKE, None, q, scales, None, None)
+
+
+def bwd(d, s=FAKE, dy=FAKE, dsum=None, gain=FAKE, rstd=FAKE, dx=FAKE, dgain=FAKE, acc=0, flag=None, ws=FAKE, nb=1 << 40):
+    return nc.nnconv_rmsnorm_bwd(d, s, dy, dsum, gain, rstd, dx, dgain, 1.0, acc, flag, ws, nb, None)
+
+
+@pytest.mark.parametrize("kw", [dict(rows=-1), dict(c=0), dict(dtype=9), dict(eps=-1.0), dict(eps=float("nan")),
+                                dict(eps=float("inf")), dict(rows=1 << 40, c=2)])
+def test_norm_descriptors(nnlib, kw):
+    d = norm(**kw)
+    assert fwd(d) == q8(d) == bwd(d) == nc.nnconv_rmsnorm_workspace_size(d)[0] == INV
+
+
+def test_norm_refusals(nnlib):
+    d = norm()
+    assert fwd(norm(dtype=nc.NNCONV_F32)) == bwd(norm(dtype=nc.NNCONV_F32)) == UNS
+    assert fwd(d, x=None) == fwd(d, gain=None) == fwd(d, y=None) == INV
+    assert fwd(d, x=FAKE + 1) == fwd(d, res=FAKE + 1) == fwd(d, gain=FAKE + 2) == MIS
+    assert fwd(d, s=FAKE + 1) == fwd(d, y=FAKE + 1) == fwd(d, rstd=FAKE + 2) == MIS
+    for group in (-1, 1, 16, 48, 256):
+        assert q8(norm(group=group)) == INV
+    assert q8(d, scales=None) == INV and q8(d, scales=FAKE + 2) == MIS
+    assert fwd(norm(rows=0)) == q8(norm(rows=0)) == OK
+    assert bwd(d, s=None) == bwd(d, dy=None) == bwd(d, gain=None) == bwd(d, rstd=None) == bwd(d, dx=None) == INV
+    assert bwd(d, acc=2) == INV
+    assert bwd(d, dy=FAKE + 1) == bwd(d, dgain=FAKE + 2) == bwd(d, flag=FAKE + 2) == bwd(d, ws=FAKE + 2) == MIS
+    st, need = nc.nnconv_rmsnorm_workspace_size(d)
+    assert st == OK and need >= 16 * 4
+    assert bwd(d, nb=need - 1) == WSP and bwd(d, ws=None) == INV
+
+
+def rec(n=2, t=100, c=16, dtype=nc.NNCONV_F16, ld=16, ldy=16):
+    return nc.nnconv_recurrence_desc(n, t, c, dtype, ld, ldy)
+
+
+def rfwd(d, x=FAKE, f=FAKE, bias=None, g=None, lengths=None, h0=None, y=FAKE, ht=None, saved=None, ws=FAKE, nb=1 << 40):
+    return nc.nnconv_recurrence_fwd(d, x, f, bias, g, lengths, h0, y, ht, saved, ws, nb, None)
+
+
+def rbwd(d, x=FAKE, f=FAKE, g=None, saved=FAKE, dy=FAKE, dht=None, dx=FAKE, df=FAKE, dg=None, dh0=None, dbias=FAKE,
+         acc=0, flag=None, ws=FAKE, nb=1 << 40):
+    return nc.nnconv_recurrence_bwd(d, x, f, None, g, None, saved, dy, dht, dx, df, dg, dh0, dbias, 1.0, acc, flag, ws, nb, None)
+
+
+@pytest.mark.parametrize("kw", [dict(n=-1), dict(t=-1), dict(c=0), dict(ld=15), dict(ldy=15), dict(dtype=5),
+                                dict(n=1 << 30, t=1 << 30), dict(ld=1 << 50)])
+def test_recurrence_descriptors(nnlib, kw):
+    d = rec(**kw)
+    assert rfwd(d) == rbwd(d) == nc.nnconv_recurrence_saved_size(d)[0] == INV
+    assert nc.nnconv_recurrence_workspace_size(d, nc.NNCONV_FWD)[0] == INV
+
+
+def test_recurrence_refusals(nnlib):
+    d = rec()
+    assert rfwd(rec(dtype=nc.NNCONV_F32)) == rbwd(rec(dtype=nc.NNCONV_F32)) == UNS
+    assert rfwd(d, x=None) == rfwd(d, f=None) == rfwd(d, y=None) == INV
+    for k in ("x", "f", "g", "y"):
+        assert rfwd(d, **{k: FAKE + 1}) == MIS
+    for k in ("bias", "lengths", "h0", "ht", "saved"):
+        assert rfwd(d, **{k: FAKE + 2}) == MIS
+    for k in ("x", "f", "saved", "dy", "dx", "df"):
+        assert rbwd(d, **{k: None}) == INV
+    assert rbwd(d, g=FAKE, dg=None) == INV and rbwd(d, acc=3) == INV
+    for k in ("dy", "dx", "df"):
+        assert rbwd(d, **{k: FAKE + 1}) == MIS
+    for k in ("saved", "dht", "dh0", "dbias", "flag"):
+        assert rbwd(d, **{k: FAKE + 2}) == MIS
+    assert nc.nnconv_recurrence_saved_size(d) == (OK, 2 * 2 * 16 * 4)
+    assert nc.nnconv_recurrence_workspace_size(d, nc.NNCONV_WGRAD)[0] == INV
+    for pass_, call in ((nc.NNCONV_FWD, rfwd), (nc.NNCONV_DGRAD, rbwd)):
+        for big in (d, rec(n=3, t=20000, c=64, ld=64, ldy=64)):
+            st, need = nc.nnconv_recurrence_workspace_size(big, pass_)
+            assert st == OK
+            if need:
+                assert call(big, nb=need - 1) == WSP and call(big, ws=None) == INV and call(big, ws=FAKE + 4) == MIS
+    assert rfwd(rec(n=0)) == OK
+
+
+def tensor(**kw):
+    base = dict(master=FAKE, grad=FAKE, w16=FAKE, m=FAKE, v=FAKE, m_scale=FAKE, v_scale=FAKE, count=100, weight_decay=0.1,
+                grad_dtype=nc.NNCONV_F32, w16_dtype=nc.NNCONV_F16, state_dtype=nc.NNCONV_F8)
+    base.update(kw)
+    return (nc.nnconv_adamw_tensor * 1)(nc.nnconv_adamw_tensor(**base))
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(count=-1), INV), (dict(master=None), INV), (dict(grad=None), INV), (dict(m=None), INV), (dict(v=None), INV),
+    (dict(m_scale=None), INV), (dict(v_scale=None), INV), (dict(weight_decay=float("nan")), INV),
+    (dict(grad_dtype=nc.NNCONV_F8), INV), (dict(grad_dtype=-1), INV), (dict(w16_dtype=nc.NNCONV_F32), INV),
+    (dict(state_dtype=nc.NNCONV_F16), INV), (dict(master=FAKE + 2), MIS), (dict(grad=FAKE + 2), MIS), (dict(w16=FAKE + 1), MIS),
+    (dict(state_dtype=nc.NNCONV_F32, m=FAKE + 2), MIS), (dict(state_dtype=nc.NNCONV_F32, v=FAKE + 1), MIS)])
+def test_adamw_plan_refusals(nnlib, kw, want):
+    plan = nc.nnconv_adamw_plan()
+    assert nc.nnconv_adamw_plan_size(tensor(**kw), 1)[0] == want
+    assert nc.nnconv_adamw_plan_init(tensor(**kw), 1, FAKE, 1 << 30, plan, None) == want
+
+
+def test_adamw_refusals(nnlib):
+    plan = nc.nnconv_adamw_plan()
+    t = tensor()
+    st, need = nc.nnconv_adamw_plan_size(t, 1)
+    assert st == OK and need >= 80
+    # 8-bit codes may start at any byte; an empty tensor may have no arrays; scales are not looked at with fp32 moments
+    assert nc.nnconv_adamw_plan_size(tensor(m=FAKE + 1, v=FAKE + 3), 1)[0] == OK
+    assert nc.nnconv_adamw_plan_size(tensor(count=0, master=None, grad=None, m=None, v=None), 1)[0] == OK
+    assert nc.nnconv_adamw_plan_size(tensor(state_dtype=nc.NNCONV_F32, m_scale=None, v_scale=None), 1)[0] == OK
+    assert nc.nnconv_adamw_plan_size(t, -1)[0] == nc.nnconv_adamw_plan_size(None, 1)[0] == INV
+    assert nc.nnconv_adamw_plan_init(t, 1, FAKE, need - 1, plan, None) == WSP
+    assert nc.nnconv_adamw_plan_init(t, 1, None, need, plan, None) == INV
+    assert nc.nnconv_adamw_plan_init(t, 1, FAKE + 8, need, plan, None) == MIS
+
+    good = nc.nnconv_adamw_plan(FAKE, 1, 1, 0)
+
+    def step(plan=good, step=FAKE, lr=1e-3, b1=0.9, b2=0.999, eps=1e-8, state=None, flag=None):
+        return nc.nnconv_adamw_update(plan, step, lr, b1, b2, eps, 0, state, flag, None)
+    nan, inf = float("nan"), float("inf")
+    assert step(step=None) == step(lr=-1.0) == step(lr=nan) == step(lr=inf) == step(eps=-1e-8) == step(eps=nan) == INV
+    assert step(b1=1.0) == step(b1=-0.1) == step(b2=1.0) == step(b2=nan) == INV
+    assert step(plan=nc.nnconv_adamw_plan(None, 1, 1, 0)) == step(plan=nc.nnconv_adamw_plan(FAKE, -1, 1, 0)) == INV
+    assert step(step=FAKE + 2) == step(state=FAKE + 2) == step(flag=FAKE + 1) == MIS
