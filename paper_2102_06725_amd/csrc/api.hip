@@ -2153,7 +2153,7 @@ NNCONV_API nnconv_status nnconv_recurrence_bwd(
     p.dh0 = dh0;
     p.ws = ws;
     const int64_t parts = recurrence_bwd_parts(p);
-    p.part = dbias ? (float *)ws : nullptr;
+    p.part = dbias ? (float *)((char *)ws + recurrence_words_bytes(p, true)) : nullptr;
     hipStream_t s = (hipStream_t)hip_stream;
     clear_stale_error();
     TRY_HIP(launch_recurrence_bwd(desc->dtype, p, s));

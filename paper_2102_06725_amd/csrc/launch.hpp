@@ -467,6 +467,7 @@ struct RecParams {
 };
 int64_t recurrence_bwd_parts(const RecParams &p);
 size_t recurrence_ws(const RecParams &p, bool backward);
+size_t recurrence_words_bytes(const RecParams &p, bool backward);
 hipError_t launch_recurrence_fwd(int dtype, const RecParams &p, hipStream_t st);
 hipError_t launch_recurrence_bwd(int dtype, const RecParams &p, hipStream_t st);
 

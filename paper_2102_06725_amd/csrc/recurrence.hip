@@ -1,5 +1,18 @@
 // recurrence.hip -- gated linear recurrence over the tokens of a sequence,
 // channel by channel, forward and backward.
+//
+// h_t = a_t h_(t-1) + u_t is a composition of affine maps, so a stretch of
+// tokens is the pair (A, H) of h_out = A h_in + H, and stretches can be
+// computed apart and joined:
+//   - a lane holds two neighbouring channels (one 4-byte load of a 16-bit
+//     tensor) and walks S tokens that it keeps in registers; a wave covers 128
+//     channels, the W waves of a workgroup W * S consecutive tokens (a chunk);
+//   - the waves exchange their (A, H) through LDS;
+//   - chunks exchange theirs through one 64-bit word per channel in the
+//     workspace (below).  The inputs are read once, and y is computed from
+//     registers.
+// Whether a token takes part is the same for a whole wave, so lengths
+// and the end of the sequence cost no divergence.
 #include "launch.hpp"
 
 namespace nnconv {
@@ -7,6 +20,11 @@ namespace nnconv {
 namespace {
 
 constexpr int SAVE = NNCONV_RECURRENCE_SAVE;
+constexpr int COLS = 128;                 // channels of a wave
+constexpr float A_MIN = 0x1p-126f;        // products of gates stay above 0: 0 * inf would be NaN
+constexpr int SHORT_T = 16;               // up to here one lane walks all tokens
+
+typedef uint32_t __attribute__((aligned(2))) u32_any;  // 4-byte access at any element
 
 // The gate a = sigma(z) and b = 1 - a = sigma(-z), each to full relative
 // precision: with a near 1 the difference 1 - a would keep few bits of the
@@ -29,125 +47,788 @@ __device__ __forceinline__ int length_of(const RecParams &p, int n) {
     return l < 0 ? 0 : l > p.t ? p.t : l;
 }
 
-// A thread per channel walks the tokens.
+// The two channels of a lane.  c >= 2: a lane at or past the last channel
+// loads the last two, and takes the second of them if it is alone there.
+struct Lane {
+    int at;            // first channel loaded
+    int k0, k1;        // channels of per-channel fp32 arrays and words, in range
+    uint32_t shift;    // 16: the first channel is the second half of the load
+    bool first, second;  // channels that exist
+
+    __device__ __forceinline__ Lane(int c0, int c) {
+        at = c0 < c - 2 ? c0 : c - 2;
+        first = c0 < c;
+        second = c0 + 1 < c;
+        shift = c0 == c - 1 ? 16 : 0;
+        k0 = first ? c0 : c - 1;
+        k1 = second ? c0 + 1 : c - 1;
+    }
+};
+
 template <class T>
-__global__ __launch_bounds__(64) void recurrence_fwd_kernel(const RecParams p) {
-    const int c = blockIdx.x * 64 + threadIdx.x;
-    if (c >= p.c) return;
-    for (int64_t n = blockIdx.y; n < p.n; n += gridDim.y) {
-        const int len = length_of(p, n);
-        float h = p.h0 ? p.h0[n * p.c + c] : 0.f;
-        const float bias = p.bias ? p.bias[c] : 0.f;
-        const uint16_t *x = (const uint16_t *)p.x + n * p.t * p.ld + c;
-        const uint16_t *f = (const uint16_t *)p.f + n * p.t * p.ld + c;
-        const uint16_t *g = p.g ? (const uint16_t *)p.g + n * p.t * p.ld + c : nullptr;
-        uint16_t *y = (uint16_t *)p.y + n * p.t * p.ldy + c;
-        for (int64_t t = 0; t < p.t; ++t) {
-            if (p.saved && t % SAVE == 0)
-                p.saved[(n * ((p.t + SAVE - 1) / SAVE) + t / SAVE) * p.c + c] = h;
-            float out = 0.f;
-            if (t < len) {
-                float a, b;
-                gate(from16<T>(f[t * p.ld]), bias, a, b);
-                h = a * h + b * from16<T>(x[t * p.ld]);
-                out = h;
-                if (g) {
-                    const float gv = from16<T>(g[t * p.ld]);
-                    out = h * gv * sigma(gv);
-                }
-            }
-            y[t * p.ldy] = (uint16_t)to16<T>(out);
+__device__ __forceinline__ void unpack(uint32_t v, float o[2]) {
+    o[0] = from16<T>(v & 0xFFFFu);
+    o[1] = from16<T>(v >> 16);
+}
+
+template <class T>
+__device__ __forceinline__ void store2(uint16_t *q, const Lane &L, float v0, float v1) {
+    const uint32_t lo = to16<T>(v0) & 0xFFFFu;
+    if (L.second)
+        *(u32_any *)q = lo | (to16<T>(v1) << 16);
+    else if (L.first)
+        q[L.shift >> 4] = (uint16_t)lo;  // q is the address of channel L.at
+}
+
+// ---- words between chunks ------------------------------------------------------
+
+// Chunks are taken in the direction of the recurrence: place k of a sequence.
+// Two arrays of 64-bit words, all ones until written: the (A, H) of every place,
+// and the state in front of every group of 2^gs places.  A word is stored and loaded at
+// once, so it needs no flag and no ordering with other memory.  Which words are
+// composed, and in which order, depends on the sizes alone, so that results
+// do not depend on which workgroup came first.
+struct RecGrid {
+    int32_t cols, chunks, gs, groups;
+    uint64_t *words;   // [n][chunks][c], null for a single chunk
+    uint64_t *states;  // [n][groups][c]
+};
+constexpr int MAX_GS = 4;
+constexpr uint64_t EMPTY = ~0ull;
+constexpr int POLLS = 4096;
+
+__device__ __forceinline__ uint64_t word(float a, float h) {
+    return (uint64_t)__builtin_bit_cast(uint32_t, a) |
+           ((uint64_t)__builtin_bit_cast(uint32_t, h) << 32);
+}
+
+__device__ __forceinline__ float word_a(uint64_t v) { return __builtin_bit_cast(float, (uint32_t)v); }
+__device__ __forceinline__ float word_h(uint64_t v) { return __builtin_bit_cast(float, (uint32_t)(v >> 32)); }
+
+__device__ __forceinline__ void put(uint64_t *row, const Lane &L, const float a[2], const float h[2]) {
+    if (L.first) __hip_atomic_store(row + L.k0, word(a[0], h[0]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (L.second) __hip_atomic_store(row + L.k1, word(a[1], h[1]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+__device__ __forceinline__ bool get(const uint64_t *row, const Lane &L, float a[2], float h[2]) {
+    const uint64_t v0 = __hip_atomic_load(row + L.k0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const uint64_t v1 = __hip_atomic_load(row + L.k1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    a[0] = word_a(v0);
+    a[1] = word_a(v1);
+    h[0] = word_h(v0);
+    h[1] = word_h(v1);
+    return !__any(v0 == EMPTY || v1 == EMPTY);
+}
+
+// Waits for a row's words, for POLLS looks at most.
+__device__ __forceinline__ bool wait(const uint64_t *row, const Lane &L, float a[2], float h[2]) {
+    for (int k = 0; k < POLLS; ++k) {
+        if (get(row, L, a, h)) return true;
+        __builtin_amdgcn_s_sleep(1);
+    }
+    return false;
+}
+
+// Before each split call: every word empty but the states in front of the
+// first places.
+__global__ __launch_bounds__(256) void recurrence_words_kernel(const RecGrid q, int64_t n, int32_t c,
+                                                               const float *init) {
+    const int64_t plain = n * q.chunks * c, total = plain + n * q.groups * c;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        uint64_t v = EMPTY;
+        if (i >= plain) {
+            const int64_t row = (i - plain) / c;
+            if (row % q.groups == 0) v = word(0.f, init ? init[row / q.groups * c + (i - plain - row * c)] : 0.f);
         }
-        if (p.ht) p.ht[n * p.c + c] = h;
+        q.words[i] = v;  // the states follow the words
     }
 }
 
-// The same from the last token back; the states inside a stretch of SAVE
-// tokens are computed again from the saved one.
-template <class T>
-__global__ __launch_bounds__(64) void recurrence_bwd_kernel(const RecParams p) {
-    __shared__ float hs[SAVE][64];
-    const int lane = threadIdx.x;
-    const int c = blockIdx.x * 64 + lane;
-    if (c >= p.c) return;
-    for (int64_t n = blockIdx.y; n < p.n; n += gridDim.y) {
-        const int len = length_of(p, n);
-        const int64_t chunks = (p.t + SAVE - 1) / SAVE;
-        float d = p.dht ? p.dht[n * p.c + c] : 0.f;  // what flows into the state from the right
-        const float bias = p.bias ? p.bias[c] : 0.f;
-        const int64_t at = n * p.t * p.ld + c;
-        const uint16_t *x = (const uint16_t *)p.x + at, *f = (const uint16_t *)p.f + at;
-        const uint16_t *g = p.g ? (const uint16_t *)p.g + at : nullptr;
-        uint16_t *dx = (uint16_t *)p.dx + at, *df = (uint16_t *)p.df + at;
-        uint16_t *dg = p.g ? (uint16_t *)p.dg + at : nullptr;
-        const uint16_t *dy = (const uint16_t *)p.dy + n * p.t * p.ldy + c;
-        float total = 0.f;
-        for (int64_t k = chunks - 1; k >= 0; --k) {
-            const int64_t lo = k * SAVE, hi = lo + SAVE < p.t ? lo + SAVE : p.t;
-            float h = p.saved[(n * chunks + k) * p.c + c];
-            for (int64_t t = lo; t < hi && t < len; ++t) {
-                float a, b;
-                hs[t - lo][lane] = h;
-                gate(from16<T>(f[t * p.ld]), bias, a, b);
-                h = a * h + b * from16<T>(x[t * p.ld]);
-            }
-            for (int64_t t = hi - 1; t >= lo; --t) {
-                float vx = 0.f, vf = 0.f, vg = 0.f;
-                if (t < len) {
-                    float a, b;
-                    gate(from16<T>(f[t * p.ld]), bias, a, b);
-                    const float xv = from16<T>(x[t * p.ld]), before = hs[t - lo][lane];
-                    const float ht = a * before + b * xv;
-                    float own = from16<T>(dy[t * p.ldy]);
-                    if (g) {
-                        const float gv = from16<T>(g[t * p.ld]), s = sigma(gv);
-                        vg = own * ht * s * (1.0f + gv * (1.0f - s));
-                        own = own * gv * s;
+__device__ __forceinline__ void compose(float A[2], float H[2], const float a[2], const float h[2]) {
+    H[0] = __builtin_fmaf(a[0], H[0], h[0]);
+    H[1] = __builtin_fmaf(a[1], H[1], h[1]);
+    A[0] = fmaxf(A[0] * a[0], A_MIN);
+    A[1] = fmaxf(A[1] * a[1], A_MIN);
+}
+
+// The state in front of place k, for all waves.  (ca, ch): the place's own
+// pair, known to wave `own`.  A word that stays empty for POLLS looks is computed here
+// instead (chunk_pair(place, a, h) walks that place's tokens), so that every wait
+// ends whatever order the workgroups run in.
+template <int W, class F>
+__device__ __forceinline__ void carry_in(const RecGrid &q, int n, int32_t c, int k, const Lane &L, int w,
+                                         int own, const float ca[2], const float ch[2], F chunk_pair,
+                                         float out[2]) {
+    __shared__ f32x4 pairs[1 << MAX_GS][64];
+    __shared__ float into[2][64];
+    const int lane = threadIdx.x & 63, g = k >> q.gs, i = k - (g << q.gs);
+    const bool last = i + 1 == 1 << q.gs;
+    uint64_t *words = q.words + (int64_t)n * q.chunks * c, *states = q.states + (int64_t)n * q.groups * c;
+    if (w == own && !last && k + 1 < q.chunks) put(words + (int64_t)k * c, L, ca, ch);
+    for (int j = w; j < i; j += W) {
+        float a[2], h[2];
+        const int place = (g << q.gs) + j;
+        if (!wait(words + (int64_t)place * c, L, a, h)) chunk_pair(place, a, h);
+        pairs[j][lane] = f32x4{a[0], h[0], a[1], h[1]};
+    }
+    __syncthreads();
+    if (w == own) {
+        float A[2] = {1.f, 1.f}, H[2] = {0.f, 0.f}, no[2], h[2];
+        for (int j = 0; j < i; ++j) {
+            const f32x4 e = pairs[j][lane];
+            const float ea[2] = {e[0], e[2]}, eh[2] = {e[1], e[3]};
+            compose(A, H, ea, eh);
+        }
+        if (!wait(states + (int64_t)g * c, L, no, h)) {
+            // from the nearest state there is; the first one was there before the call
+            int from = g;
+            while (from > 0 && !get(states + (int64_t)from * c, L, no, h)) --from;
+            if (from == 0) get(states, L, no, h);
+            for (; from < g; ++from) {
+                float ga[2] = {1.f, 1.f}, gh[2] = {0.f, 0.f}, a[2], b[2];
+                for (int j = 0; j < 1 << q.gs; ++j) {
+                    chunk_pair((from << q.gs) + j, a, b);
+                    if (j + 1 < 1 << q.gs) {
+                        compose(ga, gh, a, b);
+                        continue;
                     }
-                    d += own;
-                    vx = d * b;
-                    vf = d * (before - xv) * (a * b);
-                    d *= a;
-                    total += vf;
+                    for (int u = 0; u < 2; ++u)
+                        h[u] = __builtin_fmaf(a[u], __builtin_fmaf(ga[u], h[u], gh[u]), b[u]);
                 }
-                dx[t * p.ld] = (uint16_t)to16<T>(vx);
-                df[t * p.ld] = (uint16_t)to16<T>(vf);
-                if (dg) dg[t * p.ld] = (uint16_t)to16<T>(vg);
             }
         }
-        if (p.dh0) p.dh0[n * p.c + c] = d;
-        if (p.part) p.part[n * p.c + c] = total;
+        h[0] = __builtin_fmaf(A[0], h[0], H[0]);
+        h[1] = __builtin_fmaf(A[1], h[1], H[1]);
+        if (last && k + 1 < q.chunks) {
+            const float next[2] = {__builtin_fmaf(ca[0], h[0], ch[0]), __builtin_fmaf(ca[1], h[1], ch[1])};
+            const float zero[2] = {0.f, 0.f};
+            put(states + (int64_t)(g + 1) * c, L, zero, next);
+        }
+        into[0][lane] = h[0];
+        into[1][lane] = h[1];
     }
+    __syncthreads();
+    out[0] = into[0][lane];
+    out[1] = into[1][lane];
+}
+
+// ---- forward ------------------------------------------------------------------
+
+// Few tokens: a lane walks them all.
+template <class T>
+__global__ __launch_bounds__(64) void recurrence_fwd_short_kernel(const RecParams p) {
+    const int lane = threadIdx.x;
+    const Lane L(blockIdx.x * COLS + 2 * lane, p.c);
+    for (int64_t n = blockIdx.y; n < p.n; n += gridDim.y) {
+        const int len = length_of(p, (int)n);
+        float h[2] = {0.f, 0.f}, bias[2] = {0.f, 0.f};
+        if (p.h0) {
+            h[0] = p.h0[n * p.c + L.k0];
+            h[1] = p.h0[n * p.c + L.k1];
+        }
+        if (p.bias) {
+            bias[0] = p.bias[L.k0];
+            bias[1] = p.bias[L.k1];
+        }
+        const int64_t at = n * p.t * p.ld + L.at;
+        const uint16_t *x = (const uint16_t *)p.x + at, *f = (const uint16_t *)p.f + at;
+        const uint16_t *g = p.g ? (const uint16_t *)p.g + at : nullptr;
+        uint16_t *y = (uint16_t *)p.y + n * p.t * p.ldy + L.at;
+        if (p.saved && p.t > 0) {  // t <= SAVE: one state
+            if (L.first) p.saved[n * p.c + L.k0] = h[0];
+            if (L.second) p.saved[n * p.c + L.k1] = h[1];
+        }
+        for (int t = 0; t < p.t; ++t) {
+            float o[2] = {0.f, 0.f};
+            if (t < len) {
+                float xv[2], fv[2], gv[2];
+                unpack<T>(*(const u32_any *)(x + t * p.ld) >> L.shift, xv);
+                unpack<T>(*(const u32_any *)(f + t * p.ld) >> L.shift, fv);
+                if (g) unpack<T>(*(const u32_any *)(g + t * p.ld) >> L.shift, gv);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    float a, b;
+                    gate(fv[k], bias[k], a, b);
+                    h[k] = a * h[k] + b * xv[k];
+                    o[k] = g ? h[k] * (gv[k] * sigma(gv[k])) : h[k];
+                }
+            }
+            store2<T>(y + t * p.ldy, L, o[0], o[1]);
+        }
+        if (p.ht) {
+            if (L.first) p.ht[n * p.c + L.k0] = h[0];
+            if (L.second) p.ht[n * p.c + L.k1] = h[1];
+        }
+    }
+}
+
+// The pair of a chunk, walked token by token with the arithmetic of the kernel below.
+template <class T, int W, int S>
+__device__ void walk_fwd(const RecParams &p, int64_t n, const Lane &L, int lo, int len,
+                         const float bias[2], float A[2], float H[2]) {
+    const int64_t at = n * p.t * p.ld + L.at;
+    const uint16_t *x = (const uint16_t *)p.x + at, *f = (const uint16_t *)p.f + at;
+    A[0] = A[1] = 1.f;
+    H[0] = H[1] = 0.f;
+    for (int w = 0; w < W; ++w) {
+        float a1[2] = {1.f, 1.f}, h1[2] = {0.f, 0.f};
+        for (int t = lo + w * S; t < min(lo + w * S + S, len); ++t) {
+            float xv[2], fv[2];
+            unpack<T>(*(const u32_any *)(x + t * p.ld) >> L.shift, xv);
+            unpack<T>(*(const u32_any *)(f + t * p.ld) >> L.shift, fv);
+            for (int k = 0; k < 2; ++k) {
+                float a, b;
+                gate(fv[k], bias[k], a, b);
+                h1[k] = __builtin_fmaf(a, h1[k], b * xv[k]);
+                a1[k] *= a;
+            }
+        }
+        a1[0] = fmaxf(a1[0], A_MIN);
+        a1[1] = fmaxf(a1[1], A_MIN);
+        compose(A, H, a1, h1);
+    }
+}
+
+template <class T, bool G, int W, int S>
+__global__ __launch_bounds__(64 * W) void recurrence_fwd_kernel(const RecParams p, const RecGrid q) {
+    static_assert(SAVE % S == 0, "saved states lie at a wave's first token");
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = blockIdx.x % q.cols, rest = blockIdx.x / q.cols;
+    const int n = rest % p.n, chunk = rest / p.n;
+    const Lane L(col * COLS + 2 * lane, p.c);
+    const int len = length_of(p, n);
+    const int t0 = chunk * (W * S) + w * S, last = len > 0 ? len - 1 : 0;
+    const int64_t at = (int64_t)n * p.t * p.ld + L.at;
+    const uint16_t *x = (const uint16_t *)p.x + at, *f = (const uint16_t *)p.f + at;
+    const uint16_t *g = G ? (const uint16_t *)p.g + at : nullptr;
+    uint32_t xr[S], fr[S], gr[S];
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        const int64_t o = (int64_t)min(t0 + s, last) * p.ld;
+        xr[s] = *(const u32_any *)(x + o);
+        fr[s] = *(const u32_any *)(f + o);
+        if (G) gr[s] = *(const u32_any *)(g + o);
+    }
+    float bias[2] = {0.f, 0.f};
+    if (p.bias) {
+        bias[0] = p.bias[L.k0];
+        bias[1] = p.bias[L.k1];
+    }
+    float a[S][2], u[S][2], A[2] = {1.f, 1.f}, H[2] = {0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        float xv[2], fv[2];
+        unpack<T>(xr[s] >> L.shift, xv);
+        unpack<T>(fr[s] >> L.shift, fv);
+        const bool live = t0 + s < len;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            float b;
+            gate(fv[k], bias[k], a[s][k], b);
+            u[s][k] = b * xv[k];
+            if (!live) {
+                a[s][k] = 1.f;
+                u[s][k] = 0.f;
+            }
+            H[k] = __builtin_fmaf(a[s][k], H[k], u[s][k]);
+            A[k] *= a[s][k];
+        }
+    }
+    A[0] = fmaxf(A[0], A_MIN);
+    A[1] = fmaxf(A[1], A_MIN);
+    __shared__ f32x4 part[W][64];
+    part[w][lane] = f32x4{A[0], H[0], A[1], H[1]};
+    __syncthreads();
+    // what the waves in front make of the chunk's first state
+    float pa[2] = {1.f, 1.f}, ph[2] = {0.f, 0.f};
+    for (int v = 0; v < w; ++v) {
+        const f32x4 e = part[v][lane];
+        const float ea[2] = {e[0], e[2]}, eh[2] = {e[1], e[3]};
+        compose(pa, ph, ea, eh);
+    }
+    float h[2] = {0.f, 0.f};
+    if (q.words) {
+        float ca[2] = {pa[0], pa[1]}, ch[2] = {ph[0], ph[1]};
+        compose(ca, ch, A, H);
+        carry_in<W>(q, n, p.c, chunk, L, w, W - 1, ca, ch, [&](int place, float *a2, float *h2) {
+            walk_fwd<T, W, S>(p, n, L, place * (W * S), len, bias, a2, h2);
+        }, h);
+    } else if (p.h0) {
+        h[0] = p.h0[(int64_t)n * p.c + L.k0];
+        h[1] = p.h0[(int64_t)n * p.c + L.k1];
+    }
+    h[0] = pa[0] * h[0] + ph[0];
+    h[1] = pa[1] * h[1] + ph[1];
+    if (p.saved && t0 % SAVE == 0 && t0 < p.t) {
+        float *to = p.saved + ((int64_t)n * ((p.t + SAVE - 1) / SAVE) + t0 / SAVE) * p.c;
+        if (L.first) to[L.k0] = h[0];
+        if (L.second) to[L.k1] = h[1];
+    }
+    uint16_t *y = (uint16_t *)p.y + (int64_t)n * p.t * p.ldy + L.at;
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        const int t = t0 + s;
+        float o[2], gv[2];
+        if (G) unpack<T>(gr[s] >> L.shift, gv);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            h[k] = a[s][k] * h[k] + u[s][k];
+            o[k] = G ? h[k] * (gv[k] * sigma(gv[k])) : h[k];
+            if (t >= len) o[k] = 0.f;
+        }
+        if (t < p.t) store2<T>(y + t * p.ldy, L, o[0], o[1]);
+    }
+    if (p.ht && chunk == q.chunks - 1 && w == W - 1) {
+        if (L.first) p.ht[(int64_t)n * p.c + L.k0] = h[0];
+        if (L.second) p.ht[(int64_t)n * p.c + L.k1] = h[1];
+    }
+}
+
+// ---- backward -------------------------------------------------------------------
+
+// With own_t = dy_t g_t sigma(g_t), the gradient of h_t is d_t = own_t + r_t, where r_t
+// flows in from the right: r_(t-1) = a_t d_t.  So r obeys the same kind
+// of recurrence from the last token on, with a_t and a_t own_t.
+
+template <class T, bool G>
+struct Grad {
+    float a[2], b[2], x[2], own[2], dg[2];  // dg without the factor h_t
+
+    __device__ __forceinline__ void make(uint32_t xq, uint32_t fq, uint32_t gq, uint32_t dyq, const float bias[2], bool live) {
+        float fv[2], gv[2], dy[2];
+        unpack<T>(xq, x);
+        unpack<T>(fq, fv);
+        unpack<T>(dyq, dy);
+        if (G) unpack<T>(gq, gv);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            gate(fv[k], bias[k], a[k], b[k]);
+            own[k] = dy[k];
+            dg[k] = 0.f;
+            if (G) {
+                const float s = sigma(gv[k]), sg = gv[k] * s;
+                own[k] = dy[k] * sg;
+                dg[k] = dy[k] * (s + sg * (1.f - s));
+            }
+            if (!live) {  // the state passes through, nothing else happens
+                a[k] = 1.f;
+                b[k] = x[k] = own[k] = dg[k] = 0.f;
+            }
+        }
+    }
+};
+
+// Few tokens: a lane walks them all, forward for the states (t <= SHORT_T of
+// them, in LDS) and back.
+template <class T, bool G>
+__global__ __launch_bounds__(64) void recurrence_bwd_short_kernel(const RecParams p) {
+    __shared__ float hs[SHORT_T][2][64];
+    const int lane = threadIdx.x;
+    const Lane L(blockIdx.x * COLS + 2 * lane, p.c);
+    float bias[2] = {0.f, 0.f};
+    if (p.bias) {
+        bias[0] = p.bias[L.k0];
+        bias[1] = p.bias[L.k1];
+    }
+    for (int64_t n = blockIdx.y; n < p.n; n += gridDim.y) {
+        const int len = length_of(p, (int)n);
+        float r[2] = {0.f, 0.f}, total[2] = {0.f, 0.f};
+        if (p.dht) {
+            r[0] = p.dht[n * p.c + L.k0];
+            r[1] = p.dht[n * p.c + L.k1];
+        }
+        const int64_t at = n * p.t * p.ld + L.at;
+        const uint16_t *x = (const uint16_t *)p.x + at, *f = (const uint16_t *)p.f + at;
+        const uint16_t *g = G ? (const uint16_t *)p.g + at : nullptr;
+        const uint16_t *dy = (const uint16_t *)p.dy + n * p.t * p.ldy + L.at;
+        uint16_t *dx = (uint16_t *)p.dx + at, *df = (uint16_t *)p.df + at;
+        uint16_t *dg = G ? (uint16_t *)p.dg + at : nullptr;
+        if (len > 0) {
+            float h[2] = {p.saved[n * p.c + L.k0], p.saved[n * p.c + L.k1]};
+            for (int t = 0; t < len; ++t) {
+                float xv[2], fv[2];
+                unpack<T>(*(const u32_any *)(x + t * p.ld) >> L.shift, xv);
+                unpack<T>(*(const u32_any *)(f + t * p.ld) >> L.shift, fv);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    float a, b;
+                    gate(fv[k], bias[k], a, b);
+                    hs[t][k][lane] = h[k];
+                    h[k] = a * h[k] + b * xv[k];
+                }
+            }
+        }
+        for (int t = p.t - 1; t >= 0; --t) {
+            float vx[2] = {0.f, 0.f}, vf[2] = {0.f, 0.f}, vg[2] = {0.f, 0.f};
+            if (t < len) {
+                Grad<T, G> e;
+                e.make(*(const u32_any *)(x + t * p.ld) >> L.shift, *(const u32_any *)(f + t * p.ld) >> L.shift,
+                       G ? *(const u32_any *)(g + t * p.ld) >> L.shift : 0u, *(const u32_any *)(dy + t * p.ldy) >> L.shift, bias, true);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const float before = hs[t][k][lane], d = e.own[k] + r[k];
+                    vx[k] = d * e.b[k];
+                    vf[k] = d * (before - e.x[k]) * (e.a[k] * e.b[k]);
+                    if (G) vg[k] = e.dg[k] * (e.a[k] * before + e.b[k] * e.x[k]);
+                    r[k] = e.a[k] * d;
+                    total[k] += vf[k];
+                }
+            }
+            store2<T>(dx + t * p.ld, L, vx[0], vx[1]);
+            store2<T>(df + t * p.ld, L, vf[0], vf[1]);
+            if (G) store2<T>(dg + t * p.ld, L, vg[0], vg[1]);
+        }
+        if (p.dh0) {
+            if (L.first) p.dh0[n * p.c + L.k0] = r[0];
+            if (L.second) p.dh0[n * p.c + L.k1] = r[1];
+        }
+        if (p.part) {
+            if (L.first) p.part[n * p.c + L.k0] = total[0];
+            if (L.second) p.part[n * p.c + L.k1] = total[1];
+        }
+    }
+}
+
+// The pair of a chunk for r, walked from its last token on with the arithmetic of the kernel below.
+template <class T, bool G, int W, int S>
+__device__ void walk_bwd(const RecParams &p, int64_t n, const Lane &L, int lo, int len,
+                         const float bias[2], float A[2], float R[2]) {
+    const int64_t at = n * p.t * p.ld + L.at;
+    const uint16_t *f = (const uint16_t *)p.f + at;
+    const uint16_t *g = G ? (const uint16_t *)p.g + at : nullptr;
+    const uint16_t *dy = (const uint16_t *)p.dy + n * p.t * p.ldy + L.at;
+    A[0] = A[1] = 1.f;
+    R[0] = R[1] = 0.f;
+    for (int w = W - 1; w >= 0; --w) {
+        float a1[2] = {1.f, 1.f}, r1[2] = {0.f, 0.f};
+        const int first = lo + w * S;
+        for (int t = first; t < min(first + S, len); ++t)
+            for (int k = 0; k < 2; ++k) {  // the product in the order of the tokens
+                float fv[2], a, b;
+                unpack<T>(*(const u32_any *)(f + t * p.ld) >> L.shift, fv);
+                gate(fv[k], bias[k], a, b);
+                a1[k] *= a;
+            }
+        for (int t = min(first + S, len) - 1; t >= first; --t) {
+            Grad<T, G> e;
+            e.make(0u, *(const u32_any *)(f + t * p.ld) >> L.shift, G ? *(const u32_any *)(g + t * p.ld) >> L.shift : 0u,
+                   *(const u32_any *)(dy + t * p.ldy) >> L.shift, bias, true);
+            for (int k = 0; k < 2; ++k) r1[k] = e.a[k] * (e.own[k] + r1[k]);
+        }
+        a1[0] = fmaxf(a1[0], A_MIN);
+        a1[1] = fmaxf(a1[1], A_MIN);
+        compose(A, R, a1, r1);
+    }
+}
+
+template <class T, bool G, int W, int S>
+__global__ __launch_bounds__(64 * W) void recurrence_bwd_kernel(const RecParams p, const RecGrid q) {
+    static_assert((W * S) % SAVE == 0 && SAVE % S == 0, "a chunk is whole saved stretches");
+    constexpr int RUN = SAVE / S;  // waves that start from one saved state
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = blockIdx.x % q.cols, rest = blockIdx.x / q.cols;
+    const int n = rest % p.n, place = rest / p.n, chunk = q.chunks - 1 - place;  // the last one first
+    const Lane L(col * COLS + 2 * lane, p.c);
+    const int len = length_of(p, n);
+    const int t0 = chunk * (W * S) + w * S, last = len > 0 ? len - 1 : 0;
+    const int64_t at = (int64_t)n * p.t * p.ld + L.at;
+    const uint16_t *x = (const uint16_t *)p.x + at, *f = (const uint16_t *)p.f + at;
+    const uint16_t *g = G ? (const uint16_t *)p.g + at : nullptr;
+    const uint16_t *dy = (const uint16_t *)p.dy + (int64_t)n * p.t * p.ldy + L.at;
+    uint32_t xr[S], fr[S], gr[S], dr[S];
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        const int64_t t = min(t0 + s, last);
+        xr[s] = *(const u32_any *)(x + t * p.ld);
+        fr[s] = *(const u32_any *)(f + t * p.ld);
+        gr[s] = G ? *(const u32_any *)(g + t * p.ld) : 0u;
+        dr[s] = *(const u32_any *)(dy + t * p.ldy);
+    }
+    float h[2] = {0.f, 0.f}, bias[2] = {0.f, 0.f};
+    const int run0 = t0 - w % RUN * S;  // first token of the saved stretch
+    if (run0 < p.t) {
+        const float *from = p.saved + ((int64_t)n * ((p.t + SAVE - 1) / SAVE) + run0 / SAVE) * p.c;
+        h[0] = from[L.k0];
+        h[1] = from[L.k1];
+    }
+    if (p.bias) {
+        bias[0] = p.bias[L.k0];
+        bias[1] = p.bias[L.k1];
+    }
+    Grad<T, G> e[S];
+    float A[2] = {1.f, 1.f}, H[2] = {0.f, 0.f}, R[2] = {0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        e[s].make(xr[s] >> L.shift, fr[s] >> L.shift, gr[s] >> L.shift, dr[s] >> L.shift, bias, t0 + s < len);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            H[k] = e[s].a[k] * H[k] + e[s].b[k] * e[s].x[k];
+            A[k] *= e[s].a[k];
+        }
+    }
+#pragma unroll
+    for (int s = S - 1; s >= 0; --s)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) R[k] = e[s].a[k] * (e[s].own[k] + R[k]);
+    A[0] = fmaxf(A[0], A_MIN);
+    A[1] = fmaxf(A[1], A_MIN);
+    __shared__ f32x4 part[W][64];
+    __shared__ float part_r[W][2][64];
+    part[w][lane] = f32x4{A[0], H[0], A[1], H[1]};
+    part_r[w][0][lane] = R[0];
+    part_r[w][1][lane] = R[1];
+    __syncthreads();
+    for (int v = w - w % RUN; v < w; ++v) {
+        const f32x4 m = part[v][lane];
+        h[0] = m[0] * h[0] + m[1];
+        h[1] = m[2] * h[1] + m[3];
+    }
+    // what the waves behind make of the gradient that flows into the chunk
+    float pa[2] = {1.f, 1.f}, pr[2] = {0.f, 0.f};
+    for (int v = W - 1; v > w; --v) {
+        const f32x4 m = part[v][lane];
+        const float ma[2] = {m[0], m[2]}, mr[2] = {part_r[v][0][lane], part_r[v][1][lane]};
+        compose(pa, pr, ma, mr);
+    }
+    float r[2] = {0.f, 0.f};
+    if (q.words) {
+        float ca[2] = {pa[0], pa[1]}, cr[2] = {pr[0], pr[1]};
+        compose(ca, cr, A, R);
+        carry_in<W>(q, n, p.c, place, L, w, 0, ca, cr, [&](int at2, float *a2, float *r2) {
+            walk_bwd<T, G, W, S>(p, n, L, (q.chunks - 1 - at2) * (W * S), len, bias, a2, r2);
+        }, r);
+    } else if (p.dht) {
+        r[0] = p.dht[(int64_t)n * p.c + L.k0];
+        r[1] = p.dht[(int64_t)n * p.c + L.k1];
+    }
+    r[0] = pa[0] * r[0] + pr[0];
+    r[1] = pa[1] * r[1] + pr[1];
+    float before[S][2];
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            before[s][k] = h[k];
+            h[k] = e[s].a[k] * h[k] + e[s].b[k] * e[s].x[k];
+        }
+    uint16_t *dx = (uint16_t *)p.dx + at, *df = (uint16_t *)p.df + at;
+    uint16_t *dg = G ? (uint16_t *)p.dg + at : nullptr;
+    float total[2] = {0.f, 0.f};
+#pragma unroll
+    for (int s = S - 1; s >= 0; --s) {
+        const int t = t0 + s;
+        float vx[2], vf[2], vg[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const Grad<T, G> &m = e[s];
+            const float d = m.own[k] + r[k];
+            vx[k] = d * m.b[k];
+            vf[k] = d * (before[s][k] - m.x[k]) * (m.a[k] * m.b[k]);
+            vg[k] = m.dg[k] * (m.a[k] * before[s][k] + m.b[k] * m.x[k]);
+            if (t >= len) vx[k] = vf[k] = vg[k] = 0.f;
+            r[k] = m.a[k] * d;
+            total[k] += vf[k];
+        }
+        if (t < p.t) {
+            store2<T>(dx + t * p.ld, L, vx[0], vx[1]);
+            store2<T>(df + t * p.ld, L, vf[0], vf[1]);
+            if (G) store2<T>(dg + t * p.ld, L, vg[0], vg[1]);
+        }
+    }
+    if (p.dh0 && chunk == 0 && w == 0) {
+        if (L.first) p.dh0[(int64_t)n * p.c + L.k0] = r[0];
+        if (L.second) p.dh0[(int64_t)n * p.c + L.k1] = r[1];
+    }
+    if (p.part) {
+        __syncthreads();
+        part_r[w][0][lane] = total[0];
+        part_r[w][1][lane] = total[1];
+        __syncthreads();
+        if (w != 0) return;
+        for (int v = 1; v < W; ++v) {
+            total[0] += part_r[v][0][lane];
+            total[1] += part_r[v][1][lane];
+        }
+        float *to = p.part + ((int64_t)n * q.chunks + chunk) * p.c;
+        if (L.first) to[L.k0] = total[0];
+        if (L.second) to[L.k1] = total[1];
+    }
+}
+
+// ---- one channel: no pairs to load, a lane per sequence walks its tokens ---------
+
+template <class T>
+__global__ __launch_bounds__(64) void recurrence_fwd_single_kernel(const RecParams p) {
+    const int64_t n = (int64_t)blockIdx.x * 64 + threadIdx.x;
+    if (n >= p.n) return;
+    const int len = length_of(p, (int)n);
+    const float bias = p.bias ? p.bias[0] : 0.f;
+    float h = p.h0 ? p.h0[n] : 0.f;
+    const uint16_t *x = (const uint16_t *)p.x + n * p.t * p.ld, *f = (const uint16_t *)p.f + n * p.t * p.ld;
+    const uint16_t *g = p.g ? (const uint16_t *)p.g + n * p.t * p.ld : nullptr;
+    uint16_t *y = (uint16_t *)p.y + n * p.t * p.ldy;
+    for (int64_t t = 0; t < p.t; ++t) {
+        if (p.saved && t % SAVE == 0) p.saved[n * ((p.t + SAVE - 1) / SAVE) + t / SAVE] = h;
+        float o = 0.f;
+        if (t < len) {
+            float a, b;
+            gate(from16<T>(f[t * p.ld]), bias, a, b);
+            h = a * h + b * from16<T>(x[t * p.ld]);
+            o = h;
+            if (g) {
+                const float gv = from16<T>(g[t * p.ld]);
+                o = h * (gv * sigma(gv));
+            }
+        }
+        y[t * p.ldy] = (uint16_t)to16<T>(o);
+    }
+    if (p.ht) p.ht[n] = h;
+}
+
+template <class T>
+__global__ __launch_bounds__(64) void recurrence_bwd_single_kernel(const RecParams p) {
+    __shared__ float hs[SAVE][64];
+    const int lane = threadIdx.x;
+    const int64_t n = (int64_t)blockIdx.x * 64 + lane;
+    if (n >= p.n) return;
+    const int len = length_of(p, (int)n);
+    const float bias = p.bias ? p.bias[0] : 0.f;
+    const int64_t at = n * p.t * p.ld, stretches = (p.t + SAVE - 1) / SAVE;
+    const uint16_t *x = (const uint16_t *)p.x + at, *f = (const uint16_t *)p.f + at;
+    const uint16_t *g = p.g ? (const uint16_t *)p.g + at : nullptr;
+    const uint16_t *dy = (const uint16_t *)p.dy + n * p.t * p.ldy;
+    uint16_t *dx = (uint16_t *)p.dx + at, *df = (uint16_t *)p.df + at;
+    uint16_t *dg = p.g ? (uint16_t *)p.dg + at : nullptr;
+    float r = p.dht ? p.dht[n] : 0.f, total = 0.f;
+    for (int64_t k = stretches - 1; k >= 0; --k) {
+        const int64_t lo = k * SAVE, hi = lo + SAVE < p.t ? lo + SAVE : p.t;
+        float h = p.saved[n * stretches + k], part = 0.f;
+        for (int64_t t = lo; t < hi && t < len; ++t) {
+            float a, b;
+            hs[t - lo][lane] = h;
+            gate(from16<T>(f[t * p.ld]), bias, a, b);
+            h = a * h + b * from16<T>(x[t * p.ld]);
+        }
+        for (int64_t t = hi - 1; t >= lo; --t) {
+            float vx = 0.f, vf = 0.f, vg = 0.f;
+            if (t < len) {
+                float a, b;
+                gate(from16<T>(f[t * p.ld]), bias, a, b);
+                const float xv = from16<T>(x[t * p.ld]), before = hs[t - lo][lane];
+                float own = from16<T>(dy[t * p.ldy]);
+                if (g) {
+                    const float gv = from16<T>(g[t * p.ld]), s = sigma(gv), sg = gv * s;
+                    vg = own * (s + sg * (1.f - s)) * (a * before + b * xv);
+                    own *= sg;
+                }
+                const float d = own + r;
+                vx = d * b;
+                vf = d * (before - xv) * (a * b);
+                r = a * d;
+                part += vf;
+            }
+            dx[t * p.ld] = (uint16_t)to16<T>(vx);
+            df[t * p.ld] = (uint16_t)to16<T>(vf);
+            if (dg) dg[t * p.ld] = (uint16_t)to16<T>(vg);
+        }
+        total += part;
+    }
+    if (p.dh0) p.dh0[n] = r;
+    if (p.part) p.part[n] = total;
+}
+
+constexpr int FW = 16, FS = 8, BW = 16, BS = 4;
+constexpr int FCHUNK = FW * FS, BCHUNK = BW * BS;
+
+int64_t chunks_of(const RecParams &p, bool backward) {
+    const int k = backward ? BCHUNK : FCHUNK;
+    return p.t <= SHORT_T || p.c == 1 ? 1 : ((int64_t)p.t + k - 1) / k;
+}
+
+// Places in groups of 2^gs: about as many groups, whose states are handed on
+// one after the other, as places in one.
+RecGrid grid_of(const RecParams &p, bool backward) {
+    RecGrid q{};
+    const int64_t chunks = chunks_of(p, backward);
+    q.cols = (p.c + COLS - 1) / COLS;
+    q.chunks = (int32_t)chunks;
+    while (q.gs < MAX_GS && chunks >> (2 * q.gs) > 1) ++q.gs;
+    q.groups = (int32_t)((chunks + (1 << q.gs) - 1) >> q.gs);
+    return q;
+}
+
+int64_t word_count(const RecParams &p, bool backward) {
+    const RecGrid q = grid_of(p, backward);
+    return q.chunks > 1 ? (int64_t)p.n * ((int64_t)q.chunks + q.groups) * p.c : 0;
+}
+
+template <class T, bool G>
+hipError_t run(const RecParams &p, bool backward, hipStream_t st) {
+    const int cols = (p.c + COLS - 1) / COLS;
+    if (p.c == 1) {
+        const dim3 grid((p.n + 63) / 64);
+        if (backward)
+            hipLaunchKernelGGL((recurrence_bwd_single_kernel<T>), grid, dim3(64), 0, st, p);
+        else
+            hipLaunchKernelGGL((recurrence_fwd_single_kernel<T>), grid, dim3(64), 0, st, p);
+        return hipGetLastError();
+    }
+    if (p.t <= SHORT_T) {
+        const dim3 grid(cols, p.n < 65535 ? p.n : 65535);
+        if (backward)
+            hipLaunchKernelGGL((recurrence_bwd_short_kernel<T, G>), grid, dim3(64), 0, st, p);
+        else
+            hipLaunchKernelGGL((recurrence_fwd_short_kernel<T>), grid, dim3(64), 0, st, p);
+        return hipGetLastError();
+    }
+    RecGrid q = grid_of(p, backward);
+    const int64_t blocks = (int64_t)q.chunks * cols * p.n;
+    if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+    if (q.chunks > 1) {
+        q.words = (uint64_t *)p.ws;
+        q.states = q.words + (int64_t)p.n * q.chunks * p.c;
+        const int64_t nb = (word_count(p, backward) + 255) / 256;
+        hipLaunchKernelGGL(recurrence_words_kernel, dim3((uint32_t)(nb < 2048 ? nb : 2048)), dim3(256), 0, st, q,
+                           (int64_t)p.n, p.c, backward ? p.dht : p.h0);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (backward)
+        hipLaunchKernelGGL((recurrence_bwd_kernel<T, G, BW, BS>), dim3((uint32_t)blocks), dim3(64 * BW), 0, st, p, q);
+    else
+        hipLaunchKernelGGL((recurrence_fwd_kernel<T, G, FW, FS>), dim3((uint32_t)blocks), dim3(64 * FW), 0, st, p, q);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-int64_t recurrence_bwd_parts(const RecParams &p) { return p.n; }
+int64_t recurrence_bwd_parts(const RecParams &p) { return p.n * chunks_of(p, true); }
+
+// Words first (8-byte aligned), then, backward, the partial sums of dbias.
+size_t recurrence_words_bytes(const RecParams &p, bool backward) {
+    return sizeof(uint64_t) * (size_t)word_count(p, backward);
+}
 
 size_t recurrence_ws(const RecParams &p, bool backward) {
-    if (!backward) return 0;
+    const size_t words = recurrence_words_bytes(p, backward);
+    if (!backward) return words;
     const int64_t parts = recurrence_bwd_parts(p);
-    return sizeof(float) * (size_t)((parts + colsum_extra(parts)) * p.c);
+    return words + sizeof(float) * (size_t)((parts + colsum_extra(parts)) * p.c);
+}
+
+static hipError_t launch(int dtype, const RecParams &p, bool backward, hipStream_t st) {
+    if (p.n <= 0) return hipSuccess;
+    if (dtype == Half::id)
+        return p.g ? run<Half, true>(p, backward, st) : run<Half, false>(p, backward, st);
+    return p.g ? run<BFloat, true>(p, backward, st) : run<BFloat, false>(p, backward, st);
 }
 
 hipError_t launch_recurrence_fwd(int dtype, const RecParams &p, hipStream_t st) {
-    if (p.n <= 0) return hipSuccess;
-    const dim3 grid((p.c + 63) / 64, p.n < 65535 ? p.n : 65535);
-    if (dtype == Half::id)
-        hipLaunchKernelGGL((recurrence_fwd_kernel<Half>), grid, dim3(64), 0, st, p);
-    else
-        hipLaunchKernelGGL((recurrence_fwd_kernel<BFloat>), grid, dim3(64), 0, st, p);
-    return hipGetLastError();
+    return launch(dtype, p, false, st);
 }
 
 hipError_t launch_recurrence_bwd(int dtype, const RecParams &p, hipStream_t st) {
-    if (p.n <= 0) return hipSuccess;
-    const dim3 grid((p.c + 63) / 64, p.n < 65535 ? p.n : 65535);
-    if (dtype == Half::id)
-        hipLaunchKernelGGL((recurrence_bwd_kernel<Half>), grid, dim3(64), 0, st, p);
-    else
-        hipLaunchKernelGGL((recurrence_bwd_kernel<BFloat>), grid, dim3(64), 0, st, p);
-    return hipGetLastError();
+    return launch(dtype, p, true, st);
 }
 
 }  // namespace nnconv
