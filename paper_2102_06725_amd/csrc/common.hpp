@@ -80,6 +80,24 @@ __device__ __forceinline__ uint32_t to16<BFloat>(float v) {
     return (uint32_t)__builtin_bit_cast(uint16_t, h);
 }
 
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// Two of them in one register.
+template <class T>
+__device__ __forceinline__ uint32_t pack16(float lo, float hi);
+
+template <>
+__device__ __forceinline__ uint32_t pack16<Half>(float lo, float hi) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){lo, hi}, f16x2));
+}
+
+template <>
+__device__ __forceinline__ uint32_t pack16<BFloat>(float lo, float hi) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){lo, hi}, bf16x2));
+}
+
 // 16-bit storage -> fp32 (exact).
 template <class T>
 __device__ __forceinline__ float from16(uint32_t bits);

@@ -13,6 +13,8 @@
 //     registers.
 // Whether a token takes part is the same for a whole wave, so lengths
 // and the end of the sequence cost no divergence.
+#include <type_traits>
+
 #include "launch.hpp"
 
 namespace nnconv {
@@ -26,19 +28,23 @@ constexpr int SHORT_T = 16;               // up to here one lane walks all token
 
 typedef uint32_t __attribute__((aligned(2))) u32_any;  // 4-byte access at any element
 
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float Z_MAX = 80.f * LOG2E;
+
 // The gate a = sigma(z) and b = 1 - a = sigma(-z), each to full relative
 // precision: with a near 1 the difference 1 - a would keep few bits of the
-// long memories' rates.
+// long memories' rates.  bias is the negated bias times log2(e): -z log2(e) is one
+// multiply-add.  The limits let a NaN through.
 __device__ __forceinline__ void gate(float f, float bias, float &a, float &b) {
-    float z = f + bias;
-    z = z > 80.f ? 80.f : z < -80.f ? -80.f : z;  // a NaN stays
-    const float e = __expf(-z);
+    float z = __builtin_fmaf(f, -LOG2E, bias);
+    z = __builtin_elementwise_minimum(__builtin_elementwise_maximum(z, -Z_MAX), Z_MAX);
+    const float e = __builtin_amdgcn_exp2f(z);
     a = __builtin_amdgcn_rcpf(1.0f + e);
     b = e * a;
 }
 
 __device__ __forceinline__ float sigma(float v) {
-    return __builtin_amdgcn_rcpf(1.0f + __expf(-v));
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -LOG2E));
 }
 
 __device__ __forceinline__ int length_of(const RecParams &p, int n) {
@@ -50,7 +56,7 @@ __device__ __forceinline__ int length_of(const RecParams &p, int n) {
 // The two channels of a lane.  c >= 2: a lane at or past the last channel
 // loads the last two, and takes the second of them if it is alone there.
 struct Lane {
-    int at;            // first channel loaded
+    uint32_t at;       // first channel loaded
     int k0, k1;        // channels of per-channel fp32 arrays and words, in range
     uint32_t shift;    // 16: the first channel is the second half of the load
     bool first, second;  // channels that exist
@@ -66,25 +72,60 @@ struct Lane {
 };
 
 template <class T>
-__device__ __forceinline__ void unpack(uint32_t v, float o[2]) {
-    o[0] = from16<T>(v & 0xFFFFu);
-    o[1] = from16<T>(v >> 16);
+__device__ __forceinline__ void unpack(uint32_t v, float o[2]);
+
+template <>
+__device__ __forceinline__ void unpack<Half>(uint32_t v, float o[2]) {
+    o[0] = from16<Half>(v & 0xFFFFu);
+    o[1] = from16<Half>(v >> 16);
+}
+
+template <>
+__device__ __forceinline__ void unpack<BFloat>(uint32_t v, float o[2]) {
+    o[0] = __builtin_bit_cast(float, v << 16);
+    o[1] = __builtin_bit_cast(float, v & 0xFFFF0000u);
+}
+
+// The token at `row`, an address that is the same for the whole wave: in scalar
+// registers, so that an access costs no address arithmetic on the vector units.
+typedef __attribute__((address_space(1))) char global_char;
+
+__device__ __forceinline__ global_char *uniform(const void *row) {
+    uint64_t v = (uint64_t)row;
+    asm("" : "+s"(v));
+    return (global_char *)v;
+}
+
+typedef __attribute__((address_space(1))) u32_any global_u32_any;
+typedef __attribute__((address_space(1))) uint16_t global_u16;
+
+// A lane's two channels of a token.
+__device__ __forceinline__ uint32_t load2(const void *row, const Lane &L) {
+    return *(const global_u32_any *)(uniform(row) + (uint32_t)(2 * L.at)) >> L.shift;
+}
+
+// Stores of a wave whose 128 channels all exist, and of any.
+template <class T>
+__device__ __forceinline__ void store2_full(void *row, const Lane &L, float v0, float v1) {
+    __builtin_nontemporal_store(pack16<T>(v0, v1), (global_u32_any *)(uniform(row) + (uint32_t)(2 * L.at)));
 }
 
 template <class T>
-__device__ __forceinline__ void store2(uint16_t *q, const Lane &L, float v0, float v1) {
-    const uint32_t lo = to16<T>(v0) & 0xFFFFu;
+__device__ __forceinline__ void store2(void *row, const Lane &L, float v0, float v1) {
+    global_char *q = uniform(row) + (uint32_t)(2 * L.at);
     if (L.second)
-        *(u32_any *)q = lo | (to16<T>(v1) << 16);
+        *(global_u32_any *)q = pack16<T>(v0, v1);
     else if (L.first)
-        q[L.shift >> 4] = (uint16_t)lo;  // q is the address of channel L.at
+        ((global_u16 *)q)[L.shift >> 4] = (uint16_t)to16<T>(v0);
 }
 
 // ---- words between chunks ------------------------------------------------------
 
 // Chunks are taken in the direction of the recurrence: place k of a sequence.
 // Two arrays of 64-bit words, all ones until written: the (A, H) of every place,
-// and the state in front of every group of 2^gs places.  A word is stored and loaded at
+// and the state in front of every group of 2^gs places: a place waits for the pairs in front of
+// it in its group, all at once, and for the group's state, which the last place of
+// the group before hands on.  A word is stored and loaded at
 // once, so it needs no flag and no ordering with other memory.  Which words are
 // composed, and in which order, depends on the sizes alone, so that results
 // do not depend on which workgroup came first.
@@ -93,7 +134,7 @@ struct RecGrid {
     uint64_t *words;   // [n][chunks][c], null for a single chunk
     uint64_t *states;  // [n][groups][c]
 };
-constexpr int MAX_GS = 4;
+constexpr int GROUP = 16;  // places of a group at most
 constexpr uint64_t EMPTY = ~0ull;
 constexpr int POLLS = 4096;
 
@@ -110,24 +151,35 @@ __device__ __forceinline__ void put(uint64_t *row, const Lane &L, const float a[
     if (L.second) __hip_atomic_store(row + L.k1, word(a[1], h[1]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-__device__ __forceinline__ bool get(const uint64_t *row, const Lane &L, float a[2], float h[2]) {
-    const uint64_t v0 = __hip_atomic_load(row + L.k0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const uint64_t v1 = __hip_atomic_load(row + L.k1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    a[0] = word_a(v0);
-    a[1] = word_a(v1);
-    h[0] = word_h(v0);
-    h[1] = word_h(v1);
-    return !__any(v0 == EMPTY || v1 == EMPTY);
-}
+// A lane's two words of a row.
+struct Words {
+    uint64_t v0, v1;
 
-// Waits for a row's words, for POLLS looks at most.
-__device__ __forceinline__ bool wait(const uint64_t *row, const Lane &L, float a[2], float h[2]) {
-    for (int k = 0; k < POLLS; ++k) {
-        if (get(row, L, a, h)) return true;
-        __builtin_amdgcn_s_sleep(1);
+    __device__ __forceinline__ void load(const uint64_t *row, const Lane &L) {
+        v0 = __hip_atomic_load(row + L.k0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        v1 = __hip_atomic_load(row + L.k1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    return false;
-}
+
+    // Whether the whole wave has its words.
+    __device__ __forceinline__ bool there() const { return !__any(v0 == EMPTY || v1 == EMPTY); }
+
+    // Looks again until they are there, POLLS times at most.
+    __device__ __forceinline__ bool wait(const uint64_t *row, const Lane &L) {
+        for (int k = 0; !there(); ++k) {
+            if (k == POLLS) return false;
+            __builtin_amdgcn_s_sleep(1);
+            load(row, L);
+        }
+        return true;
+    }
+
+    __device__ __forceinline__ void unpack(float a[2], float h[2]) const {
+        a[0] = word_a(v0);
+        a[1] = word_a(v1);
+        h[0] = word_h(v0);
+        h[1] = word_h(v1);
+    }
+};
 
 // Before each split call: every word empty but the states in front of the
 // first places.
@@ -159,18 +211,30 @@ template <int W, class F>
 __device__ __forceinline__ void carry_in(const RecGrid &q, int n, int32_t c, int k, const Lane &L, int w,
                                          int own, const float ca[2], const float ch[2], F chunk_pair,
                                          float out[2]) {
-    __shared__ f32x4 pairs[1 << MAX_GS][64];
+    __shared__ f32x4 pairs[GROUP][64];
     __shared__ float into[2][64];
-    const int lane = threadIdx.x & 63, g = k >> q.gs, i = k - (g << q.gs);
-    const bool last = i + 1 == 1 << q.gs;
+    const int lane = threadIdx.x & 63, group = 1 << q.gs, g = k >> q.gs, i = k & (group - 1);
+    const bool last = i + 1 == group;
     uint64_t *words = q.words + (int64_t)n * q.chunks * c, *states = q.states + (int64_t)n * q.groups * c;
     if (w == own && !last && k + 1 < q.chunks) put(words + (int64_t)k * c, L, ca, ch);
-    for (int j = w; j < i; j += W) {
+    constexpr int R = (GROUP + W - 1) / W;
+    Words v[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (w + r * W < i) v[r].load(words + (int64_t)(g * group + w + r * W) * c, L);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int j = w + r * W;
+        if (j >= i) break;
         float a[2], h[2];
-        const int place = (g << q.gs) + j;
-        if (!wait(words + (int64_t)place * c, L, a, h)) chunk_pair(place, a, h);
+        if (v[r].wait(words + (int64_t)(g * group + j) * c, L))
+            v[r].unpack(a, h);
+        else
+            chunk_pair(g * group + j, a, h);
         pairs[j][lane] = f32x4{a[0], h[0], a[1], h[1]};
     }
+    Words s;
+    if (w == own) s.load(states + (int64_t)g * c, L);
     __syncthreads();
     if (w == own) {
         float A[2] = {1.f, 1.f}, H[2] = {0.f, 0.f}, no[2], h[2];
@@ -179,22 +243,25 @@ __device__ __forceinline__ void carry_in(const RecGrid &q, int n, int32_t c, int
             const float ea[2] = {e[0], e[2]}, eh[2] = {e[1], e[3]};
             compose(A, H, ea, eh);
         }
-        if (!wait(states + (int64_t)g * c, L, no, h)) {
+        if (s.wait(states + (int64_t)g * c, L)) {
+            s.unpack(no, h);
+        } else {
             // from the nearest state there is; the first one was there before the call
             int from = g;
-            while (from > 0 && !get(states + (int64_t)from * c, L, no, h)) --from;
-            if (from == 0) get(states, L, no, h);
+            do {
+                from = from > 0 ? from - 1 : 0;
+                s.load(states + (int64_t)from * c, L);
+            } while (from > 0 && !s.there());
+            s.unpack(no, h);
             for (; from < g; ++from) {
                 float ga[2] = {1.f, 1.f}, gh[2] = {0.f, 0.f}, a[2], b[2];
-                for (int j = 0; j < 1 << q.gs; ++j) {
-                    chunk_pair((from << q.gs) + j, a, b);
-                    if (j + 1 < 1 << q.gs) {
-                        compose(ga, gh, a, b);
-                        continue;
-                    }
-                    for (int u = 0; u < 2; ++u)
-                        h[u] = __builtin_fmaf(a[u], __builtin_fmaf(ga[u], h[u], gh[u]), b[u]);
+                for (int j = 0; j + 1 < group; ++j) {
+                    chunk_pair(from * group + j, a, b);
+                    compose(ga, gh, a, b);
                 }
+                chunk_pair(from * group + group - 1, a, b);
+                for (int u = 0; u < 2; ++u)
+                    h[u] = __builtin_fmaf(a[u], __builtin_fmaf(ga[u], h[u], gh[u]), b[u]);
             }
         }
         h[0] = __builtin_fmaf(A[0], h[0], H[0]);
@@ -227,13 +294,13 @@ __global__ __launch_bounds__(64) void recurrence_fwd_short_kernel(const RecParam
             h[1] = p.h0[n * p.c + L.k1];
         }
         if (p.bias) {
-            bias[0] = p.bias[L.k0];
-            bias[1] = p.bias[L.k1];
+            bias[0] = p.bias[L.k0] * -LOG2E;
+            bias[1] = p.bias[L.k1] * -LOG2E;
         }
-        const int64_t at = n * p.t * p.ld + L.at;
+        const int64_t at = n * p.t * p.ld;
         const uint16_t *x = (const uint16_t *)p.x + at, *f = (const uint16_t *)p.f + at;
         const uint16_t *g = p.g ? (const uint16_t *)p.g + at : nullptr;
-        uint16_t *y = (uint16_t *)p.y + n * p.t * p.ldy + L.at;
+        uint16_t *y = (uint16_t *)p.y + n * p.t * p.ldy;
         if (p.saved && p.t > 0) {  // t <= SAVE: one state
             if (L.first) p.saved[n * p.c + L.k0] = h[0];
             if (L.second) p.saved[n * p.c + L.k1] = h[1];
@@ -242,9 +309,9 @@ __global__ __launch_bounds__(64) void recurrence_fwd_short_kernel(const RecParam
             float o[2] = {0.f, 0.f};
             if (t < len) {
                 float xv[2], fv[2], gv[2];
-                unpack<T>(*(const u32_any *)(x + t * p.ld) >> L.shift, xv);
-                unpack<T>(*(const u32_any *)(f + t * p.ld) >> L.shift, fv);
-                if (g) unpack<T>(*(const u32_any *)(g + t * p.ld) >> L.shift, gv);
+                unpack<T>(load2(x + t * p.ld, L), xv);
+                unpack<T>(load2(f + t * p.ld, L), fv);
+                if (g) unpack<T>(load2(g + t * p.ld, L), gv);
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     float a, b;
@@ -266,7 +333,7 @@ __global__ __launch_bounds__(64) void recurrence_fwd_short_kernel(const RecParam
 template <class T, int W, int S>
 __device__ void walk_fwd(const RecParams &p, int64_t n, const Lane &L, int lo, int len,
                          const float bias[2], float A[2], float H[2]) {
-    const int64_t at = n * p.t * p.ld + L.at;
+    const int64_t at = n * p.t * p.ld;
     const uint16_t *x = (const uint16_t *)p.x + at, *f = (const uint16_t *)p.f + at;
     A[0] = A[1] = 1.f;
     H[0] = H[1] = 0.f;
@@ -274,8 +341,8 @@ __device__ void walk_fwd(const RecParams &p, int64_t n, const Lane &L, int lo, i
         float a1[2] = {1.f, 1.f}, h1[2] = {0.f, 0.f};
         for (int t = lo + w * S; t < min(lo + w * S + S, len); ++t) {
             float xv[2], fv[2];
-            unpack<T>(*(const u32_any *)(x + t * p.ld) >> L.shift, xv);
-            unpack<T>(*(const u32_any *)(f + t * p.ld) >> L.shift, fv);
+            unpack<T>(load2(x + t * p.ld, L), xv);
+            unpack<T>(load2(f + t * p.ld, L), fv);
             for (int k = 0; k < 2; ++k) {
                 float a, b;
                 gate(fv[k], bias[k], a, b);
@@ -290,7 +357,7 @@ __device__ void walk_fwd(const RecParams &p, int64_t n, const Lane &L, int lo, i
 }
 
 template <class T, bool G, int W, int S>
-__global__ __launch_bounds__(64 * W) void recurrence_fwd_kernel(const RecParams p, const RecGrid q) {
+__global__ __launch_bounds__(64 * W, 4) void recurrence_fwd_kernel(const RecParams p, const RecGrid q) {
     static_assert(SAVE % S == 0, "saved states lie at a wave's first token");
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = blockIdx.x % q.cols, rest = blockIdx.x / q.cols;
@@ -298,47 +365,66 @@ __global__ __launch_bounds__(64 * W) void recurrence_fwd_kernel(const RecParams 
     const Lane L(col * COLS + 2 * lane, p.c);
     const int len = length_of(p, n);
     const int t0 = chunk * (W * S) + w * S, last = len > 0 ? len - 1 : 0;
-    const int64_t at = (int64_t)n * p.t * p.ld + L.at;
+    const int64_t at = (int64_t)n * p.t * p.ld;
     const uint16_t *x = (const uint16_t *)p.x + at, *f = (const uint16_t *)p.f + at;
     const uint16_t *g = G ? (const uint16_t *)p.g + at : nullptr;
     uint32_t xr[S], fr[S], gr[S];
+    const bool whole = t0 + S <= len;           // every token takes part
+    const bool full = (col + 1) * COLS <= p.c;  // every channel exists
+    int64_t o = (int64_t)min(t0, last) * p.ld;
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-        const int64_t o = (int64_t)min(t0 + s, last) * p.ld;
-        xr[s] = *(const u32_any *)(x + o);
-        fr[s] = *(const u32_any *)(f + o);
-        if (G) gr[s] = *(const u32_any *)(g + o);
+        xr[s] = load2(x + o, L);
+        fr[s] = load2(f + o, L);
+        o += t0 + s < last ? p.ld : 0;
     }
     float bias[2] = {0.f, 0.f};
     if (p.bias) {
-        bias[0] = p.bias[L.k0];
-        bias[1] = p.bias[L.k1];
+        bias[0] = p.bias[L.k0] * -LOG2E;
+        bias[1] = p.bias[L.k1] * -LOG2E;
     }
     float a[S][2], u[S][2], A[2] = {1.f, 1.f}, H[2] = {0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < S; ++s) {
         float xv[2], fv[2];
-        unpack<T>(xr[s] >> L.shift, xv);
-        unpack<T>(fr[s] >> L.shift, fv);
-        const bool live = t0 + s < len;
+        unpack<T>(xr[s], xv);
+        unpack<T>(fr[s], fv);
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             float b;
             gate(fv[k], bias[k], a[s][k], b);
             u[s][k] = b * xv[k];
-            if (!live) {
-                a[s][k] = 1.f;
-                u[s][k] = 0.f;
-            }
+        }
+    }
+    if (!whole)
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                if (t0 + s >= len) {
+                    a[s][k] = 1.f;
+                    u[s][k] = 0.f;
+                }
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
             H[k] = __builtin_fmaf(a[s][k], H[k], u[s][k]);
             A[k] *= a[s][k];
         }
-    }
     A[0] = fmaxf(A[0], A_MIN);
     A[1] = fmaxf(A[1], A_MIN);
     __shared__ f32x4 part[W][64];
     part[w][lane] = f32x4{A[0], H[0], A[1], H[1]};
     __syncthreads();
+    if (G) {  // not needed before the state is there: on their way during the wait
+        o = (int64_t)min(t0, last) * p.ld;
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            gr[s] = load2(g + o, L);
+            o += t0 + s < last ? p.ld : 0;
+        }
+    }
     // what the waves in front make of the chunk's first state
     float pa[2] = {1.f, 1.f}, ph[2] = {0.f, 0.f};
     for (int v = 0; v < w; ++v) {
@@ -364,20 +450,30 @@ __global__ __launch_bounds__(64 * W) void recurrence_fwd_kernel(const RecParams 
         if (L.first) to[L.k0] = h[0];
         if (L.second) to[L.k1] = h[1];
     }
-    uint16_t *y = (uint16_t *)p.y + (int64_t)n * p.t * p.ldy + L.at;
+    uint16_t *y = (uint16_t *)p.y + (int64_t)n * p.t * p.ldy;
+    y += (int64_t)t0 * p.ldy;
+    auto finish = [&](auto checked) {
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-        const int t = t0 + s;
-        float o[2], gv[2];
-        if (G) unpack<T>(gr[s] >> L.shift, gv);
+        for (int s = 0; s < S; ++s, y += p.ldy) {
+            const int t = t0 + s;
+            float o[2], gv[2];
+            if (G) unpack<T>(gr[s], gv);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            h[k] = a[s][k] * h[k] + u[s][k];
-            o[k] = G ? h[k] * (gv[k] * sigma(gv[k])) : h[k];
-            if (t >= len) o[k] = 0.f;
+            for (int k = 0; k < 2; ++k) {
+                h[k] = a[s][k] * h[k] + u[s][k];
+                o[k] = G ? h[k] * (gv[k] * sigma(gv[k])) : h[k];
+                if (checked && t >= len) o[k] = 0.f;
+            }
+            if (!checked)
+                store2_full<T>(y, L, o[0], o[1]);
+            else if (t < p.t)
+                store2<T>(y, L, o[0], o[1]);
         }
-        if (t < p.t) store2<T>(y + t * p.ldy, L, o[0], o[1]);
-    }
+    };
+    if (whole && full)
+        finish(std::false_type{});
+    else
+        finish(std::true_type{});
     if (p.ht && chunk == q.chunks - 1 && w == W - 1) {
         if (L.first) p.ht[(int64_t)n * p.c + L.k0] = h[0];
         if (L.second) p.ht[(int64_t)n * p.c + L.k1] = h[1];
@@ -394,7 +490,7 @@ template <class T, bool G>
 struct Grad {
     float a[2], b[2], x[2], own[2], dg[2];  // dg without the factor h_t
 
-    __device__ __forceinline__ void make(uint32_t xq, uint32_t fq, uint32_t gq, uint32_t dyq, const float bias[2], bool live) {
+    __device__ __forceinline__ void make(uint32_t xq, uint32_t fq, uint32_t gq, uint32_t dyq, const float bias[2]) {
         float fv[2], gv[2], dy[2];
         unpack<T>(xq, x);
         unpack<T>(fq, fv);
@@ -410,11 +506,13 @@ struct Grad {
                 own[k] = dy[k] * sg;
                 dg[k] = dy[k] * (s + sg * (1.f - s));
             }
-            if (!live) {  // the state passes through, nothing else happens
-                a[k] = 1.f;
-                b[k] = x[k] = own[k] = dg[k] = 0.f;
-            }
         }
+    }
+
+    // A token past the length: the state passes through, nothing else happens.
+    __device__ __forceinline__ void pass() {
+        a[0] = a[1] = 1.f;
+        b[0] = b[1] = x[0] = x[1] = own[0] = own[1] = dg[0] = dg[1] = 0.f;
     }
 };
 
@@ -427,8 +525,8 @@ __global__ __launch_bounds__(64) void recurrence_bwd_short_kernel(const RecParam
     const Lane L(blockIdx.x * COLS + 2 * lane, p.c);
     float bias[2] = {0.f, 0.f};
     if (p.bias) {
-        bias[0] = p.bias[L.k0];
-        bias[1] = p.bias[L.k1];
+        bias[0] = p.bias[L.k0] * -LOG2E;
+        bias[1] = p.bias[L.k1] * -LOG2E;
     }
     for (int64_t n = blockIdx.y; n < p.n; n += gridDim.y) {
         const int len = length_of(p, (int)n);
@@ -437,18 +535,18 @@ __global__ __launch_bounds__(64) void recurrence_bwd_short_kernel(const RecParam
             r[0] = p.dht[n * p.c + L.k0];
             r[1] = p.dht[n * p.c + L.k1];
         }
-        const int64_t at = n * p.t * p.ld + L.at;
+        const int64_t at = n * p.t * p.ld;
         const uint16_t *x = (const uint16_t *)p.x + at, *f = (const uint16_t *)p.f + at;
         const uint16_t *g = G ? (const uint16_t *)p.g + at : nullptr;
-        const uint16_t *dy = (const uint16_t *)p.dy + n * p.t * p.ldy + L.at;
+        const uint16_t *dy = (const uint16_t *)p.dy + n * p.t * p.ldy;
         uint16_t *dx = (uint16_t *)p.dx + at, *df = (uint16_t *)p.df + at;
         uint16_t *dg = G ? (uint16_t *)p.dg + at : nullptr;
         if (len > 0) {
             float h[2] = {p.saved[n * p.c + L.k0], p.saved[n * p.c + L.k1]};
             for (int t = 0; t < len; ++t) {
                 float xv[2], fv[2];
-                unpack<T>(*(const u32_any *)(x + t * p.ld) >> L.shift, xv);
-                unpack<T>(*(const u32_any *)(f + t * p.ld) >> L.shift, fv);
+                unpack<T>(load2(x + t * p.ld, L), xv);
+                unpack<T>(load2(f + t * p.ld, L), fv);
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     float a, b;
@@ -462,8 +560,8 @@ __global__ __launch_bounds__(64) void recurrence_bwd_short_kernel(const RecParam
             float vx[2] = {0.f, 0.f}, vf[2] = {0.f, 0.f}, vg[2] = {0.f, 0.f};
             if (t < len) {
                 Grad<T, G> e;
-                e.make(*(const u32_any *)(x + t * p.ld) >> L.shift, *(const u32_any *)(f + t * p.ld) >> L.shift,
-                       G ? *(const u32_any *)(g + t * p.ld) >> L.shift : 0u, *(const u32_any *)(dy + t * p.ldy) >> L.shift, bias, true);
+                e.make(load2(x + t * p.ld, L), load2(f + t * p.ld, L),
+                       G ? load2(g + t * p.ld, L) : 0u, load2(dy + t * p.ldy, L), bias);
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const float before = hs[t][k][lane], d = e.own[k] + r[k];
@@ -493,10 +591,10 @@ __global__ __launch_bounds__(64) void recurrence_bwd_short_kernel(const RecParam
 template <class T, bool G, int W, int S>
 __device__ void walk_bwd(const RecParams &p, int64_t n, const Lane &L, int lo, int len,
                          const float bias[2], float A[2], float R[2]) {
-    const int64_t at = n * p.t * p.ld + L.at;
+    const int64_t at = n * p.t * p.ld;
     const uint16_t *f = (const uint16_t *)p.f + at;
     const uint16_t *g = G ? (const uint16_t *)p.g + at : nullptr;
-    const uint16_t *dy = (const uint16_t *)p.dy + n * p.t * p.ldy + L.at;
+    const uint16_t *dy = (const uint16_t *)p.dy + n * p.t * p.ldy;
     A[0] = A[1] = 1.f;
     R[0] = R[1] = 0.f;
     for (int w = W - 1; w >= 0; --w) {
@@ -505,14 +603,14 @@ __device__ void walk_bwd(const RecParams &p, int64_t n, const Lane &L, int lo, i
         for (int t = first; t < min(first + S, len); ++t)
             for (int k = 0; k < 2; ++k) {  // the product in the order of the tokens
                 float fv[2], a, b;
-                unpack<T>(*(const u32_any *)(f + t * p.ld) >> L.shift, fv);
+                unpack<T>(load2(f + t * p.ld, L), fv);
                 gate(fv[k], bias[k], a, b);
                 a1[k] *= a;
             }
         for (int t = min(first + S, len) - 1; t >= first; --t) {
             Grad<T, G> e;
-            e.make(0u, *(const u32_any *)(f + t * p.ld) >> L.shift, G ? *(const u32_any *)(g + t * p.ld) >> L.shift : 0u,
-                   *(const u32_any *)(dy + t * p.ldy) >> L.shift, bias, true);
+            e.make(0u, load2(f + t * p.ld, L), G ? load2(g + t * p.ld, L) : 0u,
+                   load2(dy + t * p.ldy, L), bias);
             for (int k = 0; k < 2; ++k) r1[k] = e.a[k] * (e.own[k] + r1[k]);
         }
         a1[0] = fmaxf(a1[0], A_MIN);
@@ -522,7 +620,7 @@ __device__ void walk_bwd(const RecParams &p, int64_t n, const Lane &L, int lo, i
 }
 
 template <class T, bool G, int W, int S>
-__global__ __launch_bounds__(64 * W) void recurrence_bwd_kernel(const RecParams p, const RecGrid q) {
+__global__ __launch_bounds__(64 * W, 2) void recurrence_bwd_kernel(const RecParams p, const RecGrid q) {
     static_assert((W * S) % SAVE == 0 && SAVE % S == 0, "a chunk is whole saved stretches");
     constexpr int RUN = SAVE / S;  // waves that start from one saved state
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -531,18 +629,23 @@ __global__ __launch_bounds__(64 * W) void recurrence_bwd_kernel(const RecParams 
     const Lane L(col * COLS + 2 * lane, p.c);
     const int len = length_of(p, n);
     const int t0 = chunk * (W * S) + w * S, last = len > 0 ? len - 1 : 0;
-    const int64_t at = (int64_t)n * p.t * p.ld + L.at;
+    const int64_t at = (int64_t)n * p.t * p.ld;
     const uint16_t *x = (const uint16_t *)p.x + at, *f = (const uint16_t *)p.f + at;
     const uint16_t *g = G ? (const uint16_t *)p.g + at : nullptr;
-    const uint16_t *dy = (const uint16_t *)p.dy + (int64_t)n * p.t * p.ldy + L.at;
+    const uint16_t *dy = (const uint16_t *)p.dy + (int64_t)n * p.t * p.ldy;
     uint32_t xr[S], fr[S], gr[S], dr[S];
+    const bool whole = t0 + S <= len;           // every token takes part
+    const bool full = (col + 1) * COLS <= p.c;  // every channel exists
+    int64_t o = (int64_t)min(t0, last) * p.ld;
+    dy += (int64_t)min(t0, last) * p.ldy;
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-        const int64_t t = min(t0 + s, last);
-        xr[s] = *(const u32_any *)(x + t * p.ld);
-        fr[s] = *(const u32_any *)(f + t * p.ld);
-        gr[s] = G ? *(const u32_any *)(g + t * p.ld) : 0u;
-        dr[s] = *(const u32_any *)(dy + t * p.ldy);
+        xr[s] = load2(x + o, L);
+        fr[s] = load2(f + o, L);
+        gr[s] = G ? load2(g + o, L) : 0u;
+        dr[s] = load2(dy, L);
+        o += t0 + s < last ? p.ld : 0;
+        dy += t0 + s < last ? p.ldy : 0;
     }
     float h[2] = {0.f, 0.f}, bias[2] = {0.f, 0.f};
     const int run0 = t0 - w % RUN * S;  // first token of the saved stretch
@@ -552,20 +655,23 @@ __global__ __launch_bounds__(64 * W) void recurrence_bwd_kernel(const RecParams 
         h[1] = from[L.k1];
     }
     if (p.bias) {
-        bias[0] = p.bias[L.k0];
-        bias[1] = p.bias[L.k1];
+        bias[0] = p.bias[L.k0] * -LOG2E;
+        bias[1] = p.bias[L.k1] * -LOG2E;
     }
     Grad<T, G> e[S];
     float A[2] = {1.f, 1.f}, H[2] = {0.f, 0.f}, R[2] = {0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-        e[s].make(xr[s] >> L.shift, fr[s] >> L.shift, gr[s] >> L.shift, dr[s] >> L.shift, bias, t0 + s < len);
+        e[s].make(xr[s], fr[s], gr[s], dr[s], bias);
+        if (!whole && t0 + s >= len) e[s].pass();
+    }
+#pragma unroll
+    for (int s = 0; s < S; ++s)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             H[k] = e[s].a[k] * H[k] + e[s].b[k] * e[s].x[k];
             A[k] *= e[s].a[k];
         }
-    }
 #pragma unroll
     for (int s = S - 1; s >= 0; --s)
 #pragma unroll
@@ -614,27 +720,38 @@ __global__ __launch_bounds__(64 * W) void recurrence_bwd_kernel(const RecParams 
     uint16_t *dx = (uint16_t *)p.dx + at, *df = (uint16_t *)p.df + at;
     uint16_t *dg = G ? (uint16_t *)p.dg + at : nullptr;
     float total[2] = {0.f, 0.f};
+    o = (int64_t)(t0 + S - 1) * p.ld;
+    auto finish = [&](auto checked) {
 #pragma unroll
-    for (int s = S - 1; s >= 0; --s) {
-        const int t = t0 + s;
-        float vx[2], vf[2], vg[2];
+        for (int s = S - 1; s >= 0; --s, o -= p.ld) {
+            const int t = t0 + s;
+            float vx[2], vf[2], vg[2];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const Grad<T, G> &m = e[s];
-            const float d = m.own[k] + r[k];
-            vx[k] = d * m.b[k];
-            vf[k] = d * (before[s][k] - m.x[k]) * (m.a[k] * m.b[k]);
-            vg[k] = m.dg[k] * (m.a[k] * before[s][k] + m.b[k] * m.x[k]);
-            if (t >= len) vx[k] = vf[k] = vg[k] = 0.f;
-            r[k] = m.a[k] * d;
-            total[k] += vf[k];
+            for (int k = 0; k < 2; ++k) {
+                const Grad<T, G> &m = e[s];
+                const float d = m.own[k] + r[k];
+                vx[k] = d * m.b[k];
+                vf[k] = d * (before[s][k] - m.x[k]) * (m.a[k] * m.b[k]);
+                vg[k] = m.dg[k] * (m.a[k] * before[s][k] + m.b[k] * m.x[k]);
+                if (checked && t >= len) vx[k] = vf[k] = vg[k] = 0.f;
+                r[k] = m.a[k] * d;
+                total[k] += vf[k];
+            }
+            if (!checked) {
+                store2_full<T>(dx + o, L, vx[0], vx[1]);
+                store2_full<T>(df + o, L, vf[0], vf[1]);
+                if (G) store2_full<T>(dg + o, L, vg[0], vg[1]);
+            } else if (t < p.t) {
+                store2<T>(dx + o, L, vx[0], vx[1]);
+                store2<T>(df + o, L, vf[0], vf[1]);
+                if (G) store2<T>(dg + o, L, vg[0], vg[1]);
+            }
         }
-        if (t < p.t) {
-            store2<T>(dx + t * p.ld, L, vx[0], vx[1]);
-            store2<T>(df + t * p.ld, L, vf[0], vf[1]);
-            if (G) store2<T>(dg + t * p.ld, L, vg[0], vg[1]);
-        }
-    }
+    };
+    if (whole && full)
+        finish(std::false_type{});
+    else
+        finish(std::true_type{});
     if (p.dh0 && chunk == 0 && w == 0) {
         if (L.first) p.dh0[(int64_t)n * p.c + L.k0] = r[0];
         if (L.second) p.dh0[(int64_t)n * p.c + L.k1] = r[1];
@@ -662,7 +779,7 @@ __global__ __launch_bounds__(64) void recurrence_fwd_single_kernel(const RecPara
     const int64_t n = (int64_t)blockIdx.x * 64 + threadIdx.x;
     if (n >= p.n) return;
     const int len = length_of(p, (int)n);
-    const float bias = p.bias ? p.bias[0] : 0.f;
+    const float bias = p.bias ? p.bias[0] * -LOG2E : 0.f;
     float h = p.h0 ? p.h0[n] : 0.f;
     const uint16_t *x = (const uint16_t *)p.x + n * p.t * p.ld, *f = (const uint16_t *)p.f + n * p.t * p.ld;
     const uint16_t *g = p.g ? (const uint16_t *)p.g + n * p.t * p.ld : nullptr;
@@ -692,7 +809,7 @@ __global__ __launch_bounds__(64) void recurrence_bwd_single_kernel(const RecPara
     const int64_t n = (int64_t)blockIdx.x * 64 + lane;
     if (n >= p.n) return;
     const int len = length_of(p, (int)n);
-    const float bias = p.bias ? p.bias[0] : 0.f;
+    const float bias = p.bias ? p.bias[0] * -LOG2E : 0.f;
     const int64_t at = n * p.t * p.ld, stretches = (p.t + SAVE - 1) / SAVE;
     const uint16_t *x = (const uint16_t *)p.x + at, *f = (const uint16_t *)p.f + at;
     const uint16_t *g = p.g ? (const uint16_t *)p.g + at : nullptr;
@@ -737,7 +854,7 @@ __global__ __launch_bounds__(64) void recurrence_bwd_single_kernel(const RecPara
     if (p.part) p.part[n] = total;
 }
 
-constexpr int FW = 16, FS = 8, BW = 16, BS = 4;
+constexpr int FW = 8, FS = 16, BW = 4, BS = 16;
 constexpr int FCHUNK = FW * FS, BCHUNK = BW * BS;
 
 int64_t chunks_of(const RecParams &p, bool backward) {
@@ -746,13 +863,13 @@ int64_t chunks_of(const RecParams &p, bool backward) {
 }
 
 // Places in groups of 2^gs: about as many groups, whose states are handed on
-// one after the other, as places in one.
+// one after the other, as places in one, whose pairs each place reads.
 RecGrid grid_of(const RecParams &p, bool backward) {
     RecGrid q{};
     const int64_t chunks = chunks_of(p, backward);
     q.cols = (p.c + COLS - 1) / COLS;
     q.chunks = (int32_t)chunks;
-    while (q.gs < MAX_GS && chunks >> (2 * q.gs) > 1) ++q.gs;
+    while (1 << q.gs < GROUP && chunks >> 2 * q.gs > 1) ++q.gs;
     q.groups = (int32_t)((chunks + (1 << q.gs) - 1) >> q.gs);
     return q;
 }
