@@ -74,12 +74,24 @@ struct Slot {
     }
 };
 
+// What a pass reads or writes once streams past the caches; but rows that do not start
+// on 16 bytes (ANY) share cache lines between lanes' loads, which then come from the cache.
+template <bool ANY>
 __device__ __forceinline__ u32x4 load8(const void *p, int64_t i) {
-    return *(const u32x4_any *)((const uint16_t *)p + i);
+    const u32x4_any *q = (const u32x4_any *)((const uint16_t *)p + i);
+    return ANY ? *q : __builtin_nontemporal_load(q);
 }
 
 __device__ __forceinline__ void store8(void *p, int64_t i, u32x4 v) {
-    *(u32x4_any *)((uint16_t *)p + i) = v;
+    __builtin_nontemporal_store(v, (u32x4_any *)((uint16_t *)p + i));
+}
+
+// The stored sum, kept in the caches where a training step's backward pass reads it again.
+__device__ __forceinline__ void store_sum(const NormParams &p, int64_t i, u32x4 v) {
+    if (p.rstd)
+        *(u32x4_any *)((uint16_t *)p.sum + i) = v;
+    else
+        store8(p.sum, i, v);
 }
 
 template <class T>
@@ -138,8 +150,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rmsnorm_fwd_kernel(cons
         for (int k = 0; k < V; ++k) {
             const Slot s(k * TPR + t, p.c);
             if (!live || !s.in) continue;
-            x[k] = load8(p.x, base + s.at);
-            if (p.residual) res[k] = load8(p.residual, base + s.at);
+            x[k] = load8<TAIL>(p.x, base + s.at);
+            if (p.residual) res[k] = load8<TAIL>(p.residual, base + s.at);
         }
         float ss = 0.f;
 #pragma unroll
@@ -172,7 +184,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rmsnorm_fwd_kernel(cons
                 unpack8<T>(x[k], y);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[e] = y[e] * rstd * gain[k][e];
-                if (p.sum) store8(p.sum, base + s.at, x[k]);
+                if (p.sum) store_sum(p, base + s.at, x[k]);
                 store8(p.y, base + s.at, pack8<T>(y));
             }
         } else {
@@ -183,7 +195,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rmsnorm_fwd_kernel(cons
                 most[k] = 0.f;
                 if (!live || !s.in) continue;
                 unpack8<T>(x[k], y[k]);
-                if (p.sum) store8(p.sum, base + s.at, x[k]);
+                if (p.sum) store_sum(p, base + s.at, x[k]);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     y[k][e] = y[k][e] * rstd * gain[k][e];
@@ -307,9 +319,9 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void rmsnorm_bwd_kernel(cons
         for (int k = 0; k < V; ++k) {
             const Slot s(k * TPR + t, p.c);
             if (!live || !s.in) continue;
-            x[k] = load8(p.sum, base + s.at);
-            dy[k] = load8(p.dy, base + s.at);
-            if (p.dsum) ds[k] = load8(p.dsum, base + s.at);  // before any store: dx may lie on it
+            x[k] = load8<TAIL>(p.sum, base + s.at);
+            dy[k] = load8<TAIL>(p.dy, base + s.at);
+            if (p.dsum) ds[k] = load8<TAIL>(p.dsum, base + s.at);  // before any store: dx may lie on it
         }
         float dot = 0.f;
 #pragma unroll
@@ -471,7 +483,7 @@ uint32_t blocks_for(int64_t rows, int per, int64_t most) {
     return (uint32_t)(n < most ? n : most);
 }
 
-constexpr int64_t FWD_BLOCKS = 2048, BWD_BLOCKS = 512, ANY_PARTS = 256;
+constexpr int64_t FWD_BLOCKS = 1 << 20, BWD_BLOCKS = 512, ANY_PARTS = 256;
 
 template <class T>
 void fwd(const NormParams &p, bool q8, hipStream_t st) {
