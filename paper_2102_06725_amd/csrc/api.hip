@@ -2186,8 +2186,8 @@ static nnconv_status adamw_check(const nnconv_adamw_tensor *t, int32_t n, int64_
     return *chunks > 0x7FFFFFFF ? NNCONV_ERR_INVALID_ARG : NNCONV_OK;
 }
 
-static size_t adamw_bytes(int32_t n, int64_t chunks) {
-    return (size_t)n * sizeof(nnconv_adamw_tensor) + (size_t)chunks * sizeof(AdamwChunk);
+static size_t adamw_bytes(int64_t chunks) {
+    return ADAMW_HEAD + (size_t)chunks * sizeof(AdamwChunk);
 }
 
 NNCONV_API nnconv_status nnconv_adamw_plan_size(const nnconv_adamw_tensor *tensors, int32_t n,
@@ -2196,7 +2196,7 @@ NNCONV_API nnconv_status nnconv_adamw_plan_size(const nnconv_adamw_tensor *tenso
     const nnconv_status st = adamw_check(tensors, n, &chunks);
     if (st != NNCONV_OK) return st;
     if (!bytes) return NNCONV_ERR_INVALID_ARG;
-    *bytes = adamw_bytes(n, chunks);
+    *bytes = adamw_bytes(chunks);
     return NNCONV_OK;
 }
 
@@ -2206,12 +2206,12 @@ NNCONV_API nnconv_status nnconv_adamw_plan_init(const nnconv_adamw_tensor *tenso
     int64_t chunks;
     const nnconv_status st = adamw_check(tensors, n, &chunks);
     if (st != NNCONV_OK) return st;
-    const size_t need = adamw_bytes(n, chunks);
-    if (!plan || (need > 0 && !table)) return NNCONV_ERR_INVALID_ARG;
+    const size_t need = adamw_bytes(chunks);
+    if (!plan || !table) return NNCONV_ERR_INVALID_ARG;
     if (table_bytes < need) return NNCONV_ERR_WORKSPACE;
     if (!aligned(table, 16)) return NNCONV_ERR_MISALIGNED;
     clear_stale_error();
-    TRY_HIP(launch_adamw_plan(tensors, n, adamw_table(table, n), (hipStream_t)hip_stream));
+    TRY_HIP(launch_adamw_plan(tensors, n, adamw_table(table), (hipStream_t)hip_stream));
     plan->table = table;
     plan->chunks = chunks;
     plan->tensors = n;
@@ -2232,7 +2232,7 @@ NNCONV_API nnconv_status nnconv_adamw_update(const nnconv_adamw_plan *plan, int3
         (overflow_flag && !aligned(overflow_flag, 4)) || !aligned(plan->table, 16))
         return NNCONV_ERR_MISALIGNED;
     clear_stale_error();
-    return hip_status(launch_adamw(adamw_table(plan->table, plan->tensors), plan->chunks, step, lr,
+    return hip_status(launch_adamw(adamw_table(plan->table), plan->chunks, step, lr,
                                    beta1, beta2, eps, seed, state, overflow_flag,
                                    (hipStream_t)hip_stream));
 }

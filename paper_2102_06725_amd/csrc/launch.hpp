@@ -472,15 +472,22 @@ hipError_t launch_recurrence_fwd(int dtype, const RecParams &p, hipStream_t st);
 hipError_t launch_recurrence_bwd(int dtype, const RecParams &p, hipStream_t st);
 
 // AdamW over a list of tensors, cut into chunks of ADAMW_CHUNK elements.
-constexpr int64_t ADAMW_CHUNK = 4096;
+constexpr int64_t ADAMW_CHUNK = 2048;
+constexpr size_t ADAMW_HEAD = 64;  // bytes in front of the chunks
 struct AdamwChunk {
-    int32_t tensor, index;
+    float *master;
+    const void *grad;
+    void *w16, *m, *v;
+    uint8_t *m_scale, *v_scale;
+    int64_t first;  // index of its first element in the tensor
+    int32_t count, tensor, kind;
+    float weight_decay;
 };
 struct AdamwTable {
-    nnconv_adamw_tensor *tensors;
+    uint32_t *arrived;  // workgroups of the running call that are done
     AdamwChunk *chunks;
 };
-AdamwTable adamw_table(void *buffer, int32_t tensors);
+AdamwTable adamw_table(void *buffer);
 hipError_t launch_adamw_plan(const nnconv_adamw_tensor *tensors, int32_t n, const AdamwTable &tab,
                              hipStream_t st);
 hipError_t launch_adamw(const AdamwTable &tab, int64_t chunks, int32_t *step, float lr, float beta1,
