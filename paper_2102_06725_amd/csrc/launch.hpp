@@ -473,7 +473,8 @@ hipError_t launch_recurrence_bwd(int dtype, const RecParams &p, hipStream_t st);
 
 // AdamW over a list of tensors, cut into chunks of ADAMW_CHUNK elements.
 constexpr int64_t ADAMW_CHUNK = 2048;
-constexpr size_t ADAMW_HEAD = 64;  // bytes in front of the chunks
+constexpr int ADAMW_LINE = 32;       // words from a counter to the next: a cache line
+constexpr size_t ADAMW_HEAD = 4096;  // bytes of counters in front of the chunks
 struct AdamwChunk {
     float *master;
     const void *grad;
@@ -484,7 +485,7 @@ struct AdamwChunk {
     float weight_decay;
 };
 struct AdamwTable {
-    uint32_t *arrived;  // workgroups of the running call that are done
+    uint32_t *arrived;  // counters of the running call's workgroups that are done
     AdamwChunk *chunks;
 };
 AdamwTable adamw_table(void *buffer);

@@ -470,6 +470,7 @@ class RMSNorm:
     def __init__(self, rows, c, dtype=NNCONV_F16, eps=1e-6, group=0):
         self.desc = nnconv_rmsnorm_desc(rows, c, dtype, group, eps)
         self._ws = _Workspaces()
+        self._nbytes = None
 
     @property
     def rows(self):
@@ -478,6 +479,7 @@ class RMSNorm:
     @rows.setter
     def rows(self, rows):
         self.desc.rows = rows
+        self._nbytes = None
 
     def fwd(self, x, gain, y, residual=None, sum=None, rstd=None, stream=None):
         check(nnconv_rmsnorm_fwd(self.desc, x.data_ptr(), _ptr(residual), gain.data_ptr(),
@@ -494,8 +496,10 @@ class RMSNorm:
         stream = Conv2d._stream(stream)
         ws, nb = None, 0
         if dgain is not None:
-            st, nb = nnconv_rmsnorm_workspace_size(self.desc)
-            check(st, "nnconv_rmsnorm_workspace_size")
+            if self._nbytes is None:
+                st, self._nbytes = nnconv_rmsnorm_workspace_size(self.desc)
+                check(st, "nnconv_rmsnorm_workspace_size")
+            nb = self._nbytes
             ws = self._ws.get("bwd", stream, nb, sum.device)
         check(nnconv_rmsnorm_bwd(self.desc, sum.data_ptr(), dy.data_ptr(), _ptr(dsum),
                                  gain.data_ptr(), rstd.data_ptr(), dx.data_ptr(), _ptr(dgain),
@@ -513,6 +517,7 @@ class GatedRecurrence:
         self.desc = nnconv_recurrence_desc(n, t, c, dtype, c if ld is None else ld,
                                            c if ldy is None else ldy)
         self._ws = _Workspaces()
+        self._sizes = {}  # pass -> workspace bytes of the present n and t
 
     @property
     def n(self):
@@ -521,6 +526,7 @@ class GatedRecurrence:
     @n.setter
     def n(self, n):
         self.desc.n = n
+        self._sizes.clear()
 
     @property
     def t(self):
@@ -529,6 +535,7 @@ class GatedRecurrence:
     @t.setter
     def t(self, t):
         self.desc.t = t
+        self._sizes.clear()
 
     def saved(self, device="cuda"):
         """A tensor for the states that fwd saves for bwd."""
@@ -538,8 +545,11 @@ class GatedRecurrence:
         return torch.empty(max(nb // 4, 1), dtype=torch.float32, device=device)
 
     def _workspace(self, pass_, stream, device):
-        st, nb = nnconv_recurrence_workspace_size(self.desc, pass_)
-        check(st, "nnconv_recurrence_workspace_size")
+        nb = self._sizes.get(pass_)
+        if nb is None:
+            st, nb = nnconv_recurrence_workspace_size(self.desc, pass_)
+            check(st, "nnconv_recurrence_workspace_size")
+            self._sizes[pass_] = nb
         return (None, 0) if nb == 0 else (self._ws.get(pass_, stream, nb, device).data_ptr(), nb)
 
     def fwd(self, x, f, bias, y, g=None, lengths=None, h0=None, ht=None, saved=None, stream=None):
