@@ -39,7 +39,10 @@ __device__ __forceinline__ void gate(float f, float bias, float &a, float &b) {
     float z = __builtin_fmaf(f, -LOG2E, bias);
     z = __builtin_elementwise_minimum(__builtin_elementwise_maximum(z, -Z_MAX), Z_MAX);
     const float e = __builtin_amdgcn_exp2f(z);
-    a = __builtin_amdgcn_rcpf(1.0f + e);
+    // one Newton step on the reciprocal, whose own error of up to a unit has a sign: a
+    // product of a thousand gates near 1 would add it up
+    const float d = 1.0f + e, r = __builtin_amdgcn_rcpf(d);
+    a = __builtin_fmaf(r, __builtin_fmaf(-d, r, 1.0f), r);
     b = e * a;
 }
 
@@ -134,7 +137,8 @@ struct RecGrid {
     uint64_t *words;   // [n][chunks][c], null for a single chunk
     uint64_t *states;  // [n][groups][c]
 };
-constexpr int GROUP = 16;  // places of a group at most
+constexpr int GROUP = 32;  // places of a group at most
+constexpr int ROUND = 16;  // rows of words that a workgroup has on their way at once
 constexpr uint64_t EMPTY = ~0ull;
 constexpr int POLLS = 4096;
 
@@ -217,21 +221,23 @@ __device__ __forceinline__ void carry_in(const RecGrid &q, int n, int32_t c, int
     const bool last = i + 1 == group;
     uint64_t *words = q.words + (int64_t)n * q.chunks * c, *states = q.states + (int64_t)n * q.groups * c;
     if (w == own && !last && k + 1 < q.chunks) put(words + (int64_t)k * c, L, ca, ch);
-    constexpr int R = (GROUP + W - 1) / W;
-    Words v[R];
+    constexpr int R = ROUND / W;
+    for (int j0 = w; j0 < i; j0 += ROUND) {
+        Words v[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-        if (w + r * W < i) v[r].load(words + (int64_t)(g * group + w + r * W) * c, L);
+        for (int r = 0; r < R; ++r)
+            if (j0 + r * W < i) v[r].load(words + (int64_t)(g * group + j0 + r * W) * c, L);
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int j = w + r * W;
-        if (j >= i) break;
-        float a[2], h[2];
-        if (v[r].wait(words + (int64_t)(g * group + j) * c, L))
-            v[r].unpack(a, h);
-        else
-            chunk_pair(g * group + j, a, h);
-        pairs[j][lane] = f32x4{a[0], h[0], a[1], h[1]};
+        for (int r = 0; r < R; ++r) {
+            const int j = j0 + r * W;
+            if (j >= i) break;
+            float a[2], h[2];
+            if (v[r].wait(words + (int64_t)(g * group + j) * c, L))
+                v[r].unpack(a, h);
+            else
+                chunk_pair(g * group + j, a, h);
+            pairs[j][lane] = f32x4{a[0], h[0], a[1], h[1]};
+        }
     }
     Words s;
     if (w == own) s.load(states + (int64_t)g * c, L);
