@@ -376,7 +376,7 @@ nnconv_status nnconv_sgd_update(int64_t count, float *master, float *momentum, v
  * the stored r, is the gradient of what was computed.  Rows are dense: [rows][c]. */
 typedef struct {
     int64_t rows;   /* >= 0: N*H*W of a channel-last activation, or tokens; 0 is a no-op */
-    int32_t c;      /* channels, >= 1 */
+    int32_t c;      /* channels, 1 to 2^28 */
     int32_t dtype;  /* F16 or BF16: x, residual, sum, y, dy, dsum, dx */
     int32_t group;  /* nnconv_rmsnorm_fwd_q8: channels with one scale, 32, 64 or 128;
                        0: one scale per row.  Others ignore it. */
@@ -384,7 +384,8 @@ typedef struct {
 } nnconv_rmsnorm_desc;
 
 /* Forward: y and, where the pointers are not NULL, sum (= r) and rstd
- * (fp32, [rows], for the backward pass).  residual: NULL or [rows][c].
+ * (fp32, [rows], for the backward pass).  A row whose mean square passes fp32's
+ * range has rstd 0.  residual: NULL or [rows][c].
  * gain: fp32, [c].  sum may be x or residual itself (updated in place);
  * nothing else may overlap an output.  A row of zeros with eps = 0 gives NaN,
  * as the formula does.  Any alignment of at least one element; 16-byte aligned
@@ -436,7 +437,7 @@ nnconv_status nnconv_rmsnorm_bwd(const nnconv_rmsnorm_desc *desc, const void *su
 typedef struct {
     int32_t n;      /* sequences, >= 0 */
     int32_t t;      /* tokens of each, >= 0 */
-    int32_t c;      /* channels, >= 1 */
+    int32_t c;      /* channels, 1 to 2^28 */
     int32_t dtype;  /* F16 or BF16: x, f, g, y and their gradients */
     int64_t ld;     /* elements from a token to the next in x, f, g, dx, df, dg, >= c:
                        3 * c where they are thirds of one projection's output */
@@ -464,7 +465,8 @@ nnconv_status nnconv_recurrence_workspace_size(const nnconv_recurrence_desc *des
  * may overlap anything.  ws: 8-byte aligned; calls that may overlap in time
  * need workspaces of their own.
  * INVALID_ARG: sizes below the limits above, bad dtype, null x, f or y;
- * UNSUPPORTED: dtype F32; WORKSPACE; MISALIGNED: pointers below their element
+ * UNSUPPORTED: dtype F32, more channels, a sequence of more than 2^36 elements or
+ * 2^29 tokens; WORKSPACE; MISALIGNED: pointers below their element
  * size (ws: below 8). */
 nnconv_status nnconv_recurrence_fwd(const nnconv_recurrence_desc *desc, const void *x,
                                     const void *f, const float *bias, const void *g,

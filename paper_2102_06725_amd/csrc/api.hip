@@ -1946,6 +1946,7 @@ static nnconv_status norm_check(const nnconv_rmsnorm_desc *d) {
     if (!d || d->rows < 0 || d->c < 1) return NNCONV_ERR_INVALID_ARG;
     if (!(d->eps >= 0.0f) || !__builtin_isfinite(d->eps)) return NNCONV_ERR_INVALID_ARG;
     if (d->rows > MAX_ELEMS / d->c) return NNCONV_ERR_INVALID_ARG;
+    if (d->c > MOST_CHANNELS) return NNCONV_ERR_UNSUPPORTED;
     return half_dtype(d->dtype);
 }
 
@@ -2060,6 +2061,7 @@ static nnconv_status rec_check(const nnconv_recurrence_desc *d, RecParams *p) {
     p->c = d->c;
     p->ld = d->ld;
     p->ldy = d->ldy;
+    if (d->c > MOST_CHANNELS || !recurrence_fits(*p)) return NNCONV_ERR_UNSUPPORTED;
     return half_dtype(d->dtype);
 }
 
@@ -2183,7 +2185,7 @@ static nnconv_status adamw_check(const nnconv_adamw_tensor *t, int32_t n, int64_
             return NNCONV_ERR_MISALIGNED;
         *chunks += (e.count + ADAMW_CHUNK - 1) / ADAMW_CHUNK;
     }
-    return *chunks > 0x7FFFFFFF ? NNCONV_ERR_INVALID_ARG : NNCONV_OK;
+    return *chunks > 0x3FFFFFFF ? NNCONV_ERR_UNSUPPORTED : NNCONV_OK;
 }
 
 static size_t adamw_bytes(int64_t chunks) {

@@ -17,53 +17,66 @@ __global__ __launch_bounds__(64 * WAVES) void colsum_kernel(const float *__restr
                                                             float inv_scale, int accumulate,
                                                             int32_t *flag) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int i = blockIdx.x * 64 + lane;
-    const int64_t lo = per * blockIdx.y, hi = lo + per < parts ? lo + per : parts;
-    float s = 0.f;
-    if (i < c) {
-        int64_t k = lo + w;
-        const float *src = part + k * c + i;
-        const int64_t step = (int64_t)WAVES * c;
-        for (; k + 3 * WAVES < hi; k += 4 * WAVES, src += 4 * step) {
-            const float a = src[0], b = src[step], d = src[2 * step], e = src[3 * step];
-            s += a;
-            s += b;
-            s += d;
-            s += e;
-        }
-        for (; k < hi; k += WAVES, src += step) s += *src;
-    }
     __shared__ float all[WAVES][64];
-    all[w][lane] = s;
-    __syncthreads();
-    if (w != 0 || i >= c) return;
-    s = all[0][lane];
+    const int64_t lo = per * blockIdx.y, hi = lo + per < parts ? lo + per : parts;
+    for (int64_t c0 = (int64_t)blockIdx.x * 64; c0 < c; c0 += (int64_t)gridDim.x * 64) {
+        const int64_t i = c0 + lane;
+        float s = 0.f;
+        if (i < c) {
+            int64_t k = lo + w;
+            const float *src = part + k * c + i;
+            const int64_t step = (int64_t)WAVES * c;
+            for (; k + 3 * WAVES < hi; k += 4 * WAVES, src += 4 * step) {
+                const float a = src[0], b = src[step], d = src[2 * step], e = src[3 * step];
+                s += a;
+                s += b;
+                s += d;
+                s += e;
+            }
+            for (; k < hi; k += WAVES, src += step) s += *src;
+        }
+        __syncthreads();  // the last channels' sums have been read
+        all[w][lane] = s;
+        __syncthreads();
+        if (w != 0 || i >= c) continue;
+        s = all[0][lane];
 #pragma unroll
-    for (int k = 1; k < WAVES; ++k) s += all[k][lane];
-    if (!out) {
-        next[(int64_t)blockIdx.y * c + i] = s;
-        return;
+        for (int k = 1; k < WAVES; ++k) s += all[k][lane];
+        if (!out) {
+            next[(int64_t)blockIdx.y * c + i] = s;
+            continue;
+        }
+        s *= inv_scale;
+        if (accumulate) s = out[i] + s;
+        out[i] = s;
+        if (flag && !__builtin_isfinite(s)) *flag = 1;
     }
-    s *= inv_scale;
-    if (accumulate) s = out[i] + s;
-    out[i] = s;
-    if (flag && !__builtin_isfinite(s)) *flag = 1;
 }
 
-constexpr int64_t PER = 512;  // parts that one workgroup sums at most
+// Parts that one workgroup sums, more where that would take too many workgroups.
+constexpr int64_t PER = 512, MOST = 4096;
+
+int64_t per_group(int64_t parts) {
+    const int64_t per = (parts + MOST - 1) / MOST;
+    return per < PER ? PER : per;
+}
 
 }  // namespace
 
-int64_t colsum_extra(int64_t parts) { return parts > PER ? (parts + PER - 1) / PER : 0; }
+int64_t colsum_extra(int64_t parts) {
+    const int64_t per = per_group(parts);
+    return parts > PER ? (parts + per - 1) / per : 0;
+}
 
 hipError_t launch_colsum(const float *part, int64_t parts, int32_t c, float *extra, float *out,
                          float inv_scale, int accumulate, int32_t *flag, hipStream_t st) {
-    const uint32_t nb = (uint32_t)((c + 63) / 64);
+    const int64_t cols = ((int64_t)c + 63) / 64;
+    const uint32_t nb = (uint32_t)(cols < (1 << 18) ? cols : (1 << 18));
     const int64_t more = colsum_extra(parts);
-    if (more > 0xFFFF) return hipErrorInvalidValue;
     if (more > 0) {
         hipLaunchKernelGGL(colsum_kernel, dim3(nb, (uint32_t)more), dim3(64 * WAVES), 0, st, part,
-                           parts, PER, c, extra, (float *)nullptr, 1.0f, 0, (int32_t *)nullptr);
+                           parts, per_group(parts), c, extra, (float *)nullptr, 1.0f, 0,
+                           (int32_t *)nullptr);
         part = extra;
         parts = more;
     }

@@ -465,6 +465,7 @@ struct RecParams {
     float *dh0, *part;        // part: dbias partials, or null
     void *ws;
 };
+bool recurrence_fits(const RecParams &p);
 int64_t recurrence_bwd_parts(const RecParams &p);
 size_t recurrence_ws(const RecParams &p, bool backward);
 size_t recurrence_words_bytes(const RecParams &p, bool backward);
@@ -472,6 +473,9 @@ hipError_t launch_recurrence_fwd(int dtype, const RecParams &p, hipStream_t st);
 hipError_t launch_recurrence_bwd(int dtype, const RecParams &p, hipStream_t st);
 
 // AdamW over a list of tensors, cut into chunks of ADAMW_CHUNK elements.
+// Channels of the operators of this section at most, so that counts of them stay in 32 bits.
+constexpr int32_t MOST_CHANNELS = 1 << 28;
+
 constexpr int64_t ADAMW_CHUNK = 2048;
 constexpr int ADAMW_LINE = 32;       // words from a counter to the next: a cache line
 constexpr size_t ADAMW_HEAD = 4096;  // bytes of counters in front of the chunks

@@ -420,6 +420,11 @@ __global__ __launch_bounds__(64 * W, 4) void recurrence_fwd_kernel(const RecPara
         }
     A[0] = fmaxf(A[0], A_MIN);
     A[1] = fmaxf(A[1], A_MIN);
+    float h[2] = {0.f, 0.f};
+    if (!q.words && p.h0) {  // before the barrier: ht, which another wave writes, may lie on it
+        h[0] = p.h0[(int64_t)n * p.c + L.k0];
+        h[1] = p.h0[(int64_t)n * p.c + L.k1];
+    }
     __shared__ f32x4 part[W][64];
     part[w][lane] = f32x4{A[0], H[0], A[1], H[1]};
     __syncthreads();
@@ -438,16 +443,12 @@ __global__ __launch_bounds__(64 * W, 4) void recurrence_fwd_kernel(const RecPara
         const float ea[2] = {e[0], e[2]}, eh[2] = {e[1], e[3]};
         compose(pa, ph, ea, eh);
     }
-    float h[2] = {0.f, 0.f};
     if (q.words) {
         float ca[2] = {pa[0], pa[1]}, ch[2] = {ph[0], ph[1]};
         compose(ca, ch, A, H);
         carry_in<W>(q, n, p.c, chunk, L, w, W - 1, ca, ch, [&](int place, float *a2, float *h2) {
             walk_fwd<T, W, S>(p, n, L, place * (W * S), len, bias, a2, h2);
         }, h);
-    } else if (p.h0) {
-        h[0] = p.h0[(int64_t)n * p.c + L.k0];
-        h[1] = p.h0[(int64_t)n * p.c + L.k1];
     }
     h[0] = pa[0] * h[0] + ph[0];
     h[1] = pa[1] * h[1] + ph[1];
@@ -491,6 +492,13 @@ __global__ __launch_bounds__(64 * W, 4) void recurrence_fwd_kernel(const RecPara
 // With own_t = dy_t g_t sigma(g_t), the gradient of h_t is d_t = own_t + r_t, where r_t
 // flows in from the right: r_(t-1) = a_t d_t.  So r obeys the same kind
 // of recurrence from the last token on, with a_t and a_t own_t.
+
+// r in front of a token; not fused with the product that own is, so that every place that
+// computes it gets the same bits.
+__device__ __forceinline__ float before_token(float a, float own, float r) {
+#pragma clang fp contract(off)
+    return a * (own + r);
+}
 
 template <class T, bool G>
 struct Grad {
@@ -617,7 +625,7 @@ __device__ void walk_bwd(const RecParams &p, int64_t n, const Lane &L, int lo, i
             Grad<T, G> e;
             e.make(0u, load2(f + t * p.ld, L), G ? load2(g + t * p.ld, L) : 0u,
                    load2(dy + t * p.ldy, L), bias);
-            for (int k = 0; k < 2; ++k) r1[k] = e.a[k] * (e.own[k] + r1[k]);
+            for (int k = 0; k < 2; ++k) r1[k] = before_token(e.a[k], e.own[k], r1[k]);
         }
         a1[0] = fmaxf(a1[0], A_MIN);
         a1[1] = fmaxf(a1[1], A_MIN);
@@ -681,9 +689,14 @@ __global__ __launch_bounds__(64 * W, 2) void recurrence_bwd_kernel(const RecPara
 #pragma unroll
     for (int s = S - 1; s >= 0; --s)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) R[k] = e[s].a[k] * (e[s].own[k] + R[k]);
+        for (int k = 0; k < 2; ++k) R[k] = before_token(e[s].a[k], e[s].own[k], R[k]);
     A[0] = fmaxf(A[0], A_MIN);
     A[1] = fmaxf(A[1], A_MIN);
+    float r[2] = {0.f, 0.f};
+    if (!q.words && p.dht) {  // before the barrier: dh0, which another wave writes, may lie on it
+        r[0] = p.dht[(int64_t)n * p.c + L.k0];
+        r[1] = p.dht[(int64_t)n * p.c + L.k1];
+    }
     __shared__ f32x4 part[W][64];
     __shared__ float part_r[W][2][64];
     part[w][lane] = f32x4{A[0], H[0], A[1], H[1]};
@@ -702,16 +715,12 @@ __global__ __launch_bounds__(64 * W, 2) void recurrence_bwd_kernel(const RecPara
         const float ma[2] = {m[0], m[2]}, mr[2] = {part_r[v][0][lane], part_r[v][1][lane]};
         compose(pa, pr, ma, mr);
     }
-    float r[2] = {0.f, 0.f};
     if (q.words) {
         float ca[2] = {pa[0], pa[1]}, cr[2] = {pr[0], pr[1]};
         compose(ca, cr, A, R);
         carry_in<W>(q, n, p.c, place, L, w, 0, ca, cr, [&](int at2, float *a2, float *r2) {
             walk_bwd<T, G, W, S>(p, n, L, (q.chunks - 1 - at2) * (W * S), len, bias, a2, r2);
         }, r);
-    } else if (p.dht) {
-        r[0] = p.dht[(int64_t)n * p.c + L.k0];
-        r[1] = p.dht[(int64_t)n * p.c + L.k1];
     }
     r[0] = pa[0] * r[0] + pr[0];
     r[1] = pa[1] * r[1] + pr[1];
@@ -885,9 +894,33 @@ int64_t word_count(const RecParams &p, bool backward) {
     return q.chunks > 1 ? (int64_t)p.n * ((int64_t)q.chunks + q.groups) * p.c : 0;
 }
 
+// Workgroups of one launch at most: work items of a launch are counted in 32 bits.
+constexpr int64_t MOST_BLOCKS = 1 << 22;
+
+// The sequences from n0 on, n of them.
+RecParams some(const RecParams &p, bool backward, int64_t n0, int64_t n) {
+    RecParams s = p;
+    const int64_t in = n0 * p.t * p.ld * 2, out = n0 * p.t * p.ldy * 2, state = n0 * p.c;
+    const int64_t stretches = (p.t + SAVE - 1) / SAVE;
+    auto move = [](auto &q, int64_t bytes) {
+        if (q) q = (std::remove_reference_t<decltype(q)>)((uintptr_t)q + bytes);
+    };
+    s.n = (int32_t)n;
+    for (const void **q : {&s.x, &s.f, &s.g}) move(*q, in);
+    for (void **q : {&s.dx, &s.df, &s.dg}) move(*q, in);
+    move(s.y, out);
+    move(s.dy, out);
+    move(s.lengths, n0 * 4);
+    for (const float **q : {&s.h0, &s.dht}) move(*q, state * 4);
+    for (float **q : {&s.ht, &s.dh0}) move(*q, state * 4);
+    move(s.saved, state * stretches * 4);
+    move(s.part, state * chunks_of(p, backward) * 4);
+    return s;
+}
+
 template <class T, bool G>
 hipError_t run(const RecParams &p, bool backward, hipStream_t st) {
-    const int cols = (p.c + COLS - 1) / COLS;
+    RecGrid q = grid_of(p, backward);
     if (p.c == 1) {
         const dim3 grid((p.n + 63) / 64);
         if (backward)
@@ -897,33 +930,43 @@ hipError_t run(const RecParams &p, bool backward, hipStream_t st) {
         return hipGetLastError();
     }
     if (p.t <= SHORT_T) {
-        const dim3 grid(cols, p.n < 65535 ? p.n : 65535);
+        const dim3 grid(q.cols, p.n < 65535 ? p.n : 65535);
         if (backward)
             hipLaunchKernelGGL((recurrence_bwd_short_kernel<T, G>), grid, dim3(64), 0, st, p);
         else
             hipLaunchKernelGGL((recurrence_fwd_short_kernel<T>), grid, dim3(64), 0, st, p);
         return hipGetLastError();
     }
-    RecGrid q = grid_of(p, backward);
-    const int64_t blocks = (int64_t)q.chunks * cols * p.n;
-    if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
-    if (q.chunks > 1) {
-        q.words = (uint64_t *)p.ws;
-        q.states = q.words + (int64_t)p.n * q.chunks * p.c;
-        const int64_t nb = (word_count(p, backward) + 255) / 256;
-        hipLaunchKernelGGL(recurrence_words_kernel, dim3((uint32_t)(nb < 2048 ? nb : 2048)), dim3(256), 0, st, q,
-                           (int64_t)p.n, p.c, backward ? p.dht : p.h0);
+    const int64_t each = (int64_t)q.chunks * q.cols, most = each < MOST_BLOCKS ? MOST_BLOCKS / each : 1;
+    for (int64_t n0 = 0; n0 < p.n; n0 += most) {
+        const RecParams s = some(p, backward, n0, p.n - n0 < most ? p.n - n0 : most);
+        if (q.chunks > 1) {  // launches follow each other: they share the words
+            q.words = (uint64_t *)p.ws;
+            q.states = q.words + (int64_t)s.n * q.chunks * p.c;
+            const int64_t nb = (word_count(s, backward) + 255) / 256;
+            hipLaunchKernelGGL(recurrence_words_kernel, dim3((uint32_t)(nb < 2048 ? nb : 2048)), dim3(256), 0, st, q,
+                               (int64_t)s.n, p.c, backward ? s.dht : s.h0);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        const dim3 grid((uint32_t)(each * s.n));
+        if (backward)
+            hipLaunchKernelGGL((recurrence_bwd_kernel<T, G, BW, BS>), grid, dim3(64 * BW), 0, st, s, q);
+        else
+            hipLaunchKernelGGL((recurrence_fwd_kernel<T, G, FW, FS>), grid, dim3(64 * FW), 0, st, s, q);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (backward)
-        hipLaunchKernelGGL((recurrence_bwd_kernel<T, G, BW, BS>), dim3((uint32_t)blocks), dim3(64 * BW), 0, st, p, q);
-    else
-        hipLaunchKernelGGL((recurrence_fwd_kernel<T, G, FW, FS>), dim3((uint32_t)blocks), dim3(64 * FW), 0, st, p, q);
-    return hipGetLastError();
+    return hipSuccess;
 }
 
 }  // namespace
+
+// One sequence's workgroups have to fit a launch.
+bool recurrence_fits(const RecParams &p) {
+    const RecGrid f = grid_of(p, false), b = grid_of(p, true);
+    return (int64_t)f.chunks * f.cols <= MOST_BLOCKS && (int64_t)b.chunks * b.cols <= 2 * MOST_BLOCKS;
+}
 
 int64_t recurrence_bwd_parts(const RecParams &p) { return p.n * chunks_of(p, true); }
 

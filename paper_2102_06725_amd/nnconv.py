@@ -578,7 +578,7 @@ class AdamW:
     torch.float8_e4m3fn (m) and torch.float8_e5m2 (v), or uint8, with a byte of scale for every
     NNCONV_ADAMW_BLOCK elements.  The tensors are kept: the list holds their addresses."""
 
-    def __init__(self, tensors, seed=0, stream=None):
+    def __init__(self, tensors, seed=0):
         import torch
         codes = {torch.float32: NNCONV_F32, torch.float16: NNCONV_F16, torch.bfloat16: NNCONV_BF16}
         self.tensors, self.seed = list(tensors), seed
@@ -608,7 +608,8 @@ class AdamW:
         self._table = torch.empty(max(nb, 1), dtype=torch.uint8, device=device)
         self.plan = nnconv_adamw_plan()
         check(nnconv_adamw_plan_init(arr, n, self._table.data_ptr(), nb, self.plan,
-                                     Conv2d._stream(stream)), "nnconv_adamw_plan_init")
+                                     current_stream()), "nnconv_adamw_plan_init")
+        torch.cuda.current_stream().synchronize()  # the plan is there for steps on any stream
 
     def step(self, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, state=None, overflow_flag=None,
              stream=None):

@@ -323,3 +323,33 @@ def test_two_streams_at_once(nnlib):
     t.cuda.synchronize()
     for (_, _, y, _), want in zip(sets, alone):
         assert bool((y.view(t.int16) == want.view(t.int16)).all())
+
+
+def test_more_sequences_than_a_launch_takes(nnlib):
+    """2^22 workgroups and some: the same bits as calls on a few of the sequences."""
+    t = U.torch()
+    n, tt, c = (1 << 22) + 5, 17, 2
+    g = t.Generator(device="cuda").manual_seed(2)
+    mk = lambda *s: t.randn(s, generator=g, device="cuda")  # noqa: E731
+    x, f, dy = (mk(n, tt, c).half() for _ in range(3))
+    bias, h0, dht = mk(c), mk(n, c), mk(n, c)
+
+    def both(lo, hi):
+        op = nc.GatedRecurrence(hi - lo, tt, c, dtype=nc.NNCONV_F16)
+        a = [v[lo:hi] for v in (x, f, dy, h0, dht)]
+        y, ht, saved = t.empty_like(a[0]), t.empty_like(a[3]), op.saved()
+        dx, df, dh0, dbias = t.empty_like(a[0]), t.empty_like(a[0]), t.empty_like(a[3]), t.empty(c, device="cuda")
+        op.fwd(a[0], a[1], bias, y, h0=a[3], ht=ht, saved=saved)
+        op.bwd(a[0], a[1], bias, saved, a[2], dx, df, dht=a[4], dh0=dh0, dbias=dbias)
+        return [y, ht, saved.view(-1, c), dx, df, dh0], dbias
+    whole, dbias = both(0, n)
+    for lo, hi in ((0, 9), ((1 << 22) - 4, n), (n // 2, n // 2 + 100)):
+        part, _ = both(lo, hi)
+        for a, b in zip(whole, part):
+            assert bool((a[lo:hi].contiguous().view(t.uint8) == b.contiguous().view(t.uint8)).all())
+    # every workgroup's share of the bias gradient is counted once
+    want = t.zeros(c, dtype=t.float64, device="cuda")
+    for k in range(0, n, 1 << 20):
+        want += whole[4][k:k + (1 << 20)].double().sum((0, 1))
+    # df is rounded to 11 bits in the sum that is compared with: a random walk over 7e7 terms below 2
+    assert float((dbias.double() - want).abs().max()) <= 8 * (n * tt) ** 0.5 * 2.0 ** -11

@@ -148,3 +148,19 @@ def test_adamw_refusals(nnlib):
     assert step(b1=1.0) == step(b1=-0.1) == step(b2=1.0) == step(b2=nan) == INV
     assert step(plan=nc.nnconv_adamw_plan(None, 1, 1, 0)) == step(plan=nc.nnconv_adamw_plan(FAKE, -1, 1, 0)) == INV
     assert step(step=FAKE + 2) == step(state=FAKE + 2) == step(flag=FAKE + 1) == MIS
+
+
+def test_limits(nnlib):
+    """Sizes whose counts would leave 32 bits are refused; the largest ones below are not."""
+    def size(n, t, c):
+        return nc.nnconv_recurrence_workspace_size(rec(n=n, t=t, c=c, ld=c, ldy=c), nc.NNCONV_DGRAD)[0]
+    assert size(1, 1 << 29, 2) == size(2 ** 31 - 1, 17, 2) == size(1, 17, 1 << 28) == OK
+    assert size(1, (1 << 29) + 200, 2) == size(1, 2 ** 31 - 1, 2) == size(1, 17, (1 << 28) + 1) == UNS
+    assert nc.nnconv_rmsnorm_workspace_size(norm(rows=1, c=1 << 28))[0] == OK
+    assert nc.nnconv_rmsnorm_workspace_size(norm(rows=1, c=(1 << 28) + 1))[0] == UNS
+    assert nc.nnconv_adamw_plan_size(tensor(count=1 << 40), 1)[0] == OK
+    assert nc.nnconv_adamw_plan_size(tensor(count=(1 << 40) + 1), 1)[0] == INV
+    # partial sums of the bias gradient stay a small part of the work
+    d = rec(n=1, t=1 << 20, c=64, ld=64, ldy=64)
+    st, need = nc.nnconv_recurrence_workspace_size(d, nc.NNCONV_DGRAD)
+    assert need <= (1 << 20) * 64 // 2
