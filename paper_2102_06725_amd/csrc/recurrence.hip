@@ -63,11 +63,13 @@ struct Lane {
     int k0, k1;        // channels of per-channel fp32 arrays and words, in range
     uint32_t shift;    // 16: the first channel is the second half of the load
     bool first, second;  // channels that exist
+    bool odd;            // c is odd
 
     __device__ __forceinline__ Lane(int c0, int c) {
         at = c0 < c - 2 ? c0 : c - 2;
         first = c0 < c;
         second = c0 + 1 < c;
+        odd = c & 1;
         shift = c0 == c - 1 ? 16 : 0;
         k0 = first ? c0 : c - 1;
         k1 = second ? c0 + 1 : c - 1;
@@ -107,19 +109,24 @@ __device__ __forceinline__ uint32_t load2(const void *row, const Lane &L) {
     return *(const global_u32_any *)(uniform(row) + (uint32_t)(2 * L.at)) >> L.shift;
 }
 
-// Stores of a wave whose 128 channels all exist, and of any.
-template <class T>
-__device__ __forceinline__ void store2_full(void *row, const Lane &L, float v0, float v1) {
-    __builtin_nontemporal_store(pack16<T>(v0, v1), (global_u32_any *)(uniform(row) + (uint32_t)(2 * L.at)));
-}
-
-template <class T>
-__device__ __forceinline__ void store2(void *row, const Lane &L, float v0, float v1) {
-    global_char *q = uniform(row) + (uint32_t)(2 * L.at);
-    if (L.second)
-        *(global_u32_any *)q = pack16<T>(v0, v1);
-    else if (L.first)
-        ((global_u16 *)q)[L.shift >> 4] = (uint16_t)to16<T>(v0);
+// N tensors' two channels of a token, in one masked region.  full (the same for the wave): all its
+// 128 channels exist.
+template <class T, int N>
+__device__ __forceinline__ void store2(void *const row[N], const Lane &L, bool full, const float v[N][2]) {
+    uint32_t q[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) q[k] = pack16<T>(v[k][0], v[k][1]);
+    auto all = [&]() {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            __builtin_nontemporal_store(q[k], (global_u32_any *)(uniform(row[k]) + (uint32_t)(2 * L.at)));
+    };
+    if (full) return all();
+    if (L.second) all();
+    if (L.odd && L.shift)  // the last channel of an odd count: alone in its lane
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            ((global_u16 *)(uniform(row[k]) + (uint32_t)(2 * L.at)))[1] = (uint16_t)q[k];
 }
 
 // ---- words between chunks ------------------------------------------------------
@@ -326,7 +333,8 @@ __global__ __launch_bounds__(64) void recurrence_fwd_short_kernel(const RecParam
                     o[k] = g ? h[k] * (gv[k] * sigma(gv[k])) : h[k];
                 }
             }
-            store2<T>(y + t * p.ldy, L, o[0], o[1]);
+            void *const row[1] = {y + t * p.ldy};
+            store2<T, 1>(row, L, false, &o);
         }
         if (p.ht) {
             if (L.first) p.ht[n * p.c + L.k0] = h[0];
@@ -471,10 +479,8 @@ __global__ __launch_bounds__(64 * W, 4) void recurrence_fwd_kernel(const RecPara
                 o[k] = G ? h[k] * (gv[k] * sigma(gv[k])) : h[k];
                 if (checked && t >= len) o[k] = 0.f;
             }
-            if (!checked)
-                store2_full<T>(y, L, o[0], o[1]);
-            else if (t < p.t)
-                store2<T>(y, L, o[0], o[1]);
+            void *const row[1] = {y};
+            if (!checked || t < p.t) store2<T, 1>(row, L, !checked, &o);
         }
     };
     if (whole && full)
@@ -571,7 +577,7 @@ __global__ __launch_bounds__(64) void recurrence_bwd_short_kernel(const RecParam
             }
         }
         for (int t = p.t - 1; t >= 0; --t) {
-            float vx[2] = {0.f, 0.f}, vf[2] = {0.f, 0.f}, vg[2] = {0.f, 0.f};
+            float out[3][2] = {{0.f, 0.f}, {0.f, 0.f}, {0.f, 0.f}};  // dx, df, dg
             if (t < len) {
                 Grad<T, G> e;
                 e.make(load2(x + t * p.ld, L), load2(f + t * p.ld, L),
@@ -579,16 +585,15 @@ __global__ __launch_bounds__(64) void recurrence_bwd_short_kernel(const RecParam
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const float before = hs[t][k][lane], d = e.own[k] + r[k];
-                    vx[k] = d * e.b[k];
-                    vf[k] = d * (before - e.x[k]) * (e.a[k] * e.b[k]);
-                    if (G) vg[k] = e.dg[k] * (e.a[k] * before + e.b[k] * e.x[k]);
+                    out[0][k] = d * e.b[k];
+                    out[1][k] = d * (before - e.x[k]) * (e.a[k] * e.b[k]);
+                    if (G) out[2][k] = e.dg[k] * (e.a[k] * before + e.b[k] * e.x[k]);
                     r[k] = e.a[k] * d;
-                    total[k] += vf[k];
+                    total[k] += out[1][k];
                 }
             }
-            store2<T>(dx + t * p.ld, L, vx[0], vx[1]);
-            store2<T>(df + t * p.ld, L, vf[0], vf[1]);
-            if (G) store2<T>(dg + t * p.ld, L, vg[0], vg[1]);
+            void *const row[3] = {dx + t * p.ld, df + t * p.ld, dg + t * p.ld};
+            store2<T, G ? 3 : 2>(row, L, false, out);
         }
         if (p.dh0) {
             if (L.first) p.dh0[n * p.c + L.k0] = r[0];
@@ -740,27 +745,20 @@ __global__ __launch_bounds__(64 * W, 2) void recurrence_bwd_kernel(const RecPara
 #pragma unroll
         for (int s = S - 1; s >= 0; --s, o -= p.ld) {
             const int t = t0 + s;
-            float vx[2], vf[2], vg[2];
+            float out[3][2];  // dx, df, dg
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const Grad<T, G> &m = e[s];
                 const float d = m.own[k] + r[k];
-                vx[k] = d * m.b[k];
-                vf[k] = d * (before[s][k] - m.x[k]) * (m.a[k] * m.b[k]);
-                vg[k] = m.dg[k] * (m.a[k] * before[s][k] + m.b[k] * m.x[k]);
-                if (checked && t >= len) vx[k] = vf[k] = vg[k] = 0.f;
+                out[0][k] = d * m.b[k];
+                out[1][k] = d * (before[s][k] - m.x[k]) * (m.a[k] * m.b[k]);
+                out[2][k] = m.dg[k] * (m.a[k] * before[s][k] + m.b[k] * m.x[k]);
+                if (checked && t >= len) out[0][k] = out[1][k] = out[2][k] = 0.f;
                 r[k] = m.a[k] * d;
-                total[k] += vf[k];
+                total[k] += out[1][k];
             }
-            if (!checked) {
-                store2_full<T>(dx + o, L, vx[0], vx[1]);
-                store2_full<T>(df + o, L, vf[0], vf[1]);
-                if (G) store2_full<T>(dg + o, L, vg[0], vg[1]);
-            } else if (t < p.t) {
-                store2<T>(dx + o, L, vx[0], vx[1]);
-                store2<T>(df + o, L, vf[0], vf[1]);
-                if (G) store2<T>(dg + o, L, vg[0], vg[1]);
-            }
+            void *const row[3] = {dx + o, df + o, dg + o};
+            if (!checked || t < p.t) store2<T, G ? 3 : 2>(row, L, !checked, out);
         }
     };
     if (whole && full)
