@@ -130,8 +130,8 @@ __device__ __forceinline__ float scale_of(float most, float &inv) {
 // ---- forward -------------------------------------------------------------------------
 
 template <class T, int TPR, int V, bool TAIL, bool Q8>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rmsnorm_fwd_kernel(const NormParams p) {
-    constexpr int WG = TPR < 256 ? 256 : TPR, ROWS = WG / TPR;
+__global__ __launch_bounds__(TPR <= 64 ? 256 : TPR) void rmsnorm_fwd_kernel(const NormParams p) {
+    constexpr int WG = TPR <= 64 ? 256 : TPR, ROWS = WG / TPR;
     __shared__ float buf[2][TPR > 64 ? TPR / 64 : 1];
     const int t = threadIdx.x % TPR;
     float gain[V][8];
@@ -435,23 +435,30 @@ __global__ __launch_bounds__(256) void rmsnorm_dgain_any_kernel(const NormBwdPar
 
 // ---- which kernel ---------------------------------------------------------------------
 
-// Threads of a row and vectors of each: the fewest threads that leave a thread few
-// vectors.
+// Threads of a row and vectors of each.  One vector a thread wherever a workgroup is enough:
+// more threads have more loads on their way, and the waits of one row's reduction are
+// covered by other workgroups.  Against a wave a row with 4 vectors and 256 threads with 4 (us, forward with
+// a residual, 16 bits):
+//   2048 channels:  8 rows 4.3 -> 2.6,  8192 rows 27.7 -> 23.8,  32768 rows 100 -> 80
+//   8192 channels:  8 rows 4.6 -> 3.1,  8192 rows 102 -> 84,     32768 rows 410 -> 350
+// The backward pass keeps sums of dgain in registers and writes them once a
+// workgroup; from 2049 channels on it is the faster with two vectors (4096 channels, 32768 rows:
+// 175 us, 186 with one; 8192 channels: 352 and 369).
 struct Shape {
     int tpr, v;
 };
 
-Shape shape_of(int64_t c) {
+Shape shape_of(int64_t c, bool backward) {
     if (c < 8 || c > 16384) return {0, 0};
     if (c <= 64) return {8, 1};
     if (c <= 128) return {16, 1};
     if (c <= 256) return {32, 1};
     if (c <= 512) return {64, 1};
-    if (c <= 1024) return {64, 2};
-    if (c <= 2048) return {64, 4};
-    if (c <= 4096) return {256, 2};
-    if (c <= 8192) return {256, 4};
-    return {512, 4};
+    if (c <= 1024) return {128, 1};
+    if (c <= 2048) return {256, 1};
+    if (c <= 4096) return backward ? Shape{256, 2} : Shape{512, 1};
+    if (c <= 8192) return backward ? Shape{512, 2} : Shape{1024, 1};
+    return backward ? Shape{512, 4} : Shape{1024, 2};
 }
 
 template <class F>
@@ -462,12 +469,25 @@ void with_shape(Shape s, F f) {
     SHAPE(16, 1);
     SHAPE(32, 1);
     SHAPE(64, 1);
-    SHAPE(64, 2);
-    SHAPE(64, 4);
-    SHAPE(256, 2);
-    SHAPE(256, 4);
-    SHAPE(512, 4);
+    SHAPE(128, 1);
+    SHAPE(256, 1);
 #undef SHAPE
+}
+
+template <class F>
+void with_fwd_shape(Shape s, F f) {
+    if (s.tpr == 512) return f(std::integral_constant<int, 512>{}, std::integral_constant<int, 1>{});
+    if (s.tpr == 1024 && s.v == 1) return f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 1>{});
+    if (s.tpr == 1024) return f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
+    with_shape(s, f);
+}
+
+template <class F>
+void with_bwd_shape(Shape s, F f) {
+    if (s.tpr == 256 && s.v == 2) return f(std::integral_constant<int, 256>{}, std::integral_constant<int, 2>{});
+    if (s.tpr == 512 && s.v == 2) return f(std::integral_constant<int, 512>{}, std::integral_constant<int, 2>{});
+    if (s.tpr == 512) return f(std::integral_constant<int, 512>{}, std::integral_constant<int, 4>{});
+    with_shape(s, f);
 }
 
 template <class F>
@@ -483,19 +503,19 @@ uint32_t blocks_for(int64_t rows, int per, int64_t most) {
     return (uint32_t)(n < most ? n : most);
 }
 
-constexpr int64_t FWD_BLOCKS = 1 << 20, BWD_BLOCKS = 512, ANY_PARTS = 256;
+constexpr int64_t FWD_BLOCKS = 1 << 20, BWD_BLOCKS = 512, BWD_FEW = 128, ANY_PARTS = 256;
 
 template <class T>
 void fwd(const NormParams &p, bool q8, hipStream_t st) {
-    const Shape s = shape_of(p.c);
+    const Shape s = shape_of(p.c, false);
     with_bool(q8, [&](auto q) {
         if (s.tpr == 0) {
             hipLaunchKernelGGL((rmsnorm_fwd_any_kernel<T, decltype(q)::value>), dim3(blocks_for(p.rows, 1, FWD_BLOCKS)),
                                dim3(512), 0, st, p);
             return;
         }
-        with_shape(s, [&](auto tpr, auto v) {
-            constexpr int TPR = decltype(tpr)::value, WG = TPR < 256 ? 256 : TPR;
+        with_fwd_shape(s, [&](auto tpr, auto v) {
+            constexpr int TPR = decltype(tpr)::value, WG = TPR <= 64 ? 256 : TPR;
             with_bool(p.c % 8 != 0, [&](auto tail) {
                 hipLaunchKernelGGL((rmsnorm_fwd_kernel<T, TPR, decltype(v)::value, decltype(tail)::value, decltype(q)::value>),
                                    dim3(blocks_for(p.rows, WG / TPR, FWD_BLOCKS)), dim3(WG), 0, st, p);
@@ -506,14 +526,14 @@ void fwd(const NormParams &p, bool q8, hipStream_t st) {
 
 template <class T>
 void bwd(const NormBwdParams &p, hipStream_t st) {
-    const Shape s = shape_of(p.c);
+    const Shape s = shape_of(p.c, true);
     if (s.tpr == 0) {
         if (p.part)  // first: dx may lie on dy
             hipLaunchKernelGGL((rmsnorm_dgain_any_kernel<T>), dim3((p.c + 255) / 256, p.parts), dim3(256), 0, st, p);
         hipLaunchKernelGGL((rmsnorm_bwd_any_kernel<T>), dim3(blocks_for(p.rows, 1, FWD_BLOCKS)), dim3(512), 0, st, p);
         return;
     }
-    with_shape(s, [&](auto tpr, auto v) {
+    with_bwd_shape(s, [&](auto tpr, auto v) {
         constexpr int TPR = decltype(tpr)::value, WG = TPR < 512 ? 512 : TPR;
         with_bool(p.c % 8 != 0, [&](auto tail) {
             hipLaunchKernelGGL((rmsnorm_bwd_kernel<T, TPR, decltype(v)::value, decltype(tail)::value>), dim3(p.parts), dim3(WG),
@@ -526,9 +546,13 @@ void bwd(const NormBwdParams &p, hipStream_t st) {
 
 // Partial sums of dgain: one per workgroup of the backward pass.
 int32_t rmsnorm_bwd_parts(int64_t rows, int32_t c) {
-    const Shape s = shape_of(c);
+    const Shape s = shape_of(c, true);
     if (s.tpr == 0) return (int32_t)(rows < ANY_PARTS ? rows : ANY_PARTS);
-    return (int32_t)blocks_for(rows, s.tpr < 512 ? 512 / s.tpr : 1, BWD_BLOCKS);
+    // at least two rows a team, so that the partial sums stay small beside the rows, unless that leaves
+    // few workgroups
+    const int64_t each = blocks_for(rows, s.tpr < 512 ? 512 / s.tpr : 1, INT32_MAX), half = each / 2;
+    const int64_t few = each < BWD_FEW ? each : BWD_FEW;
+    return (int32_t)(half < few ? few : half < BWD_BLOCKS ? half : BWD_BLOCKS);
 }
 
 hipError_t launch_rmsnorm_fwd(int dtype, const NormParams &p, bool q8, hipStream_t st) {

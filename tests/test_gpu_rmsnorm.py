@@ -33,6 +33,9 @@ CASES = [  # rows, c, dtype, residual, where the sum goes, elements past 16-byte
     (5, 4100, "bf16", True, "own", 5), (2, 8192, "f16", True, "own", 0), (3, 8200, "bf16", True, "own", 0),
     (2, 16384, "bf16", True, "own", 0), (2, 16392, "f16", True, "own", 0), (1, 40001, "f16", True, "own", 0),
     (5000, 96, "f16", True, "own", 0), (1, 2048, "f16", True, "own", 0),
+    # every team of threads with a last vector that is shared, in place, and enough rows for several a team
+    (700, 771, "bf16", True, "residual", 0), (600, 1025, "f16", True, "x", 0), (300, 3001, "f16", True, "own", 1),
+    (140, 7777, "bf16", True, "residual", 0), (140, 9001, "f16", True, "x", 0),
 ]
 
 
