@@ -9,7 +9,7 @@ namespace {
 constexpr int WAVES = 16;
 
 // 64 channels per workgroup; wave w adds parts w, w + 16, ... in increasing
-// order, four loads in flight, and wave 0 the 16 waves' sums.  With out a
+// order, eight loads in flight, and wave 0 the 16 waves' sums.  With out a
 // null pointer the sums of this workgroup's share of the parts go to next.
 __global__ __launch_bounds__(64 * WAVES) void colsum_kernel(const float *__restrict__ part,
                                                             int64_t parts, int64_t per, int32_t c,
@@ -26,12 +26,12 @@ __global__ __launch_bounds__(64 * WAVES) void colsum_kernel(const float *__restr
             int64_t k = lo + w;
             const float *src = part + k * c + i;
             const int64_t step = (int64_t)WAVES * c;
-            for (; k + 3 * WAVES < hi; k += 4 * WAVES, src += 4 * step) {
-                const float a = src[0], b = src[step], d = src[2 * step], e = src[3 * step];
-                s += a;
-                s += b;
-                s += d;
-                s += e;
+            for (; k + 7 * WAVES < hi; k += 8 * WAVES, src += 8 * step) {
+                float v[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) v[u] = src[u * step];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) s += v[u];
             }
             for (; k < hi; k += WAVES, src += step) s += *src;
         }

@@ -469,6 +469,7 @@ class RMSNorm:
 
     def __init__(self, rows, c, dtype=NNCONV_F16, eps=1e-6, group=0):
         self.desc = nnconv_rmsnorm_desc(rows, c, dtype, group, eps)
+        self._lib, self._ref = load(), ctypes.byref(self.desc)
         self._ws = _Workspaces()
         self._nbytes = None
 
@@ -482,18 +483,19 @@ class RMSNorm:
         self._nbytes = None
 
     def fwd(self, x, gain, y, residual=None, sum=None, rstd=None, stream=None):
-        check(nnconv_rmsnorm_fwd(self.desc, x.data_ptr(), _ptr(residual), gain.data_ptr(),
-                                 _ptr(sum), y.data_ptr(), _ptr(rstd),
-                                 Conv2d._stream(stream)), "nnconv_rmsnorm_fwd")
+        check(self._lib.nnconv_rmsnorm_fwd(
+            self._ref, x.data_ptr(), _ptr(residual), gain.data_ptr(), _ptr(sum), y.data_ptr(),
+            _ptr(rstd), current_stream() if stream is None else stream), "nnconv_rmsnorm_fwd")
 
     def fwd_q8(self, x, gain, q, scales, residual=None, sum=None, rstd=None, stream=None):
-        check(nnconv_rmsnorm_fwd_q8(self.desc, x.data_ptr(), _ptr(residual), gain.data_ptr(),
-                                    _ptr(sum), q.data_ptr(), scales.data_ptr(), _ptr(rstd),
-                                    Conv2d._stream(stream)), "nnconv_rmsnorm_fwd_q8")
+        check(self._lib.nnconv_rmsnorm_fwd_q8(
+            self._ref, x.data_ptr(), _ptr(residual), gain.data_ptr(), _ptr(sum), q.data_ptr(),
+            scales.data_ptr(), _ptr(rstd), current_stream() if stream is None else stream),
+            "nnconv_rmsnorm_fwd_q8")
 
     def bwd(self, sum, dy, gain, rstd, dx, dgain=None, dsum=None, inv_loss_scale=1.0,
             accumulate=0, overflow_flag=None, stream=None):
-        stream = Conv2d._stream(stream)
+        stream = current_stream() if stream is None else stream
         ws, nb = None, 0
         if dgain is not None:
             if self._nbytes is None:
@@ -501,10 +503,10 @@ class RMSNorm:
                 check(st, "nnconv_rmsnorm_workspace_size")
             nb = self._nbytes
             ws = self._ws.get("bwd", stream, nb, sum.device)
-        check(nnconv_rmsnorm_bwd(self.desc, sum.data_ptr(), dy.data_ptr(), _ptr(dsum),
-                                 gain.data_ptr(), rstd.data_ptr(), dx.data_ptr(), _ptr(dgain),
-                                 inv_loss_scale, accumulate, _ptr(overflow_flag), _ptr(ws), nb,
-                                 stream), "nnconv_rmsnorm_bwd")
+        check(self._lib.nnconv_rmsnorm_bwd(
+            self._ref, sum.data_ptr(), dy.data_ptr(), _ptr(dsum), gain.data_ptr(), rstd.data_ptr(),
+            dx.data_ptr(), _ptr(dgain), inv_loss_scale, accumulate, _ptr(overflow_flag), _ptr(ws),
+            nb, stream), "nnconv_rmsnorm_bwd")
 
 
 class GatedRecurrence:
@@ -516,6 +518,7 @@ class GatedRecurrence:
     def __init__(self, n, t, c, ld=None, ldy=None, dtype=NNCONV_F16):
         self.desc = nnconv_recurrence_desc(n, t, c, dtype, c if ld is None else ld,
                                            c if ldy is None else ldy)
+        self._lib, self._ref = load(), ctypes.byref(self.desc)
         self._ws = _Workspaces()
         self._sizes = {}  # pass -> workspace bytes of the present n and t
 
@@ -553,21 +556,21 @@ class GatedRecurrence:
         return (None, 0) if nb == 0 else (self._ws.get(pass_, stream, nb, device).data_ptr(), nb)
 
     def fwd(self, x, f, bias, y, g=None, lengths=None, h0=None, ht=None, saved=None, stream=None):
-        stream = Conv2d._stream(stream)
+        stream = current_stream() if stream is None else stream
         ws, nb = self._workspace(NNCONV_FWD, stream, x.device)
-        check(nnconv_recurrence_fwd(self.desc, x.data_ptr(), f.data_ptr(), _ptr(bias), _ptr(g),
-                                    _ptr(lengths), _ptr(h0), y.data_ptr(), _ptr(ht), _ptr(saved),
-                                    ws, nb, stream), "nnconv_recurrence_fwd")
+        check(self._lib.nnconv_recurrence_fwd(
+            self._ref, x.data_ptr(), f.data_ptr(), _ptr(bias), _ptr(g), _ptr(lengths), _ptr(h0),
+            y.data_ptr(), _ptr(ht), _ptr(saved), ws, nb, stream), "nnconv_recurrence_fwd")
 
     def bwd(self, x, f, bias, saved, dy, dx, df, g=None, dg=None, lengths=None, dht=None, dh0=None,
             dbias=None, inv_loss_scale=1.0, accumulate=0, overflow_flag=None, stream=None):
-        stream = Conv2d._stream(stream)
+        stream = current_stream() if stream is None else stream
         ws, nb = self._workspace(NNCONV_DGRAD, stream, x.device)
-        check(nnconv_recurrence_bwd(self.desc, x.data_ptr(), f.data_ptr(), _ptr(bias), _ptr(g),
-                                    _ptr(lengths), saved.data_ptr(), dy.data_ptr(), _ptr(dht),
-                                    dx.data_ptr(), df.data_ptr(), _ptr(dg), _ptr(dh0),
-                                    _ptr(dbias), inv_loss_scale, accumulate, _ptr(overflow_flag),
-                                    ws, nb, stream), "nnconv_recurrence_bwd")
+        check(self._lib.nnconv_recurrence_bwd(
+            self._ref, x.data_ptr(), f.data_ptr(), _ptr(bias), _ptr(g), _ptr(lengths),
+            saved.data_ptr(), dy.data_ptr(), _ptr(dht), dx.data_ptr(), df.data_ptr(), _ptr(dg),
+            _ptr(dh0), _ptr(dbias), inv_loss_scale, accumulate, _ptr(overflow_flag), ws, nb,
+            stream), "nnconv_recurrence_bwd")
 
 
 class AdamW:
@@ -584,24 +587,30 @@ class AdamW:
         self.tensors, self.seed = list(tensors), seed
         n = len(self.tensors)
         arr = (nnconv_adamw_tensor * max(n, 1))()
+        fp32, scale = {torch.float32}, {torch.uint8, torch.float8_e8m0fnu}
+        m8, v8 = {torch.float8_e4m3fn, torch.uint8}, {torch.float8_e5m2, torch.uint8}
+
+        def address(key, v, size, types):
+            if v.numel() != size or not v.is_contiguous():
+                raise ValueError("AdamW: %s has another size than the master, or is not dense" % key)
+            if v.dtype not in types:
+                raise ValueError("AdamW: %s has type %s" % (key, v.dtype))
+            return v.data_ptr()
+
         for a, t in zip(arr, self.tensors):
-            every = {k: t.get(k) for k in ("master", "grad", "w16", "m", "v", "m_scale", "v_scale")}
-            count = every["master"].numel()
-            f8 = every["m_scale"] is not None
-            blocks = -(-count // NNCONV_ADAMW_BLOCK)
-            for k, v in every.items():
-                if v is None:
-                    continue
-                if not v.is_contiguous() or v.numel() != (blocks if k.endswith("_scale") else count):
-                    raise ValueError("AdamW: %s has another size than the master, or is not dense" % k)
-                if v.element_size() != (1 if f8 and k[0] in "mv" and k != "master" else
-                                        2 if k == "w16" else v.element_size() if k == "grad" else 4):
-                    raise ValueError("AdamW: %s has type %s" % (k, v.dtype))
-                setattr(a, k, v.data_ptr())
-            a.count, a.weight_decay = count, float(t.get("weight_decay", 0.0))
-            a.grad_dtype = codes.get(every["grad"].dtype, -1)
-            a.w16_dtype = NNCONV_F16 if every["w16"] is None else codes.get(every["w16"].dtype, -1)
-            a.state_dtype = NNCONV_F8 if f8 else NNCONV_F32
+            master, grad, w16 = t["master"], t["grad"], t.get("w16")
+            count = master.numel()
+            f8 = t.get("m_scale") is not None
+            a.master = address("master", master, count, fp32)
+            a.grad = address("grad", grad, count, (grad.dtype,))
+            a.m, a.v = address("m", t["m"], count, m8 if f8 else fp32), address("v", t["v"], count, v8 if f8 else fp32)
+            if w16 is not None:
+                a.w16, a.w16_dtype = address("w16", w16, count, {torch.float16, torch.bfloat16}), codes[w16.dtype]
+            if f8:
+                blocks = -(-count // NNCONV_ADAMW_BLOCK)
+                a.m_scale, a.v_scale = (address(k, t[k], blocks, scale) for k in ("m_scale", "v_scale"))
+            a.count, a.weight_decay = count, t.get("weight_decay", 0.0)
+            a.grad_dtype, a.state_dtype = codes.get(grad.dtype, -1), NNCONV_F8 if f8 else NNCONV_F32
         st, nb = nnconv_adamw_plan_size(arr, n)
         check(st, "nnconv_adamw_plan_size")
         device = self.tensors[0]["master"].device if n else "cuda"
