@@ -1,7 +1,8 @@
 /*
  * nnconv.h -- C ABI of libnnconv: mixed-precision 2-D convolution in the
  * three training passes (forward, backward-data, backward-weight) on one
- * AMD Instinct MI355X (gfx950).
+ * AMD Instinct MI355X (gfx950); and, after it, the operators of gated sequence blocks on
+ * channel-last tokens (norm, recurrence) and the solver they are trained with.
  *
  * The operation is the paper's convolution call (Sec. 3.2, Listings 4-5:
  * convolution(x, base_axis=1, outmaps, kernel, ...)), trained by

@@ -3,9 +3,14 @@
 //
 // Bound by memory: 30 bytes a parameter with fp32 gradients, moments and a
 // 16-bit copy, 18 (and a 32nd) with 8-bit moments.  The list is cut into chunks, whose
-// records (addresses and all) lie in the plan; a fixed number of workgroups walks
-// them.  A lane takes 4 neighbouring elements at a time, in 16-byte accesses
-// at any alignment; 16 lanes hold a block of 8-bit moments.
+// records (addresses and all) lie in the plan; as many workgroups as fit the chip at once
+// (1280; 2048 took 7 % longer) walk them, each with the next record on its way.  A lane takes 4 neighbouring elements at a time, in 16-byte accesses
+// at any alignment; 16 lanes hold a block of 8-bit moments.  (8 neighbouring elements a lane
+// with 8-bit moments, half as many accesses, but each of half cache lines: 1479 us where 4 take 1160.)
+//
+// Measured: 23.5 M parameters in 159 tensors 126 us (5.6 TB/s); 302 M with 8-bit moments 1.16 ms
+// (4.7 TB/s; a copy of that size 4.83); without the hash and the rounding it would
+// take 1.15 ms.
 #include "launch.hpp"
 
 namespace nnconv {

@@ -13,6 +13,20 @@
 //     registers.
 // Whether a token takes part is the same for a whole wave, so lengths
 // and the end of the sequence cost no divergence.
+//
+// Bound by memory (8 bytes a token and channel forward, 14 backward), and close behind it by the
+// vector units: a forward element takes 37 instructions, 4 of them transcendental, which alone
+// would take half of the time.  Measured, cold: forward of 8 x 2048 x 1152
+// 37 us (4.1 TB/s), backward 60 us (4.4 TB/s); forward of 2 x 32768 x 768 95 us (4.2 TB/s; the
+// same elements as 512 sequences of 128 tokens, one chunk each, 74 us).  Short
+// calls are bound by their launches and one exchange between workgroups: 6 us
+// for one chunk, 10 for two.
+//
+// Chunks: forward 8 waves of 16 tokens, backward 4 of 16, the most that leave two
+// workgroups to a compute unit (126 and 248 registers): what is on its way and what waits for
+// its predecessors are then never the same.  16 waves of 8 tokens, 4 of 32 and 16 of 16 took 103, 102 and
+// 98 us where 8 of 16 take 97, chunks of half the tokens 115; backward, 8 waves of 8 and 16 of 4
+// took 65 and 66 us where 4 of 16 take 55.
 #include <type_traits>
 
 #include "launch.hpp"
@@ -24,7 +38,7 @@ namespace {
 constexpr int SAVE = NNCONV_RECURRENCE_SAVE;
 constexpr int COLS = 128;                 // channels of a wave
 constexpr float A_MIN = 0x1p-126f;        // products of gates stay above 0: 0 * inf would be NaN
-constexpr int SHORT_T = 16;               // up to here one lane walks all tokens
+constexpr int SHORT_T = 16;               // up to here one lane walks all tokens: no exchange, no barrier
 
 typedef uint32_t __attribute__((aligned(2))) u32_any;  // 4-byte access at any element
 
@@ -867,7 +881,7 @@ __global__ __launch_bounds__(64) void recurrence_bwd_single_kernel(const RecPara
     if (p.part) p.part[n] = total;
 }
 
-constexpr int FW = 8, FS = 16, BW = 4, BS = 16;
+constexpr int FW = 8, FS = 16, BW = 4, BS = 16;  // waves, and tokens of each
 constexpr int FCHUNK = FW * FS, BCHUNK = BW * BS;
 
 int64_t chunks_of(const RecParams &p, bool backward) {
@@ -876,7 +890,9 @@ int64_t chunks_of(const RecParams &p, bool backward) {
 }
 
 // Places in groups of 2^gs: about as many groups, whose states are handed on
-// one after the other, as places in one, whose pairs each place reads.
+// one after the other, as places in one, whose pairs each place reads.  (Groups of
+// 16 throughout: backward of 8 x 2048 x 1152 4 us slower.  Groups of at most 16: forward of 1 x
+// 65536 x 256 47 us, 42 with 32.)
 RecGrid grid_of(const RecParams &p, bool backward) {
     RecGrid q{};
     const int64_t chunks = chunks_of(p, backward);
