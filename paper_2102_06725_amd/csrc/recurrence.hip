@@ -70,23 +70,23 @@ __device__ __forceinline__ int length_of(const RecParams &p, int n) {
     return l < 0 ? 0 : l > p.t ? p.t : l;
 }
 
-// The two channels of a lane.  c >= 2: a lane at or past the last channel
-// loads the last two, and takes the second of them if it is alone there.
+// The two channels of a lane.  c >= 2: a lane whose second channel would be past the end (the
+// last one of an odd count) takes the last two, the first of which is its neighbour's, and writes the second
+// alone: the neighbour may be in another workgroup, and states may be updated in place.
+// Lanes past the end load the last two and write nothing.
 struct Lane {
-    uint32_t at;       // first channel loaded
-    int k0, k1;        // channels of per-channel fp32 arrays and words, in range
-    uint32_t shift;    // 16: the first channel is the second half of the load
-    bool first, second;  // channels that exist
-    bool odd;            // c is odd
+    uint32_t at;  // first channel
+    int k0, k1;   // the channels, for per-channel fp32 arrays and words
+    bool both, second;  // channels that it writes
+    bool odd;           // c is odd, the same for all lanes
 
     __device__ __forceinline__ Lane(int c0, int c) {
         at = c0 < c - 2 ? c0 : c - 2;
-        first = c0 < c;
-        second = c0 + 1 < c;
+        both = c0 + 1 < c;
+        second = c0 < c;
         odd = c & 1;
-        shift = c0 == c - 1 ? 16 : 0;
-        k0 = first ? c0 : c - 1;
-        k1 = second ? c0 + 1 : c - 1;
+        k0 = at;
+        k1 = at + 1;
     }
 };
 
@@ -120,7 +120,7 @@ typedef __attribute__((address_space(1))) uint16_t global_u16;
 
 // A lane's two channels of a token.
 __device__ __forceinline__ uint32_t load2(const void *row, const Lane &L) {
-    return *(const global_u32_any *)(uniform(row) + (uint32_t)(2 * L.at)) >> L.shift;
+    return *(const global_u32_any *)(uniform(row) + (uint32_t)(2 * L.at));
 }
 
 // N tensors' two channels of a token, in one masked region.  full (the same for the wave): all its
@@ -130,17 +130,21 @@ __device__ __forceinline__ void store2(void *const row[N], const Lane &L, bool f
     uint32_t q[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) q[k] = pack16<T>(v[k][0], v[k][1]);
-    auto all = [&]() {
+    if (full || L.both)
 #pragma unroll
         for (int k = 0; k < N; ++k)
             __builtin_nontemporal_store(q[k], (global_u32_any *)(uniform(row[k]) + (uint32_t)(2 * L.at)));
-    };
-    if (full) return all();
-    if (L.second) all();
-    if (L.odd && L.shift)  // the last channel of an odd count: alone in its lane
+    if (!full && L.odd)
+        if (L.second && !L.both)
 #pragma unroll
-        for (int k = 0; k < N; ++k)
-            ((global_u16 *)(uniform(row[k]) + (uint32_t)(2 * L.at)))[1] = (uint16_t)q[k];
+            for (int k = 0; k < N; ++k)
+                ((global_u16 *)(uniform(row[k]) + (uint32_t)(2 * L.at)))[1] = (uint16_t)(q[k] >> 16);
+}
+
+// Two fp32 values of a per-channel array.
+__device__ __forceinline__ void put2(float *to, const Lane &L, float v0, float v1) {
+    if (L.both) to[L.k0] = v0;
+    if (L.second) to[L.k1] = v1;
 }
 
 // ---- words between chunks ------------------------------------------------------
@@ -172,7 +176,7 @@ __device__ __forceinline__ float word_a(uint64_t v) { return __builtin_bit_cast(
 __device__ __forceinline__ float word_h(uint64_t v) { return __builtin_bit_cast(float, (uint32_t)(v >> 32)); }
 
 __device__ __forceinline__ void put(uint64_t *row, const Lane &L, const float a[2], const float h[2]) {
-    if (L.first) __hip_atomic_store(row + L.k0, word(a[0], h[0]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (L.both) __hip_atomic_store(row + L.k0, word(a[0], h[0]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (L.second) __hip_atomic_store(row + L.k1, word(a[1], h[1]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
@@ -329,8 +333,7 @@ __global__ __launch_bounds__(64) void recurrence_fwd_short_kernel(const RecParam
         const uint16_t *g = p.g ? (const uint16_t *)p.g + at : nullptr;
         uint16_t *y = (uint16_t *)p.y + n * p.t * p.ldy;
         if (p.saved && p.t > 0) {  // t <= SAVE: one state
-            if (L.first) p.saved[n * p.c + L.k0] = h[0];
-            if (L.second) p.saved[n * p.c + L.k1] = h[1];
+            put2(p.saved + n * p.c, L, h[0], h[1]);
         }
         for (int t = 0; t < p.t; ++t) {
             float o[2] = {0.f, 0.f};
@@ -350,10 +353,7 @@ __global__ __launch_bounds__(64) void recurrence_fwd_short_kernel(const RecParam
             void *const row[1] = {y + t * p.ldy};
             store2<T, 1>(row, L, false, &o);
         }
-        if (p.ht) {
-            if (L.first) p.ht[n * p.c + L.k0] = h[0];
-            if (L.second) p.ht[n * p.c + L.k1] = h[1];
-        }
+        if (p.ht) put2(p.ht + n * p.c, L, h[0], h[1]);
     }
 }
 
@@ -476,8 +476,7 @@ __global__ __launch_bounds__(64 * W, 4) void recurrence_fwd_kernel(const RecPara
     h[1] = pa[1] * h[1] + ph[1];
     if (p.saved && t0 % SAVE == 0 && t0 < p.t) {
         float *to = p.saved + ((int64_t)n * ((p.t + SAVE - 1) / SAVE) + t0 / SAVE) * p.c;
-        if (L.first) to[L.k0] = h[0];
-        if (L.second) to[L.k1] = h[1];
+        put2(to, L, h[0], h[1]);
     }
     uint16_t *y = (uint16_t *)p.y + (int64_t)n * p.t * p.ldy;
     y += (int64_t)t0 * p.ldy;
@@ -501,10 +500,7 @@ __global__ __launch_bounds__(64 * W, 4) void recurrence_fwd_kernel(const RecPara
         finish(std::false_type{});
     else
         finish(std::true_type{});
-    if (p.ht && chunk == q.chunks - 1 && w == W - 1) {
-        if (L.first) p.ht[(int64_t)n * p.c + L.k0] = h[0];
-        if (L.second) p.ht[(int64_t)n * p.c + L.k1] = h[1];
-    }
+    if (p.ht && chunk == q.chunks - 1 && w == W - 1) put2(p.ht + (int64_t)n * p.c, L, h[0], h[1]);
 }
 
 // ---- backward -------------------------------------------------------------------
@@ -609,14 +605,8 @@ __global__ __launch_bounds__(64) void recurrence_bwd_short_kernel(const RecParam
             void *const row[3] = {dx + t * p.ld, df + t * p.ld, dg + t * p.ld};
             store2<T, G ? 3 : 2>(row, L, false, out);
         }
-        if (p.dh0) {
-            if (L.first) p.dh0[n * p.c + L.k0] = r[0];
-            if (L.second) p.dh0[n * p.c + L.k1] = r[1];
-        }
-        if (p.part) {
-            if (L.first) p.part[n * p.c + L.k0] = total[0];
-            if (L.second) p.part[n * p.c + L.k1] = total[1];
-        }
+        if (p.dh0) put2(p.dh0 + n * p.c, L, r[0], r[1]);
+        if (p.part) put2(p.part + n * p.c, L, total[0], total[1]);
     }
 }
 
@@ -779,10 +769,7 @@ __global__ __launch_bounds__(64 * W, 2) void recurrence_bwd_kernel(const RecPara
         finish(std::false_type{});
     else
         finish(std::true_type{});
-    if (p.dh0 && chunk == 0 && w == 0) {
-        if (L.first) p.dh0[(int64_t)n * p.c + L.k0] = r[0];
-        if (L.second) p.dh0[(int64_t)n * p.c + L.k1] = r[1];
-    }
+    if (p.dh0 && chunk == 0 && w == 0) put2(p.dh0 + (int64_t)n * p.c, L, r[0], r[1]);
     if (p.part) {
         __syncthreads();
         part_r[w][0][lane] = total[0];
@@ -794,8 +781,7 @@ __global__ __launch_bounds__(64 * W, 2) void recurrence_bwd_kernel(const RecPara
             total[1] += part_r[v][1][lane];
         }
         float *to = p.part + ((int64_t)n * q.chunks + chunk) * p.c;
-        if (L.first) to[L.k0] = total[0];
-        if (L.second) to[L.k1] = total[1];
+        put2(to, L, total[0], total[1]);
     }
 }
 

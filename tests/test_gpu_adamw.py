@@ -287,3 +287,26 @@ def test_handle_refuses_tensors_that_do_not_fit(nnlib):
             nc.AdamW([dict(good, **bad)])
     with pytest.raises(nc.NNConvError):
         nc.AdamW([dict(good, grad=z(10, t.float64))])
+
+
+def test_offsets_past_32_bits(nnlib):
+    """A tensor of more than 2^32 elements: its last ones take the step that they take in a tensor of their own."""
+    t = U.torch()
+    n, last = (1 << 32) + 5000, 4096 + 904  # the tail starts at a chunk's edge
+    g = t.Generator(device="cuda").manual_seed(3)
+    grad, w = t.randn(last, generator=g, device="cuda").half(), t.randn(last, generator=g, device="cuda")
+    big = dict(master=t.zeros(n, device="cuda"), grad=t.zeros(n, dtype=t.float16, device="cuda"),
+               m=t.zeros(n, dtype=t.float8_e4m3fn, device="cuda"), v=t.zeros(n, dtype=t.float8_e5m2, device="cuda"),
+               m_scale=t.zeros(-(-n // 64), dtype=t.uint8, device="cuda"), v_scale=t.zeros(-(-n // 64), dtype=t.uint8, device="cuda"),
+               weight_decay=0.1)
+    big["master"][-last:] = w
+    big["grad"][-last:] = grad
+    small = dict(master=w.clone(), grad=grad, m=t.zeros(last, device="cuda"), v=t.zeros(last, device="cuda"), weight_decay=0.1)
+    step = t.zeros(1, dtype=t.int32, device="cuda")
+    nc.AdamW([big]).step(step, 1e-3)
+    nc.AdamW([small]).step(step.zero_(), 1e-3)
+    assert bool((big["master"][-last:] == small["master"]).all())  # the first step's moments are unrounded in it
+    assert not bool(big["master"][:-last].any())
+    scale = (big["v_scale"][-(-(n - last) // 64):].float() - 127).exp2().repeat_interleave(64)[:last]
+    v = big["v"].view(t.uint8)[-last:].view(t.float8_e5m2).float() * scale
+    assert bool(((v - small["v"]).abs() <= 0.25 * small["v"] + scale * 2.0 ** -16).all())

@@ -353,3 +353,45 @@ def test_more_sequences_than_a_launch_takes(nnlib):
         want += whole[4][k:k + (1 << 20)].double().sum((0, 1))
     # df is rounded to 11 bits in the sum that is compared with: a random walk over 7e7 terms below 2
     assert float((dbias.double() - want).abs().max()) <= 8 * (n * tt) ** 0.5 * 2.0 ** -11
+
+
+def test_offsets_past_32_bits(nnlib):
+    """Sequences that start 3 and more GB into the tensors: the bits of a call on the last one alone."""
+    t = U.torch()
+    n, tt, c = 3, 300001, 800  # 2.2e9 elements of the packed input, 0.7e9 of y
+    g = t.Generator(device="cuda").manual_seed(3)
+    proj = t.empty((n, tt, 3 * c), dtype=t.float16, device="cuda")
+    for i in range(n):
+        proj[i] = t.randn((tt, 3 * c), generator=g, device="cuda")
+    dy = t.randn((n, tt, c), generator=g, device="cuda").half()
+    bias, h0 = t.rand(c, generator=g, device="cuda") * 6, t.randn((n, c), generator=g, device="cuda")
+
+    def both(lo):
+        m = n - lo
+        p, d, h = proj[lo:], dy[lo:], h0[lo:].contiguous()
+        op = nc.GatedRecurrence(m, tt, c, ld=3 * c, dtype=nc.NNCONV_F16)
+        x, f, gate = (p[..., i * c:(i + 1) * c] for i in range(3))
+        y, dp, ht, saved = t.empty_like(d), t.empty_like(p), t.empty_like(h), op.saved()
+        dx, df, dg = (dp[..., i * c:(i + 1) * c] for i in range(3))
+        op.fwd(x, f, bias, y, g=gate, h0=h, ht=ht, saved=saved)
+        op.bwd(x, f, bias, saved, d, dx, df, g=gate, dg=dg)
+        return y[-1], ht[-1], dp[-1]
+    for a, b in zip(both(0), both(n - 1)):
+        assert bool((a.view(t.uint8) == b.view(t.uint8)).all())
+
+
+@pytest.mark.parametrize("t", [1, 16, 17, 64])
+@pytest.mark.parametrize("c", [129, 257, 131])
+def test_states_in_place_where_a_channel_is_alone(nnlib, t, c):
+    """An odd count's last channel, in a workgroup of its own too: many calls in place are one long sequence."""
+    calls = 40
+    whole = Case(8, t * calls, c, "f16", with_g=False, seed=2)
+    y, ht = whole.forward()
+    h = whole.h0
+    for k in range(calls):
+        part = Case(8, t, c, "f16", with_g=False)
+        part.x, part.f = whole.x[:, k * t:(k + 1) * t], whole.f[:, k * t:(k + 1) * t]
+        part.bias, part.h0 = whole.bias, h
+        yk, h = part.forward(in_place=True)
+        assert np.abs(yk - y[:, k * t:(k + 1) * t]).max() <= 2.0 ** -9 * max(1.0, np.abs(y).max())
+    U.close32(h, ht, ULP * (24 + 4 * t * calls) * max(np.abs(h).max(), np.abs(whole.x).max()))

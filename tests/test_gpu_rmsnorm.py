@@ -243,3 +243,27 @@ def test_other_stream_graph_and_repeats(nnlib):
         g.replay()
         t.cuda.synchronize()
         assert all(bool((a == b).all()) for a, b in zip(first, bits())), "replay %d" % k
+
+
+def test_offsets_past_32_bits(nnlib):
+    """Rows past 2^32 bytes and 2^31 elements: the bits of calls on the last rows alone."""
+    t = U.torch()
+    rows, c, last = 550001, 4104, 300  # 2.26e9 elements
+    g = t.Generator(device="cuda").manual_seed(3)
+    x = t.empty((rows, c), dtype=t.float16, device="cuda")
+    for k in range(0, rows, 50000):
+        x[k:k + 50000] = t.randn((min(50000, rows - k), c), generator=g, device="cuda")
+    gain = t.rand(c, generator=g, device="cuda")
+
+    def three(v):
+        n = v.shape[0]
+        op = nc.RMSNorm(n, c, dtype=nc.NNCONV_F16, group=64)
+        y, rstd = t.empty_like(v), t.empty(n, device="cuda")
+        op.fwd(v, gain, y, rstd=rstd)
+        q, scales = t.empty((n, c), dtype=t.uint8, device="cuda"), t.empty((n, -(-c // 64)), device="cuda")
+        op.fwd_q8(v, gain, q, scales)
+        dx = t.empty_like(v)
+        op.bwd(v, y, gain, rstd, dx, dsum=v)
+        return [k[-last:].clone() for k in (y, rstd, q, scales, dx)]
+    for a, b in zip(three(x), three(x[-last:].clone())):
+        assert bool((a.view(t.uint8) == b.view(t.uint8)).all())
