@@ -118,27 +118,31 @@ __device__ __forceinline__ global_char *uniform(const void *row) {
 typedef __attribute__((address_space(1))) u32_any global_u32_any;
 typedef __attribute__((address_space(1))) uint16_t global_u16;
 
-// A lane's two channels of a token.
+// A lane's two channels of a token.  U: the token is the same for the whole wave.
+template <bool U = true>
 __device__ __forceinline__ uint32_t load2(const void *row, const Lane &L) {
-    return *(const global_u32_any *)(uniform(row) + (uint32_t)(2 * L.at));
+    global_char *r = U ? uniform(row) : (global_char *)(uintptr_t)row;
+    return *(const global_u32_any *)(r + (uint32_t)(2 * L.at));
 }
 
 // N tensors' two channels of a token, in one masked region.  full (the same for the wave): all its
-// 128 channels exist.
-template <class T, int N>
+// channels exist.
+template <class T, int N, bool U = true>
 __device__ __forceinline__ void store2(void *const row[N], const Lane &L, bool full, const float v[N][2]) {
     uint32_t q[N];
+    global_char *to[N];
 #pragma unroll
-    for (int k = 0; k < N; ++k) q[k] = pack16<T>(v[k][0], v[k][1]);
+    for (int k = 0; k < N; ++k) {
+        q[k] = pack16<T>(v[k][0], v[k][1]);
+        to[k] = (U ? uniform(row[k]) : (global_char *)(uintptr_t)row[k]) + (uint32_t)(2 * L.at);
+    }
     if (full || L.both)
 #pragma unroll
-        for (int k = 0; k < N; ++k)
-            __builtin_nontemporal_store(q[k], (global_u32_any *)(uniform(row[k]) + (uint32_t)(2 * L.at)));
+        for (int k = 0; k < N; ++k) __builtin_nontemporal_store(q[k], (global_u32_any *)to[k]);
     if (!full && L.odd)
         if (L.second && !L.both)
 #pragma unroll
-            for (int k = 0; k < N; ++k)
-                ((global_u16 *)(uniform(row[k]) + (uint32_t)(2 * L.at)))[1] = (uint16_t)(q[k] >> 16);
+            for (int k = 0; k < N; ++k) ((global_u16 *)to[k])[1] = (uint16_t)(q[k] >> 16);
 }
 
 // Two fp32 values of a per-channel array.
@@ -146,6 +150,28 @@ __device__ __forceinline__ void put2(float *to, const Lane &L, float v0, float v
     if (L.both) to[L.k0] = v0;
     if (L.second) to[L.k1] = v1;
 }
+
+// Few channels: a wave's lanes are NG teams of 64 / NG, which take S tokens each, one team's after
+// the other's; otherwise the wave is one team.
+template <int NG>
+struct Team {
+    static constexpr int LANES = 64 / NG;
+    int lane, w;  // in the wave, and the wave
+    int c;        // lane in the team
+    int r;        // the team among the workgroup's, the same for a wave that is one
+
+    __device__ __forceinline__ Team() {
+        lane = threadIdx.x & 63;
+        w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        c = NG == 1 ? lane : lane % LANES;
+        r = NG == 1 ? w : w * NG + lane / LANES;
+    }
+
+    // Place in LDS of team v's value for this lane's channels.
+    __device__ __forceinline__ int of(int v) const { return v * LANES + c; }
+    __device__ __forceinline__ bool first_of_wave() const { return NG == 1 || lane < LANES; }
+    static __device__ __forceinline__ bool all(bool b) { return NG == 1 ? b : (bool)__all(b); }
+};
 
 // ---- words between chunks ------------------------------------------------------
 
@@ -233,11 +259,11 @@ __device__ __forceinline__ void compose(float A[2], float H[2], const float a[2]
 }
 
 // The state in front of place k, for all waves.  (ca, ch): the place's own
-// pair, known to wave `own`.  A word that stays empty for POLLS looks is computed here
+// pair, known to wave `own`, whose lanes with `writes` publish it.  A word that stays empty for POLLS looks is computed here
 // instead (chunk_pair(place, a, h) walks that place's tokens), so that every wait
 // ends whatever order the workgroups run in.
 template <int W, class F>
-__device__ __forceinline__ void carry_in(const RecGrid &q, int n, int32_t c, int k, const Lane &L, int w,
+__device__ __forceinline__ void carry_in(const RecGrid &q, int n, int32_t c, int k, const Lane &L, bool writes, int w,
                                          int own, const float ca[2], const float ch[2], F chunk_pair,
                                          float out[2]) {
     __shared__ f32x4 pairs[GROUP][64];
@@ -245,7 +271,7 @@ __device__ __forceinline__ void carry_in(const RecGrid &q, int n, int32_t c, int
     const int lane = threadIdx.x & 63, group = 1 << q.gs, g = k >> q.gs, i = k & (group - 1);
     const bool last = i + 1 == group;
     uint64_t *words = q.words + (int64_t)n * q.chunks * c, *states = q.states + (int64_t)n * q.groups * c;
-    if (w == own && !last && k + 1 < q.chunks) put(words + (int64_t)k * c, L, ca, ch);
+    if (w == own && writes && !last && k + 1 < q.chunks) put(words + (int64_t)k * c, L, ca, ch);
     constexpr int R = ROUND / W;
     for (int j0 = w; j0 < i; j0 += ROUND) {
         Words v[R];
@@ -297,7 +323,7 @@ __device__ __forceinline__ void carry_in(const RecGrid &q, int n, int32_t c, int
         }
         h[0] = __builtin_fmaf(A[0], h[0], H[0]);
         h[1] = __builtin_fmaf(A[1], h[1], H[1]);
-        if (last && k + 1 < q.chunks) {
+        if (writes && last && k + 1 < q.chunks) {
             const float next[2] = {__builtin_fmaf(ca[0], h[0], ch[0]), __builtin_fmaf(ca[1], h[1], ch[1])};
             const float zero[2] = {0.f, 0.f};
             put(states + (int64_t)(g + 1) * c, L, zero, next);
@@ -384,26 +410,29 @@ __device__ void walk_fwd(const RecParams &p, int64_t n, const Lane &L, int lo, i
     }
 }
 
-template <class T, bool G, int W, int S>
+template <class T, bool G, int W, int S, int NG>
 __global__ __launch_bounds__(64 * W, 4) void recurrence_fwd_kernel(const RecParams p, const RecGrid q) {
-    static_assert(SAVE % S == 0, "saved states lie at a wave's first token");
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    static_assert(SAVE % S == 0, "saved states lie at a team's first token");
+    constexpr bool U = NG == 1;
+    constexpr int TEAMS = W * NG, CHUNK = TEAMS * S;
+    const Team<NG> team;
+    const int w = team.w;
     const int col = blockIdx.x % q.cols, rest = blockIdx.x / q.cols;
     const int n = rest % p.n, chunk = rest / p.n;
-    const Lane L(col * COLS + 2 * lane, p.c);
+    const Lane L(2 * (col * team.LANES + team.c), p.c);
     const int len = length_of(p, n);
-    const int t0 = chunk * (W * S) + w * S, last = len > 0 ? len - 1 : 0;
+    const int t0 = chunk * CHUNK + team.r * S, last = len > 0 ? len - 1 : 0;
     const int64_t at = (int64_t)n * p.t * p.ld;
     const uint16_t *x = (const uint16_t *)p.x + at, *f = (const uint16_t *)p.f + at;
     const uint16_t *g = G ? (const uint16_t *)p.g + at : nullptr;
     uint32_t xr[S], fr[S], gr[S];
     const bool whole = t0 + S <= len;           // every token takes part
-    const bool full = (col + 1) * COLS <= p.c;  // every channel exists
+    const bool full = (col + 1) * 2 * team.LANES <= p.c;  // every channel exists
     int64_t o = (int64_t)min(t0, last) * p.ld;
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-        xr[s] = load2(x + o, L);
-        fr[s] = load2(f + o, L);
+        xr[s] = load2<U>(x + o, L);
+        fr[s] = load2<U>(f + o, L);
         o += t0 + s < last ? p.ld : 0;
     }
     float bias[2] = {0.f, 0.f};
@@ -447,29 +476,36 @@ __global__ __launch_bounds__(64 * W, 4) void recurrence_fwd_kernel(const RecPara
         h[0] = p.h0[(int64_t)n * p.c + L.k0];
         h[1] = p.h0[(int64_t)n * p.c + L.k1];
     }
-    __shared__ f32x4 part[W][64];
-    part[w][lane] = f32x4{A[0], H[0], A[1], H[1]};
+    __shared__ f32x4 part[W * 64];
+    part[threadIdx.x] = f32x4{A[0], H[0], A[1], H[1]};
     __syncthreads();
     if (G) {  // not needed before the state is there: on their way during the wait
         o = (int64_t)min(t0, last) * p.ld;
 #pragma unroll
         for (int s = 0; s < S; ++s) {
-            gr[s] = load2(g + o, L);
+            gr[s] = load2<U>(g + o, L);
             o += t0 + s < last ? p.ld : 0;
         }
     }
-    // what the waves in front make of the chunk's first state
+    // what the teams in front make of the chunk's first state
     float pa[2] = {1.f, 1.f}, ph[2] = {0.f, 0.f};
-    for (int v = 0; v < w; ++v) {
-        const f32x4 e = part[v][lane];
+    for (int v = 0; v < w * NG + NG - 1; ++v) {
+        if (v >= team.r) continue;
+        const f32x4 e = part[team.of(v)];
         const float ea[2] = {e[0], e[2]}, eh[2] = {e[1], e[3]};
         compose(pa, ph, ea, eh);
     }
     if (q.words) {
         float ca[2] = {pa[0], pa[1]}, ch[2] = {ph[0], ph[1]};
         compose(ca, ch, A, H);
-        carry_in<W>(q, n, p.c, chunk, L, w, W - 1, ca, ch, [&](int place, float *a2, float *h2) {
-            walk_fwd<T, W, S>(p, n, L, place * (W * S), len, bias, a2, h2);
+        if (NG > 1)  // the last team's is the chunk's
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                ca[k] = __shfl(ca[k], 64 - team.LANES + team.c);
+                ch[k] = __shfl(ch[k], 64 - team.LANES + team.c);
+            }
+        carry_in<W>(q, n, p.c, chunk, L, team.first_of_wave(), w, W - 1, ca, ch, [&](int place, float *a2, float *h2) {
+            walk_fwd<T, TEAMS, S>(p, n, L, place * CHUNK, len, bias, a2, h2);
         }, h);
     }
     h[0] = pa[0] * h[0] + ph[0];
@@ -493,14 +529,14 @@ __global__ __launch_bounds__(64 * W, 4) void recurrence_fwd_kernel(const RecPara
                 if (checked && t >= len) o[k] = 0.f;
             }
             void *const row[1] = {y};
-            if (!checked || t < p.t) store2<T, 1>(row, L, !checked, &o);
+            if (!checked || t < p.t) store2<T, 1, U>(row, L, !checked, &o);
         }
     };
-    if (whole && full)
+    if (team.all(whole) && full)
         finish(std::false_type{});
     else
         finish(std::true_type{});
-    if (p.ht && chunk == q.chunks - 1 && w == W - 1) put2(p.ht + (int64_t)n * p.c, L, h[0], h[1]);
+    if (p.ht && chunk == q.chunks - 1 && team.r == TEAMS - 1) put2(p.ht + (int64_t)n * p.c, L, h[0], h[1]);
 }
 
 // ---- backward -------------------------------------------------------------------
@@ -642,36 +678,39 @@ __device__ void walk_bwd(const RecParams &p, int64_t n, const Lane &L, int lo, i
     }
 }
 
-template <class T, bool G, int W, int S>
+template <class T, bool G, int W, int S, int NG>
 __global__ __launch_bounds__(64 * W, 2) void recurrence_bwd_kernel(const RecParams p, const RecGrid q) {
     static_assert((W * S) % SAVE == 0 && SAVE % S == 0, "a chunk is whole saved stretches");
-    constexpr int RUN = SAVE / S;  // waves that start from one saved state
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int RUN = SAVE / S;  // teams that start from one saved state
+    constexpr bool U = NG == 1;
+    constexpr int TEAMS = W * NG, CHUNK = TEAMS * S;
+    const Team<NG> team;
+    const int w = team.w;
     const int col = blockIdx.x % q.cols, rest = blockIdx.x / q.cols;
     const int n = rest % p.n, place = rest / p.n, chunk = q.chunks - 1 - place;  // the last one first
-    const Lane L(col * COLS + 2 * lane, p.c);
+    const Lane L(2 * (col * team.LANES + team.c), p.c);
     const int len = length_of(p, n);
-    const int t0 = chunk * (W * S) + w * S, last = len > 0 ? len - 1 : 0;
+    const int t0 = chunk * CHUNK + team.r * S, last = len > 0 ? len - 1 : 0;
     const int64_t at = (int64_t)n * p.t * p.ld;
     const uint16_t *x = (const uint16_t *)p.x + at, *f = (const uint16_t *)p.f + at;
     const uint16_t *g = G ? (const uint16_t *)p.g + at : nullptr;
     const uint16_t *dy = (const uint16_t *)p.dy + (int64_t)n * p.t * p.ldy;
     uint32_t xr[S], fr[S], gr[S], dr[S];
     const bool whole = t0 + S <= len;           // every token takes part
-    const bool full = (col + 1) * COLS <= p.c;  // every channel exists
+    const bool full = (col + 1) * 2 * team.LANES <= p.c;  // every channel exists
     int64_t o = (int64_t)min(t0, last) * p.ld;
     dy += (int64_t)min(t0, last) * p.ldy;
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-        xr[s] = load2(x + o, L);
-        fr[s] = load2(f + o, L);
-        gr[s] = G ? load2(g + o, L) : 0u;
-        dr[s] = load2(dy, L);
+        xr[s] = load2<U>(x + o, L);
+        fr[s] = load2<U>(f + o, L);
+        gr[s] = G ? load2<U>(g + o, L) : 0u;
+        dr[s] = load2<U>(dy, L);
         o += t0 + s < last ? p.ld : 0;
         dy += t0 + s < last ? p.ldy : 0;
     }
     float h[2] = {0.f, 0.f}, bias[2] = {0.f, 0.f};
-    const int run0 = t0 - w % RUN * S;  // first token of the saved stretch
+    const int run0 = t0 - team.r % RUN * S;  // first token of the saved stretch
     if (run0 < p.t) {
         const float *from = p.saved + ((int64_t)n * ((p.t + SAVE - 1) / SAVE) + run0 / SAVE) * p.c;
         h[0] = from[L.k0];
@@ -706,29 +745,38 @@ __global__ __launch_bounds__(64 * W, 2) void recurrence_bwd_kernel(const RecPara
         r[0] = p.dht[(int64_t)n * p.c + L.k0];
         r[1] = p.dht[(int64_t)n * p.c + L.k1];
     }
-    __shared__ f32x4 part[W][64];
-    __shared__ float part_r[W][2][64];
-    part[w][lane] = f32x4{A[0], H[0], A[1], H[1]};
-    part_r[w][0][lane] = R[0];
-    part_r[w][1][lane] = R[1];
+    __shared__ f32x4 part[W * 64];
+    __shared__ float part_r[2][W * 64];
+    part[threadIdx.x] = f32x4{A[0], H[0], A[1], H[1]};
+    part_r[0][threadIdx.x] = R[0];
+    part_r[1][threadIdx.x] = R[1];
     __syncthreads();
-    for (int v = w - w % RUN; v < w; ++v) {
-        const f32x4 m = part[v][lane];
+    for (int k = 0; k < RUN - 1; ++k) {
+        const int v = team.r - team.r % RUN + k;
+        if (v >= team.r) continue;
+        const f32x4 m = part[team.of(v)];
         h[0] = m[0] * h[0] + m[1];
         h[1] = m[2] * h[1] + m[3];
     }
-    // what the waves behind make of the gradient that flows into the chunk
+    // what the teams behind make of the gradient that flows into the chunk
     float pa[2] = {1.f, 1.f}, pr[2] = {0.f, 0.f};
-    for (int v = W - 1; v > w; --v) {
-        const f32x4 m = part[v][lane];
-        const float ma[2] = {m[0], m[2]}, mr[2] = {part_r[v][0][lane], part_r[v][1][lane]};
+    for (int v = TEAMS - 1; v > w * NG; --v) {
+        if (v <= team.r) continue;
+        const f32x4 m = part[team.of(v)];
+        const float ma[2] = {m[0], m[2]}, mr[2] = {part_r[0][team.of(v)], part_r[1][team.of(v)]};
         compose(pa, pr, ma, mr);
     }
     if (q.words) {
         float ca[2] = {pa[0], pa[1]}, cr[2] = {pr[0], pr[1]};
         compose(ca, cr, A, R);
-        carry_in<W>(q, n, p.c, place, L, w, 0, ca, cr, [&](int at2, float *a2, float *r2) {
-            walk_bwd<T, G, W, S>(p, n, L, (q.chunks - 1 - at2) * (W * S), len, bias, a2, r2);
+        if (NG > 1)  // the first team's is the chunk's
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                ca[k] = __shfl(ca[k], team.c);
+                cr[k] = __shfl(cr[k], team.c);
+            }
+        carry_in<W>(q, n, p.c, place, L, team.first_of_wave(), w, 0, ca, cr, [&](int at2, float *a2, float *r2) {
+            walk_bwd<T, G, TEAMS, S>(p, n, L, (q.chunks - 1 - at2) * CHUNK, len, bias, a2, r2);
         }, r);
     }
     r[0] = pa[0] * r[0] + pr[0];
@@ -762,23 +810,23 @@ __global__ __launch_bounds__(64 * W, 2) void recurrence_bwd_kernel(const RecPara
                 total[k] += out[1][k];
             }
             void *const row[3] = {dx + o, df + o, dg + o};
-            if (!checked || t < p.t) store2<T, G ? 3 : 2>(row, L, !checked, out);
+            if (!checked || t < p.t) store2<T, G ? 3 : 2, U>(row, L, !checked, out);
         }
     };
-    if (whole && full)
+    if (team.all(whole) && full)
         finish(std::false_type{});
     else
         finish(std::true_type{});
-    if (p.dh0 && chunk == 0 && w == 0) put2(p.dh0 + (int64_t)n * p.c, L, r[0], r[1]);
+    if (p.dh0 && chunk == 0 && team.r == 0) put2(p.dh0 + (int64_t)n * p.c, L, r[0], r[1]);
     if (p.part) {
         __syncthreads();
-        part_r[w][0][lane] = total[0];
-        part_r[w][1][lane] = total[1];
+        part_r[0][threadIdx.x] = total[0];
+        part_r[1][threadIdx.x] = total[1];
         __syncthreads();
-        if (w != 0) return;
-        for (int v = 1; v < W; ++v) {
-            total[0] += part_r[v][0][lane];
-            total[1] += part_r[v][1][lane];
+        if (w != 0 || !team.first_of_wave()) return;
+        for (int v = 1; v < TEAMS; ++v) {
+            total[0] += part_r[0][team.of(v)];
+            total[1] += part_r[1][team.of(v)];
         }
         float *to = p.part + ((int64_t)n * q.chunks + chunk) * p.c;
         put2(to, L, total[0], total[1]);
@@ -868,10 +916,12 @@ __global__ __launch_bounds__(64) void recurrence_bwd_single_kernel(const RecPara
 }
 
 constexpr int FW = 8, FS = 16, BW = 4, BS = 16;  // waves, and tokens of each
-constexpr int FCHUNK = FW * FS, BCHUNK = BW * BS;
+
+// Teams of a wave: as many as leave each the lanes for all channels.
+int teams_of(const RecParams &p) { return p.c <= 16 ? 8 : p.c <= 32 ? 4 : p.c <= 64 ? 2 : 1; }
 
 int64_t chunks_of(const RecParams &p, bool backward) {
-    const int k = backward ? BCHUNK : FCHUNK;
+    const int k = (backward ? BW * BS : FW * FS) * teams_of(p);
     return p.t <= SHORT_T || p.c == 1 ? 1 : ((int64_t)p.t + k - 1) / k;
 }
 
@@ -882,7 +932,7 @@ int64_t chunks_of(const RecParams &p, bool backward) {
 RecGrid grid_of(const RecParams &p, bool backward) {
     RecGrid q{};
     const int64_t chunks = chunks_of(p, backward);
-    q.cols = (p.c + COLS - 1) / COLS;
+    q.cols = (p.c + COLS - 1) / COLS;  // one where a wave is several teams
     q.chunks = (int32_t)chunks;
     while (1 << q.gs < GROUP && chunks >> 2 * q.gs > 1) ++q.gs;
     q.groups = (int32_t)((chunks + (1 << q.gs) - 1) >> q.gs);
@@ -918,6 +968,14 @@ RecParams some(const RecParams &p, bool backward, int64_t n0, int64_t n) {
     return s;
 }
 
+template <class T, bool G, int NG>
+void launch_split(const RecParams &s, const RecGrid &q, bool backward, uint32_t blocks, hipStream_t st) {
+    if (backward)
+        hipLaunchKernelGGL((recurrence_bwd_kernel<T, G, BW, BS, NG>), dim3(blocks), dim3(64 * BW), 0, st, s, q);
+    else
+        hipLaunchKernelGGL((recurrence_fwd_kernel<T, G, FW, FS, NG>), dim3(blocks), dim3(64 * FW), 0, st, s, q);
+}
+
 template <class T, bool G>
 hipError_t run(const RecParams &p, bool backward, hipStream_t st) {
     RecGrid q = grid_of(p, backward);
@@ -949,11 +1007,13 @@ hipError_t run(const RecParams &p, bool backward, hipStream_t st) {
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
         }
-        const dim3 grid((uint32_t)(each * s.n));
-        if (backward)
-            hipLaunchKernelGGL((recurrence_bwd_kernel<T, G, BW, BS>), grid, dim3(64 * BW), 0, st, s, q);
-        else
-            hipLaunchKernelGGL((recurrence_fwd_kernel<T, G, FW, FS>), grid, dim3(64 * FW), 0, st, s, q);
+        const uint32_t blocks = (uint32_t)(each * s.n);
+        switch (teams_of(p)) {
+            case 1: launch_split<T, G, 1>(s, q, backward, blocks, st); break;
+            case 2: launch_split<T, G, 2>(s, q, backward, blocks, st); break;
+            case 4: launch_split<T, G, 4>(s, q, backward, blocks, st); break;
+            default: launch_split<T, G, 8>(s, q, backward, blocks, st); break;
+        }
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
