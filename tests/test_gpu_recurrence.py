@@ -162,6 +162,13 @@ CASES = [
     dict(n=4, t=1, c=72, dtype="f16", lengths=[0, 1, 2, -1]),
     dict(n=3, t=700, c=20, dtype="bf16", lengths=[0, 320, 699], carry=False),
     dict(n=2, t=90, c=16, dtype="f16", lengths=[0, 0], pad=1),
+    # every number of waves and of teams of a wave, and the lengths where they change
+    dict(n=2, t=6, c=200, dtype="f16"), dict(n=2, t=7, c=200, dtype="bf16"), dict(n=2, t=16, c=131, dtype="f16"),
+    dict(n=2, t=17, c=130, dtype="f16"), dict(n=2, t=32, c=130, dtype="bf16", lengths=[31, 17]), dict(n=2, t=48, c=66, dtype="f16"),
+    dict(n=3, t=64, c=64, dtype="f16"), dict(n=3, t=65, c=63, dtype="bf16", lengths=[0, 64, 33]), dict(n=2, t=32, c=33, dtype="f16"),
+    dict(n=2, t=33, c=64, dtype="f16"), dict(n=2, t=64, c=32, dtype="f16"), dict(n=2, t=130, c=31, dtype="bf16"),
+    dict(n=2, t=1300, c=17, dtype="f16", pad=34), dict(n=2, t=128, c=16, dtype="f16"), dict(n=2, t=129, c=2, dtype="f16"),
+    dict(n=2, t=2500, c=15, dtype="bf16", lengths=[1025, 2500]), dict(n=1, t=9000, c=3, dtype="f16", with_g=False),
     # nothing to do but to hand the state on
     dict(n=3, t=0, c=10, dtype="f16"),
 ]
