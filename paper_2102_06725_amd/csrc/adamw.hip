@@ -1,16 +1,16 @@
-// adamw.hip -- AdamW over a list of tensors in one launch, with fp32 moments
-// or 8-bit ones.
+// adamw.hip -- AdamW over a list of tensors in one launch, with fp32 moments or 8-bit ones.
 //
-// Bound by memory: 30 bytes a parameter with fp32 gradients, moments and a
-// 16-bit copy, 18 (and a 32nd) with 8-bit moments.  The list is cut into chunks, whose
-// records (addresses and all) lie in the plan; as many workgroups as fit the chip at once
-// (1280; 2048 took 7 % longer) walk them, each with the next record on its way.  A lane takes 4 neighbouring elements at a time, in 16-byte accesses
-// at any alignment; 16 lanes hold a block of 8-bit moments.  (8 neighbouring elements a lane
-// with 8-bit moments, half as many accesses, but each of half cache lines: 1479 us where 4 take 1160.)
+// Bound by memory: 30 bytes a parameter with fp32 gradients, moments and a 16-bit copy, 18 (and
+// a 32nd) with 8-bit moments.  The list is cut into chunks, whose records (addresses and all)
+// lie in the plan; as many workgroups as fit the chip at once (1280; 2048 took 7 % longer) walk
+// them, each with the next record on its way.  A lane takes 4 neighbouring elements at a time,
+// in 16-byte accesses at any alignment; 16 lanes hold a block of 8-bit moments.  (8
+// neighbouring elements a lane with 8-bit moments, half as many accesses, but each of half
+// cache lines: 1479 us where 4 take 1160.)
 //
-// Measured: 23.5 M parameters in 159 tensors 126 us (5.6 TB/s); 302 M with 8-bit moments 1.16 ms
-// (4.7 TB/s; a copy of that size 4.83); without the hash and the rounding it would
-// take 1.15 ms.
+// Measured: 23.5 M parameters in 159 tensors 126 us (5.6 TB/s); 302 M with 8-bit moments 1.16
+// ms (4.7 TB/s; a copy of that size 4.83); without the hash and the rounding it would take 1.15
+// ms.
 #include "launch.hpp"
 
 namespace nnconv {
@@ -73,8 +73,8 @@ __device__ __forceinline__ uint32_t dither_bits(uint32_t key, uint32_t i) {
 
 __device__ __forceinline__ float pow2(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }
 
-// beta^t for t >= 0, in 64 bits by squaring: 1 - beta^t would lose most of
-// its bits in 32 for a beta near 1.
+// beta^t for t >= 0, in 64 bits by squaring: 1 - beta^t would lose most of its bits in 32 for a
+// beta near 1.
 __device__ __forceinline__ double power(double b, int32_t t) {
     double r = 1.0;
     for (; t > 0; t >>= 1, b *= b)
@@ -83,9 +83,8 @@ __device__ __forceinline__ double power(double b, int32_t t) {
 }
 
 // Magnitude of the 8-bit code of y >= 0 in units of 2^k: LOW smallest exponent, M mantissa
-// bits; u in (0, 1).  y lies within the range of the format at that scale, and so does
-// its rounding: the largest value is a whole number of the topmost spacings.
-// A NaN stays.
+// bits; u in (0, 1).  y lies within the range of the format at that scale, and so does its
+// rounding: the largest value is a whole number of the topmost spacings. A NaN stays.
 template <int LOW, int M, bool KEEP>
 __device__ __forceinline__ float round_random(float y, int k, float u) {
     int e = __builtin_amdgcn_frexp_expf(y) - 1 - M;  // exponent of the spacing
@@ -374,9 +373,9 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(const AdamwTable tab, in
                  : full ? go(c, Lanes<false, true>{}) : go(c, Lanes<false, false>{})))
             return;
     }
-    // The last workgroup counts the step: by then all have read the count.  They
-    // arrive in teams first: at one address, one after the other, the 384 workgroups of an
-    // update of 0.8 M parameters took 2.4 of its 10.1 us.
+    // The last workgroup counts the step: by then all have read the count.  They arrive in
+    // teams first: at one address, one after the other, the 384 workgroups of an update of 0.8
+    // M parameters took 2.4 of its 10.1 us.
     __syncthreads();
     if (threadIdx.x != 0) return;
     const uint32_t blocks = gridDim.x;

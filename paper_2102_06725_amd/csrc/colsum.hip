@@ -1,6 +1,6 @@
-// colsum.hip -- per-channel sums of fp32 partials [parts][c], in a fixed
-// order, with the loss-scale step of a parameter gradient.  Bound by the latency of
-// a few rounds of loads: 4 to 5 us for 128 to 512 parts.
+// colsum.hip -- per-channel sums of fp32 partials [parts][c], in a fixed order, with the
+// loss-scale step of a parameter gradient.  Bound by the latency of a few rounds of loads: 4 to
+// 5 us for 128 to 512 parts.
 #include "launch.hpp"
 
 namespace nnconv {
@@ -9,9 +9,9 @@ namespace {
 
 constexpr int WAVES = 16;
 
-// 64 channels per workgroup; wave w adds parts w, w + 16, ... in increasing
-// order, eight loads in flight, and wave 0 the 16 waves' sums.  With out a
-// null pointer the sums of this workgroup's share of the parts go to next.
+// 64 channels per workgroup; wave w adds parts w, w + 16, ... in increasing order, eight loads
+// in flight, and wave 0 the 16 waves' sums.  With out a null pointer the sums of this
+// workgroup's share of the parts go to next.
 __global__ __launch_bounds__(64 * WAVES) void colsum_kernel(const float *__restrict__ part,
                                                             int64_t parts, int64_t per, int32_t c,
                                                             float *next, float *out,

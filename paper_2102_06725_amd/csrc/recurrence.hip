@@ -5,8 +5,7 @@ namespace nnconv {
 
 namespace {
 
-// Before each split call: every word empty but the states in front of the
-// first places.
+// Before each split call: every word empty but the states in front of the first places.
 __global__ __launch_bounds__(256) void recurrence_words_kernel(const RecGrid q, int64_t n, int32_t c,
                                                                const float *init) {
     const int64_t plain = n * q.chunks * c, total = plain + n * q.groups * c;
@@ -20,12 +19,13 @@ __global__ __launch_bounds__(256) void recurrence_words_kernel(const RecGrid q, 
     }
 }
 
-// Teams of a wave: as many as leave each the lanes for all channels.  (One team throughout: forward of 54 x
-// 1511 x 16, ragged, 20.6 us, 17.2 with eight; forward and backward of 2 x 38104 x 40 75 us, 61 with two.)
+// Teams of a wave: as many as leave each the lanes for all channels.  (One team throughout:
+// forward of 54 x 1511 x 16, ragged, 20.6 us, 17.2 with eight; forward and backward of 2 x
+// 38104 x 40 75 us, 61 with two.)
 int teams_of(const RecParams &p) { return p.c <= 16 ? 8 : p.c <= 32 ? 4 : p.c <= 64 ? 2 : 1; }
 
-// Waves of a workgroup: no more than the tokens need.  (Eight throughout: forward of 4096 x 16 x 1152
-// 401 us, one wave 113; backward 470 and 184.)
+// Waves of a workgroup: no more than the tokens need.  (Eight throughout: forward of 4096 x 16
+// x 1152 401 us, one wave 113; backward 470 and 184.)
 int waves_of(const RecParams &p, bool backward) {
     const int most = backward ? BWD_WAVES : FWD_WAVES, each = TOKENS * teams_of(p);
     if (teams_of(p) > 1) return p.t <= each ? 1 : most;
@@ -39,10 +39,10 @@ int64_t chunks_of(const RecParams &p, bool backward) {
     return p.t <= SHORT_T || p.c == 1 ? 1 : ((int64_t)p.t + k - 1) / k;
 }
 
-// Places in groups of 2^gs: about as many groups, whose states are handed on
-// one after the other, as places in one, whose pairs each place reads.  (Groups of
-// 16 throughout: backward of 8 x 2048 x 1152 4 us slower.  Groups of at most 16: forward of 1 x
-// 65536 x 256 47 us, 42 with 32.)
+// Places in groups of 2^gs: about as many groups, whose states are handed on one after the
+// other, as places in one, whose pairs each place reads.  (Groups of 16 throughout: backward of
+// 8 x 2048 x 1152 4 us slower.  Groups of at most 16: forward of 1 x 65536 x 256 47 us, 42 with
+// 32.)
 RecGrid grid_of(const RecParams &p, bool backward) {
     RecGrid q{};
     const int64_t chunks = chunks_of(p, backward);

@@ -1,32 +1,31 @@
-// recurrence.hpp -- what the kernels of the gated linear recurrence share: gates,
-// lanes, and the exchange between workgroups.
+// recurrence.hpp -- what the kernels of the gated linear recurrence share: gates, lanes, and
+// the exchange between workgroups.
 //
-// h_t = a_t h_(t-1) + u_t is a composition of affine maps, so a stretch of
-// tokens is the pair (A, H) of h_out = A h_in + H, and stretches can be
-// computed apart and joined:
+// h_t = a_t h_(t-1) + u_t is a composition of affine maps, so a stretch of tokens is the pair
+// (A, H) of h_out = A h_in + H, and stretches can be computed apart and joined:
 //   - a lane holds two neighbouring channels (one 4-byte load of a 16-bit
-//     tensor) and walks S tokens that it keeps in registers; a wave covers 128
-//     channels, the W waves of a workgroup W * S consecutive tokens (a chunk);
+//     tensor) and walks 16 tokens that it keeps in registers; a wave covers 128
+//     channels (or, of 64 channels and fewer, 16 tokens with each of its teams of
+//     lanes), and the waves of a workgroup consecutive tokens (a chunk);
 //   - the waves exchange their (A, H) through LDS;
 //   - chunks exchange theirs through one 64-bit word per channel in the
 //     workspace (below).  The inputs are read once, and y is computed from
 //     registers.
-// Whether a token takes part is the same for a whole wave, so lengths
-// and the end of the sequence cost no divergence.
+// Whether a token takes part is the same for a whole wave, so lengths and the end of the
+// sequence cost no divergence.
 //
-// Bound by memory (8 bytes a token and channel forward, 14 backward), and close behind it by the
-// vector units: a forward element takes 37 instructions, 4 of them transcendental, which alone
-// would take half of the time.  Measured, cold: forward of 8 x 2048 x 1152
-// 37 us (4.1 TB/s), backward 60 us (4.4 TB/s); forward of 2 x 32768 x 768 95 us (4.2 TB/s; the
-// same elements as 512 sequences of 128 tokens, one chunk each, 74 us).  Short
-// calls are bound by their launches and one exchange between workgroups: 6 us
-// for one chunk, 10 for two.
+// Bound by memory (8 bytes a token and channel forward, 14 backward), and close behind it by
+// the vector units: a forward element takes 37 instructions, 4 of them transcendental, which
+// alone would take half of the time.  Measured, cold: forward of 8 x 2048 x 1152 37 us (4.1
+// TB/s), backward 60 us (4.4 TB/s); forward of 2 x 32768 x 768 95 us (4.2 TB/s; the same
+// elements as 512 sequences of 128 tokens, one chunk each, 74 us).  Short calls are bound by
+// their launches and one exchange between workgroups: 6 us for one chunk, 10 for two.
 //
-// Chunks: forward 8 waves of 16 tokens, backward 4 of 16, the most that leave two
-// workgroups to a compute unit (126 and 248 registers): what is on its way and what waits for
-// its predecessors are then never the same.  16 waves of 8 tokens, 4 of 32 and 16 of 16 took 103, 102 and
-// 98 us where 8 of 16 take 97, chunks of half the tokens 115; backward, 8 waves of 8 and 16 of 4
-// took 65 and 66 us where 4 of 16 take 55.
+// Chunks: forward 8 waves of 16 tokens, backward 4 of 16, the most that leave two workgroups to
+// a compute unit (126 and 248 registers): what is on its way and what waits for its
+// predecessors are then never the same.  16 waves of 8 tokens, 4 of 32 and 16 of 16 took 103,
+// 102 and 98 us where 8 of 16 take 97, chunks of half the tokens 115; backward, 8 waves of 8
+// and 16 of 4 took 65 and 66 us where 4 of 16 take 55.
 #pragma once
 
 #include <type_traits>
@@ -35,7 +34,8 @@
 
 namespace nnconv {
 
-// How a call is split.  Chunks of waves * teams * 16 tokens; more than one only with the most waves.
+// How a call is split.  Chunks of waves * teams * 16 tokens; more than one only with the most
+// waves.
 struct RecGrid {
     int32_t cols, waves, teams, chunks, gs, groups;
     uint64_t *words;   // [n][chunks][c], null for a single chunk
@@ -44,11 +44,12 @@ struct RecGrid {
 
 constexpr int FWD_WAVES = 8, BWD_WAVES = 4;  // at most
 constexpr int TOKENS = 16;                   // of a team
-constexpr int SHORT_T = 6;                   // up to here a lane walks all tokens (forward of 4096 x 6 x 1152 39
-                                             // us, 52 as a chunk; with 8 tokens 54 and 59, backward 164 and 128)
+// Up to here a lane walks all tokens, without a barrier (forward of 4096 x 6 x 1152 39 us, 52 as
+// a chunk; with 8 tokens 54 and 59, backward 164 and 128).
+constexpr int SHORT_T = 6;
 
-// One column of channels and one chunk a workgroup; `blocks` of them.  dtype, and whether p.g is
-// given, choose the kernel, and q.waves and q.teams.
+// One column of channels and one chunk a workgroup; `blocks` of them.  dtype, and whether p.g
+// is given, choose the kernel, and q.waves and q.teams.
 void launch_recurrence_fwd_chunks(int dtype, const RecParams &p, const RecGrid &q, uint32_t blocks, hipStream_t st);
 void launch_recurrence_bwd_chunks(int dtype, const RecParams &p, const RecGrid &q, uint32_t blocks, hipStream_t st);
 // t <= SHORT_T; c = 1.
@@ -70,16 +71,15 @@ typedef uint32_t __attribute__((aligned(2))) u32_any;  // 4-byte access at any e
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float Z_MAX = 80.f * LOG2E;
 
-// The gate a = sigma(z) and b = 1 - a = sigma(-z), each to full relative
-// precision: with a near 1 the difference 1 - a would keep few bits of the
-// long memories' rates.  bias is the negated bias times log2(e): -z log2(e) is one
-// multiply-add.  The limits let a NaN through.
+// The gate a = sigma(z) and b = 1 - a = sigma(-z), each to full relative precision: with a near
+// 1 the difference 1 - a would keep few bits of the long memories' rates.  bias is the negated
+// bias times log2(e): -z log2(e) is one multiply-add.  The limits let a NaN through.
 __device__ __forceinline__ void gate(float f, float bias, float &a, float &b) {
     float z = __builtin_fmaf(f, -LOG2E, bias);
     z = __builtin_elementwise_minimum(__builtin_elementwise_maximum(z, -Z_MAX), Z_MAX);
     const float e = __builtin_amdgcn_exp2f(z);
-    // one Newton step on the reciprocal, whose own error of up to a unit has a sign: a
-    // product of a thousand gates near 1 would add it up
+    // one Newton step on the reciprocal, whose own error of up to a unit has a sign: a product
+    // of a thousand gates near 1 would add it up
     const float d = 1.0f + e, r = __builtin_amdgcn_rcpf(d);
     a = __builtin_fmaf(r, __builtin_fmaf(-d, r, 1.0f), r);
     b = e * a;
@@ -96,9 +96,9 @@ __device__ __forceinline__ int length_of(const RecParams &p, int n) {
 }
 
 // The two channels of a lane.  c >= 2: a lane whose second channel would be past the end (the
-// last one of an odd count) takes the last two, the first of which is its neighbour's, and writes the second
-// alone: the neighbour may be in another workgroup, and states may be updated in place.
-// Lanes past the end load the last two and write nothing.
+// last one of an odd count) takes the last two, the first of which is its neighbour's, and
+// writes the second alone: the neighbour may be in another workgroup, and states may be updated
+// in place. Lanes past the end load the last two and write nothing.
 struct Lane {
     uint32_t at;  // first channel
     int k0, k1;   // the channels, for per-channel fp32 arrays and words
@@ -130,8 +130,8 @@ __device__ __forceinline__ void unpack<BFloat>(uint32_t v, float o[2]) {
     o[1] = __builtin_bit_cast(float, v & 0xFFFF0000u);
 }
 
-// The token at `row`, an address that is the same for the whole wave: in scalar
-// registers, so that an access costs no address arithmetic on the vector units.
+// The token at `row`, an address that is the same for the whole wave: in scalar registers, so
+// that an access costs no address arithmetic on the vector units.
 typedef __attribute__((address_space(1))) char global_char;
 
 __device__ __forceinline__ global_char *uniform(const void *row) {
@@ -150,8 +150,8 @@ __device__ __forceinline__ uint32_t load2(const void *row, const Lane &L) {
     return *(const global_u32_any *)(r + (uint32_t)(2 * L.at));
 }
 
-// N tensors' two channels of a token, in one masked region.  full (the same for the wave): all its
-// channels exist.
+// N tensors' two channels of a token, in one masked region.  full (the same for the wave): all
+// its channels exist.
 template <class T, int N, bool U = true>
 __device__ __forceinline__ void store2(void *const row[N], const Lane &L, bool full, const float v[N][2]) {
     uint32_t q[N];
@@ -176,8 +176,8 @@ __device__ __forceinline__ void put2(float *to, const Lane &L, float v0, float v
     if (L.second) to[L.k1] = v1;
 }
 
-// Few channels: a wave's lanes are NG teams of 64 / NG, which take S tokens each, one team's after
-// the other's; otherwise the wave is one team.
+// Few channels: a wave's lanes are NG teams of 64 / NG, which take S tokens each, one team's
+// after the other's; otherwise the wave is one team.
 template <int NG>
 struct Team {
     static constexpr int LANES = 64 / NG;
@@ -200,14 +200,13 @@ struct Team {
 
 // ---- words between chunks ------------------------------------------------------
 
-// Chunks are taken in the direction of the recurrence: place k of a sequence.
-// Two arrays of 64-bit words, all ones until written: the (A, H) of every place,
-// and the state in front of every group of 2^gs places: a place waits for the pairs in front of
-// it in its group, all at once, and for the group's state, which the last place of
-// the group before hands on.  A word is stored and loaded at
-// once, so it needs no flag and no ordering with other memory.  Which words are
-// composed, and in which order, depends on the sizes alone, so that results
-// do not depend on which workgroup came first.
+// Chunks are taken in the direction of the recurrence: place k of a sequence. Two arrays of
+// 64-bit words, all ones until written: the (A, H) of every place, and the state in front of
+// every group of 2^gs places: a place waits for the pairs in front of it in its group, all at
+// once, and for the group's state, which the last place of the group before hands on.  A word
+// is stored and loaded at once, so it needs no flag and no ordering with other memory.  Which
+// words are composed, and in which order, depends on the sizes alone, so that results do not
+// depend on which workgroup came first.
 constexpr int GROUP = 32;  // places of a group at most
 constexpr int ROUND = 16;  // rows of words that a workgroup has on their way at once
 constexpr int POLLS = 4096;
@@ -262,9 +261,9 @@ __device__ __forceinline__ void compose(float A[2], float H[2], const float a[2]
     A[1] = fmaxf(A[1] * a[1], A_MIN);
 }
 
-// The state in front of place k, for all waves.  (ca, ch): the place's own
-// pair, known to wave `own`, whose lanes with `writes` publish it.  A word that stays empty for POLLS looks is computed here
-// instead (chunk_pair(place, a, h) walks that place's tokens), so that every wait
+// The state in front of place k, for all waves.  (ca, ch): the place's own pair, known to wave
+// `own`, whose lanes with `writes` publish it.  A word that stays empty for POLLS looks is
+// computed here instead (chunk_pair(place, a, h) walks that place's tokens), so that every wait
 // ends whatever order the workgroups run in.
 template <int W, class F>
 __device__ __forceinline__ void carry_in(const RecGrid &q, int n, int32_t c, int k, const Lane &L, bool writes, int w,

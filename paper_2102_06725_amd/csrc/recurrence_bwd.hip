@@ -5,9 +5,9 @@ namespace nnconv {
 
 namespace {
 
-// With own_t = dy_t g_t sigma(g_t), the gradient of h_t is d_t = own_t + r_t, where r_t
-// flows in from the right: r_(t-1) = a_t d_t.  So r obeys the same kind
-// of recurrence from the last token on, with a_t and a_t own_t.
+// With own_t = dy_t g_t sigma(g_t), the gradient of h_t is d_t = own_t + r_t, where r_t flows
+// in from the right: r_(t-1) = a_t d_t.  So r obeys the same kind of recurrence from the last
+// token on, with a_t and a_t own_t.
 
 // r in front of a token; not fused with the product that own is, so that every place that
 // computes it gets the same bits.
@@ -46,8 +46,8 @@ struct Grad {
     }
 };
 
-// Few tokens: a lane walks them all, forward for the states (t <= SHORT_T of
-// them, in LDS) and back.
+// Few tokens: a lane walks them all, forward for the states (t <= SHORT_T of them, in LDS) and
+// back.
 template <class T, bool G>
 __global__ __launch_bounds__(64) void recurrence_bwd_short_kernel(const RecParams p) {
     __shared__ float hs[SHORT_T][2][64];
@@ -110,7 +110,8 @@ __global__ __launch_bounds__(64) void recurrence_bwd_short_kernel(const RecParam
     }
 }
 
-// The pair of a chunk for r, walked from its last token on with the arithmetic of the kernel below.
+// The pair of a chunk for r, walked from its last token on with the arithmetic of the kernel
+// below.
 template <class T, bool G, int W, int S>
 __device__ void walk_bwd(const RecParams &p, int64_t n, const Lane &L, int lo, int len,
                          const float bias[2], float A[2], float R[2]) {

@@ -1,18 +1,16 @@
-// rmsnorm.hip -- root-mean-square norm over the channels of channel-last rows,
-// with the residual's addition in front, a 16-bit or 8-bit output, and its
-// backward pass.
+// rmsnorm.hip -- root-mean-square norm over the channels of channel-last rows, with the
+// residual's addition in front, a 16-bit or 8-bit output, and its backward pass.
 //
-// Bound by memory: a row is read once into registers, 8 channels (one
-// 16-byte access) at a time, and everything is computed from there.  TPR threads
-// hold a row of up to 8 * V * TPR channels, vector k * TPR + i of it in
-// thread i: parts of a wave, a wave, or a workgroup, so that short rows fill waves
-// and long ones fit the registers.  Rows of any channel count and
-// alignment run on the same kernels: the last vector of a row whose channels are no multiple of 8
-// starts at channel c - 8, and the channels it shares with the one before count once.
+// Bound by memory: a row is read once into registers, 8 channels (one 16-byte access) at a
+// time, and everything is computed from there.  TPR threads hold a row of up to 8 * V * TPR
+// channels, vector k * TPR + i of it in thread i: parts of a wave, a wave, or a workgroup, so
+// that short rows fill waves and long ones fit the registers.  Rows of any channel count and
+// alignment run on the same kernels: the last vector of a row whose channels are no multiple of
+// 8 starts at channel c - 8, and the channels it shares with the one before count once.
 //
-// Measured: 16384 x 4096 with a residual to 8 bits 83 us (5.7 TB/s); 200704 x 256
-// forward 66 us (6.2 TB/s), backward 65 us and 5 us for the sum of dgain's parts; 12345 x 771 (rows at
-// every alignment) 16, 17 and 4 us.
+// Measured: 16384 x 4096 with a residual to 8 bits 83 us (5.7 TB/s); 200704 x 256 forward 66 us
+// (6.2 TB/s), backward 65 us and 5 us for the sum of dgain's parts; 12345 x 771 (rows at every
+// alignment) 16, 17 and 4 us.
 #include <type_traits>
 
 #include "launch.hpp"
@@ -66,7 +64,8 @@ __device__ __forceinline__ float row_reduce(float v, float *buf, F op) {
     return v;
 }
 
-// One vector of a row: where it starts, and its channels below `skip` belong to the vector before.
+// One vector of a row: where it starts, and its channels below `skip` belong to the vector
+// before.
 struct Slot {
     int at, skip;
     bool in;
@@ -78,8 +77,8 @@ struct Slot {
     }
 };
 
-// What a pass reads or writes once streams past the caches; but rows that do not start
-// on 16 bytes (ANY) share cache lines between lanes' loads, which then come from the cache.
+// What a pass reads or writes once streams past the caches; but rows that do not start on 16
+// bytes (ANY) share cache lines between lanes' loads, which then come from the cache.
 template <bool ANY>
 __device__ __forceinline__ u32x4 load8(const void *p, int64_t i) {
     const u32x4_any *q = (const u32x4_any *)((const uint16_t *)p + i);
@@ -245,8 +244,8 @@ __global__ __launch_bounds__(TPR <= 64 ? 256 : TPR) void rmsnorm_fwd_kernel(cons
     }
 }
 
-// Rows that the registers do not hold, and rows of fewer channels than a vector:
-// a workgroup per row, which reads it again for the output (and for the scales).
+// Rows that the registers do not hold, and rows of fewer channels than a vector: a workgroup
+// per row, which reads it again for the output (and for the scales).
 template <class T, bool Q8>
 __global__ __launch_bounds__(512) void rmsnorm_fwd_any_kernel(const NormParams p) {
     __shared__ float buf[2][8];
@@ -297,8 +296,8 @@ __global__ __launch_bounds__(512) void rmsnorm_fwd_any_kernel(const NormParams p
 
 // ---- backward ------------------------------------------------------------------------
 
-// dx, and the workgroup's share of dgain: a thread keeps the sums of its channels over all its rows in
-// registers, which are added up once, in a fixed order.
+// dx, and the workgroup's share of dgain: a thread keeps the sums of its channels over all its
+// rows in registers, which are added up once, in a fixed order.
 template <class T, int TPR, int V, bool TAIL>
 __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void rmsnorm_bwd_kernel(const NormBwdParams p) {
     constexpr int WG = TPR < 512 ? 512 : TPR, ROWS = WG / TPR, LANES = TPR < 64 ? TPR : 64;
@@ -440,14 +439,14 @@ __global__ __launch_bounds__(256) void rmsnorm_dgain_any_kernel(const NormBwdPar
 // ---- which kernel ---------------------------------------------------------------------
 
 // Threads of a row and vectors of each.  One vector a thread wherever a workgroup is enough:
-// more threads have more loads on their way, and the waits of one row's reduction are
-// covered by other workgroups.  Against a wave a row with 4 vectors and 256 threads with 4 (us, forward with
-// a residual, 16 bits):
+// more threads have more loads on their way, and the waits of one row's reduction are covered
+// by other workgroups.  Against a wave a row with 4 vectors and 256 threads with 4 (us, forward
+// with a residual, 16 bits):
 //   2048 channels:  8 rows 4.3 -> 2.6,  8192 rows 27.7 -> 23.8,  32768 rows 100 -> 80
 //   8192 channels:  8 rows 4.6 -> 3.1,  8192 rows 102 -> 84,     32768 rows 410 -> 350
-// The backward pass keeps sums of dgain in registers and writes them once a
-// workgroup; from 2049 channels on it is the faster with two vectors (4096 channels, 32768 rows:
-// 175 us, 186 with one; 8192 channels: 352 and 369).
+// The backward pass keeps sums of dgain in registers and writes them once a workgroup; from
+// 2049 channels on it is the faster with two vectors (4096 channels, 32768 rows: 175 us, 186
+// with one; 8192 channels: 352 and 369).
 struct Shape {
     int tpr, v;
 };
@@ -552,8 +551,8 @@ void bwd(const NormBwdParams &p, hipStream_t st) {
 int32_t rmsnorm_bwd_parts(int64_t rows, int32_t c) {
     const Shape s = shape_of(c, true);
     if (s.tpr == 0) return (int32_t)(rows < ANY_PARTS ? rows : ANY_PARTS);
-    // at least two rows a team, so that the partial sums stay small beside the rows, unless that leaves
-    // few workgroups
+    // at least two rows a team, so that the partial sums stay small beside the rows, unless
+    // that leaves few workgroups
     const int64_t each = blocks_for(rows, s.tpr < 512 ? 512 / s.tpr : 1, INT32_MAX), half = each / 2;
     const int64_t few = each < BWD_FEW ? each : BWD_FEW;
     return (int32_t)(half < few ? few : half < BWD_BLOCKS ? half : BWD_BLOCKS);
