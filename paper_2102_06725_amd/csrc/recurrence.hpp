@@ -16,13 +16,13 @@
 //
 // Bound by memory (8 bytes a token and channel forward, 14 backward), and close behind it by
 // the vector units: a forward element takes 37 instructions, 4 of them transcendental, which
-// alone would take half of the time.  Measured, cold: forward of 8 x 2048 x 1152 37 us (4.1
-// TB/s), backward 60 us (4.4 TB/s); forward of 2 x 32768 x 768 95 us (4.2 TB/s; the same
+// alone would take half of the time.  Measured, cold: forward of 8 x 2048 x 1152 36 us (4.2
+// TB/s), backward 59 us (4.5 TB/s); forward of 2 x 32768 x 768 93 us (4.3 TB/s; the same
 // elements as 512 sequences of 128 tokens, one chunk each, 74 us).  Short calls are bound by
 // their launches and one exchange between workgroups: 6 us for one chunk, 10 for two.
 //
 // Chunks: forward 8 waves of 16 tokens, backward 4 of 16, the most that leave two workgroups to
-// a compute unit (126 and 248 registers): what is on its way and what waits for its
+// a compute unit (123 and 254 registers): what is on its way and what waits for its
 // predecessors are then never the same.  16 waves of 8 tokens, 4 of 32 and 16 of 16 took 103,
 // 102 and 98 us where 8 of 16 take 97, chunks of half the tokens 115; backward, 8 waves of 8
 // and 16 of 4 took 65 and 66 us where 4 of 16 take 55.
