@@ -62,6 +62,7 @@ int64_t word_count(const RecParams &p, bool backward) {
 
 // Workgroups of one launch at most: work items of a launch are counted in 32 bits.
 constexpr int64_t MOST_BLOCKS = 1 << 22;
+constexpr int32_t MOST_TOKENS = 1 << 29;
 
 // The sequences from n0 on, n of them.
 RecParams some(const RecParams &p, bool backward, int64_t n0, int64_t n) {
@@ -114,8 +115,10 @@ hipError_t launch(int dtype, const RecParams &p, bool backward, hipStream_t st) 
 
 }  // namespace
 
-// One sequence's workgroups have to fit a launch.
+// One sequence's workgroups have to fit a launch, and its tokens' numbers 32 bits, also those of
+// a last workgroup's places past the end.
 bool recurrence_fits(const RecParams &p) {
+    if (p.t > MOST_TOKENS) return false;
     const RecGrid f = grid_of(p, false), b = grid_of(p, true);
     return (int64_t)f.chunks * f.cols <= MOST_BLOCKS && (int64_t)b.chunks * b.cols <= 2 * MOST_BLOCKS;
 }
