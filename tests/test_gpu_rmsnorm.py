@@ -36,6 +36,10 @@ CASES = [  # rows, c, dtype, residual, where the sum goes, elements past 16-byte
     # every team of threads with a last vector that is shared, in place, and enough rows for several a team
     (700, 771, "bf16", True, "residual", 0), (600, 1025, "f16", True, "x", 0), (300, 3001, "f16", True, "own", 1),
     (140, 7777, "bf16", True, "residual", 0), (140, 9001, "f16", True, "x", 0),
+    # rows of one to four vectors, more of them than a workgroup takes at once
+    (5003, 8, "f16", True, "residual", 1), (5003, 9, "bf16", True, "x", 0), (2111, 15, "f16", True, "own", 0),
+    (2111, 16, "bf16", True, "residual", 0), (2111, 17, "f16", True, "x", 3), (1301, 24, "bf16", True, "own", 0),
+    (1301, 31, "f16", True, "residual", 0), (1301, 32, "bf16", False, None, 0), (1301, 33, "f16", True, "own", 0),
 ]
 
 
@@ -115,7 +119,9 @@ def test_forward_and_backward(nnlib, rows, c, dtype, residual, where, shift):
 Q8 = [(r, c, dt, res, sh, g) for r, c, dt, res, sh in
       [(1, 1, "f16", True, 0), (9, 33, "bf16", True, 0), (70, 64, "f16", False, 0), (13, 100, "f16", True, 1),
        (5, 256, "bf16", True, 0), (40, 771, "bf16", True, 0), (6, 1000, "f16", True, 0), (3, 2048, "bf16", True, 0),
-       (3, 4096, "f16", True, 0), (2, 4104, "f16", True, 3), (2, 8192, "bf16", True, 0), (2, 20000, "bf16", True, 0)]
+       (3, 4096, "f16", True, 0), (2, 4104, "f16", True, 3), (2, 8192, "bf16", True, 0), (2, 20000, "bf16", True, 0),
+       (601, 8, "f16", True, 1), (601, 9, "bf16", True, 0), (601, 16, "f16", False, 0), (601, 23, "bf16", True, 0),
+       (601, 32, "f16", True, 0)]
       for g in (0, 32, 64, 128)]
 
 
