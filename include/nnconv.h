@@ -403,7 +403,8 @@ nnconv_status nnconv_rmsnorm_fwd(const nnconv_rmsnorm_desc *desc, const void *x,
  *   scale = max |y| / 448 over the row, or over each group of `group` channels
  *           (the last group of a row may be short); 0 where that is below 2^-126
  *   q     = e4m3(y / scale), to nearest even, y unrounded; 0 where scale is 0
- * so that q * scale stands for y.  q: [rows][c] bytes; scales:
+ * so that q * scale stands for y; y is in fp32, and both quotients are rounded to
+ * fp32 as a division is.  q: [rows][c] bytes; scales:
  * [rows][ceil(c / group)], or [rows].  The maximum passes over NaN; a NaN y has
  * a NaN code, and an infinite y an infinite scale and a NaN code.  Otherwise as
  * nnconv_rmsnorm_fwd; INVALID_ARG too for another group and null scales. */

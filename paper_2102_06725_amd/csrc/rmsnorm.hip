@@ -8,7 +8,7 @@
 // alignment run on the same kernels: the last vector of a row whose channels are no multiple of
 // 8 starts at channel c - 8, and the channels it shares with the one before count once.
 //
-// Measured: 16384 x 4096 with a residual to 8 bits 83 us (5.7 TB/s); 200704 x 256 forward 66 us
+// Measured: 16384 x 4096 with a residual to 8 bits 84 us (5.6 TB/s); 200704 x 256 forward 66 us
 // (6.2 TB/s), backward 65 us and 5 us for the sum of dgain's parts; 12345 x 771 (rows at every
 // alignment) 16, 17 and 4 us.
 #include <type_traits>
@@ -123,12 +123,33 @@ __device__ __forceinline__ void load_gain(const float *g, const Slot &s, float o
     }
 }
 
-__device__ __forceinline__ float scale_of(float most, float &inv) {
-    float scale = most * (1.0f / 448.0f);
-    if (scale < 0x1p-126f) scale = 0.f;
-    inv = scale > 0.f ? 1.0f / scale : 0.f;
-    return scale;
-}
+// Division by a group's scale, max |y| / 448.  y * inv is off by an ulp or two, which moves a code
+// that lies near a tie; the correction by the product's remainder makes it the fp32 quotient y / scale
+// (three instructions an element where a division takes ten).  With a tiny scale y and the scale are
+// multiplied by 2^64 first, which keeps the remainder above the smallest fp32 number.
+struct Scale {
+    float value, by, inv, up;
+    __device__ __forceinline__ explicit Scale(float most) {
+        value = most / 448.0f;
+        if (value < 0x1p-126f) value = 0.f;
+        up = value < 0x1p-64f ? 0x1p64f : 1.0f;
+        by = value * up;
+        inv = value > 0.f ? 1.0f / by : 0.f;
+        if (inv == 0.f) by = 0.f;  // no scale, or an infinite one: the quotients are 0 or NaN
+    }
+    // y[k] = y[k] / value
+    template <int N>
+    __device__ __forceinline__ void divide(float (&y)[N]) const {
+        if (up != 1.0f)
+#pragma unroll
+            for (int k = 0; k < N; ++k) y[k] *= up;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float q = y[k] * inv;
+            y[k] = __builtin_fmaf(__builtin_fmaf(-q, by, y[k]), inv, q);
+        }
+    }
+};
 
 // ---- forward -------------------------------------------------------------------------
 
@@ -222,15 +243,15 @@ __global__ __launch_bounds__(TPR <= 64 ? 256 : TPR) void rmsnorm_fwd_kernel(cons
                 const int vec = k * TPR + t;
                 const Slot s(vec, p.c);
                 if (!live || !s.in) continue;
-                float inv;
-                const float scale = scale_of(p.groups == 1 ? row_most : most[k], inv);
+                const Scale scale(p.groups == 1 ? row_most : most[k]);
                 if (p.groups == 1 ? vec == 0 : vec % wide == 0)
-                    p.scales[row * p.groups + (p.groups == 1 ? 0 : vec / wide)] = scale;
+                    p.scales[row * p.groups + (p.groups == 1 ? 0 : vec / wide)] = scale.value;
+                scale.divide(y[k]);
                 int q0 = 0, q1 = 0;
-                q0 = __builtin_amdgcn_cvt_pk_fp8_f32(y[k][0] * inv, y[k][1] * inv, q0, false);
-                q0 = __builtin_amdgcn_cvt_pk_fp8_f32(y[k][2] * inv, y[k][3] * inv, q0, true);
-                q1 = __builtin_amdgcn_cvt_pk_fp8_f32(y[k][4] * inv, y[k][5] * inv, q1, false);
-                q1 = __builtin_amdgcn_cvt_pk_fp8_f32(y[k][6] * inv, y[k][7] * inv, q1, true);
+                q0 = __builtin_amdgcn_cvt_pk_fp8_f32(y[k][0], y[k][1], q0, false);
+                q0 = __builtin_amdgcn_cvt_pk_fp8_f32(y[k][2], y[k][3], q0, true);
+                q1 = __builtin_amdgcn_cvt_pk_fp8_f32(y[k][4], y[k][5], q1, false);
+                q1 = __builtin_amdgcn_cvt_pk_fp8_f32(y[k][6], y[k][7], q1, true);
                 uint8_t *to = (uint8_t *)p.y + base + s.at;
                 if (!TAIL || s.skip == 0) {
                     *(u32x2_any *)to = u32x2{(uint32_t)q0, (uint32_t)q1};
@@ -270,25 +291,27 @@ __global__ __launch_bounds__(512) void rmsnorm_fwd_any_kernel(const NormParams p
         const float rstd = 1.0f / sqrtf(row_reduce<512>(ss, buf[0], Add()) / (float)p.c + p.eps);
         if (p.rstd && t == 0) p.rstd[row] = rstd;
         auto y = [&](int i) { return again(i) * rstd * p.gain[i]; };
-        auto put8 = [&](int i, float q) {
-            ((uint8_t *)p.y)[base + i] = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(q, q, 0, false);
+        auto put8 = [&](int i, const Scale &scale) {
+            float q[1] = {y(i)};
+            scale.divide(q);
+            ((uint8_t *)p.y)[base + i] = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[0], 0, false);
         };
         if constexpr (!Q8) {
             for (int i = t; i < p.c; i += 512) ((uint16_t *)p.y)[base + i] = (uint16_t)to16<T>(y(i));
         } else if (p.groups == 1) {
-            float most = 0.f, inv;
+            float most = 0.f;
             for (int i = t; i < p.c; i += 512) most = fmaxf(most, fabsf(y(i)));
-            const float scale = scale_of(row_reduce<512>(most, buf[1], Max()), inv);
-            if (t == 0) p.scales[row] = scale;
-            for (int i = t; i < p.c; i += 512) put8(i, y(i) * inv);
+            const Scale scale(row_reduce<512>(most, buf[1], Max()));
+            if (t == 0) p.scales[row] = scale.value;
+            for (int i = t; i < p.c; i += 512) put8(i, scale);
         } else {
             for (int g = t >> 6; g < p.groups; g += 8) {  // a wave per group
                 const int lo = g * p.group, hi = min(lo + p.group, p.c);
-                float most = 0.f, inv;
+                float most = 0.f;
                 for (int i = lo + (t & 63); i < hi; i += 64) most = fmaxf(most, fabsf(y(i)));
-                const float scale = scale_of(lanes_reduce<64>(most, Max()), inv);
-                if ((t & 63) == 0) p.scales[row * p.groups + g] = scale;
-                for (int i = lo + (t & 63); i < hi; i += 64) put8(i, y(i) * inv);
+                const Scale scale(lanes_reduce<64>(most, Max()));
+                if ((t & 63) == 0) p.scales[row * p.groups + g] = scale.value;
+                for (int i = lo + (t & 63); i < hi; i += 64) put8(i, scale);
             }
         }
     }
