@@ -447,19 +447,41 @@ def _ptr(t):
 
 
 class _Workspaces:
-    """Workspaces of a handle, one per stream and kind, so that calls on several streams
-    do not share one.  A torch tensor each, allocated on first use."""
+    """Workspaces of a handle, torch tensors that are allocated on first use.
+
+    Each device, stream and kind has its own, so that calls on several streams do not share one,
+    and each call that torch captures into a graph has one of the graph's memory, so that graphs
+    of a handle may be replayed beside each other and beside its calls.  A workspace that became
+    too small is kept until the handle goes: a graph that the caller captured by other means may
+    hold its address."""
 
     def __init__(self):
         self._held = {}
+        self._kept = []
 
     def get(self, kind, stream, nbytes, device):
-        t = self._held.get((kind, stream))
+        import torch
+        if device.type == "cuda" and torch.cuda.is_current_stream_capturing():
+            return self._new(nbytes, stream, device)
+        t = self._held.get((kind, stream, device))
         if t is None or t.numel() < nbytes:
-            import torch
-            t = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=device)
-            self._held[kind, stream] = t
+            if t is not None:  # doubled, so that all that is kept is no more than what is in use
+                self._kept.append(t)
+                nbytes = max(nbytes, 2 * t.numel())
+            t = self._held[kind, stream, device] = self._new(nbytes, stream, device)
         return t
+
+    @staticmethod
+    def _new(nbytes, stream, device):
+        """Memory that is free on `stream`: another stream's may still be in use there, and
+        torch hands it on in the order of the stream that it was allocated on."""
+        import torch
+        nbytes = max(nbytes, 1)
+        if device.type != "cuda" or stream == current_stream():
+            return torch.empty(nbytes, dtype=torch.uint8, device=device)
+        s = torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
+        with torch.cuda.stream(s):
+            return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
 class RMSNorm:
