@@ -484,14 +484,65 @@ class _Workspaces:
             return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
-class RMSNorm:
+def _all_dense(tensors, dtype, count, gpu):
+    """Whether the tensors, Nones aside, are dense ones of `count` elements on the device."""
+    for t in tensors:
+        if t is not None and not (t.dtype is dtype and t.numel() == count and t.is_contiguous() and t.get_device() == gpu):
+            return False
+    return True
+
+
+class _Handle:
+    """The checks that the handles below share: torch tensors of another type, size, layout or
+    device than the call's are refused, since it would read or write past their end.  Other
+    objects with data_ptr() are taken as they are.
+
+    A call looks its tensors over in one expression (a third of a microsecond each); only where
+    that fails are they looked at one by one, for the name of the one to refuse."""
+
+    def __init__(self, desc):
+        import torch
+        self.desc, self._lib, self._ref = desc, load(), ctypes.byref(desc)
+        self._tensor, self._f32, self._i32 = torch.Tensor, torch.float32, torch.int32
+        self._dtype = {NNCONV_F16: torch.float16, NNCONV_BF16: torch.bfloat16, NNCONV_F32: torch.float32}.get(desc.dtype)
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self._get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+    def _gpu(self, name, t):
+        """The device that a call's tensors have to be on."""
+        if isinstance(t, self._tensor):
+            return t.get_device()
+        if t is None:
+            raise ValueError("%s: %s is needed" % (type(self).__name__, name))
+        return self._get_device()
+
+    def _stream(self, stream, gpu):
+        if gpu < 0 or gpu != self._get_device():
+            raise ValueError("%s: the tensors are not on the current device" % type(self).__name__)
+        if stream is not None:
+            return stream
+        return current_stream() if self._raw_stream is None else self._raw_stream(gpu)
+
+    def _refuse(self, name, t, want):
+        raise ValueError("%s: %s: %s with strides %s of %s on %s, where %s are expected" % (
+            type(self).__name__, name, tuple(t.shape), t.stride(), t.dtype, t.device, want))
+
+    def _dense(self, dtype, count, gpu, more=False, **tensors):
+        """One by one: dense, of `count` elements (or more)."""
+        for name, t in tensors.items():
+            if isinstance(t, self._tensor) and not (
+                    t.dtype is dtype and t.is_contiguous() and t.get_device() == gpu
+                    and (t.numel() == count or more and t.numel() > count)):
+                self._refuse(name, t, "%d%s dense elements of %s on device %d" % (count, " or more" if more else "", dtype, gpu))
+
+
+class RMSNorm(_Handle):
     """Root-mean-square norm of [rows][c] torch tensors (dense, on the current device), with
     the residual's addition: nnconv_rmsnorm_*.  `rows` may be changed between calls (a serving
-    program's batch)."""
+    program's batch).  Tensors that do not fit are refused with a ValueError."""
 
     def __init__(self, rows, c, dtype=NNCONV_F16, eps=1e-6, group=0):
-        self.desc = nnconv_rmsnorm_desc(rows, c, dtype, group, eps)
-        self._lib, self._ref = load(), ctypes.byref(self.desc)
+        super().__init__(nnconv_rmsnorm_desc(rows, c, dtype, group, eps))
         self._ws = _Workspaces()
         self._nbytes = None
 
@@ -504,20 +555,51 @@ class RMSNorm:
         self.desc.rows = rows
         self._nbytes = None
 
+    def _fits(self, rows, c, gpu, wide, channels, each):
+        """Whether tensors of [rows][c], of c and of rows elements are these."""
+        try:
+            return (_all_dense(wide, self._dtype, rows * c, gpu) and _all_dense(channels, self._f32, c, gpu)
+                    and _all_dense(each, self._f32, rows, gpu))
+        except AttributeError:  # an object that is no tensor
+            return False
+
     def fwd(self, x, gain, y, residual=None, sum=None, rstd=None, stream=None):
+        rows, c, gpu = self.desc.rows, self.desc.c, self._gpu("x", x)
+        if not self._fits(rows, c, gpu, (x, residual, sum, y), (gain,), (rstd,)):
+            self._dense(self._dtype, rows * c, gpu, x=x, residual=residual, sum=sum, y=y)
+            self._dense(self._f32, c, gpu, gain=gain)
+            self._dense(self._f32, rows, gpu, rstd=rstd)
         check(self._lib.nnconv_rmsnorm_fwd(
-            self._ref, x.data_ptr(), _ptr(residual), gain.data_ptr(), _ptr(sum), y.data_ptr(),
-            _ptr(rstd), current_stream() if stream is None else stream), "nnconv_rmsnorm_fwd")
+            self._ref, x.data_ptr(), None if residual is None else residual.data_ptr(), _ptr(gain),
+            None if sum is None else sum.data_ptr(), _ptr(y), None if rstd is None else rstd.data_ptr(),
+            self._stream(stream, gpu)), "nnconv_rmsnorm_fwd")
 
     def fwd_q8(self, x, gain, q, scales, residual=None, sum=None, rstd=None, stream=None):
+        """q: torch.float8_e4m3fn or uint8."""
+        import torch
+        rows, c, gpu = self.desc.rows, self.desc.c, self._gpu("x", x)
+        if not self._fits(rows, c, gpu, (x, residual, sum), (gain,), (rstd,)):
+            self._dense(self._dtype, rows * c, gpu, x=x, residual=residual, sum=sum)
+            self._dense(self._f32, c, gpu, gain=gain)
+            self._dense(self._f32, rows, gpu, rstd=rstd)
+        q8 = torch.uint8 if getattr(q, "dtype", None) is torch.uint8 else torch.float8_e4m3fn
+        self._dense(q8, rows * c, gpu, q=q)
+        groups = -(-c // self.desc.group) if self.desc.group > 0 else 1
+        self._dense(self._f32, rows * groups, gpu, scales=scales)
         check(self._lib.nnconv_rmsnorm_fwd_q8(
-            self._ref, x.data_ptr(), _ptr(residual), gain.data_ptr(), _ptr(sum), q.data_ptr(),
-            scales.data_ptr(), _ptr(rstd), current_stream() if stream is None else stream),
-            "nnconv_rmsnorm_fwd_q8")
+            self._ref, x.data_ptr(), _ptr(residual), _ptr(gain), _ptr(sum), _ptr(q), _ptr(scales), _ptr(rstd),
+            self._stream(stream, gpu)), "nnconv_rmsnorm_fwd_q8")
 
     def bwd(self, sum, dy, gain, rstd, dx, dgain=None, dsum=None, inv_loss_scale=1.0,
             accumulate=0, overflow_flag=None, stream=None):
-        stream = current_stream() if stream is None else stream
+        rows, c, gpu = self.desc.rows, self.desc.c, self._gpu("sum", sum)
+        if not self._fits(rows, c, gpu, (sum, dy, dsum, dx), (gain, dgain), (rstd,)):
+            self._dense(self._dtype, rows * c, gpu, sum=sum, dy=dy, dsum=dsum, dx=dx)
+            self._dense(self._f32, c, gpu, gain=gain, dgain=dgain)
+            self._dense(self._f32, rows, gpu, rstd=rstd)
+        if overflow_flag is not None:
+            self._dense(self._i32, 1, gpu, more=True, overflow_flag=overflow_flag)
+        stream = self._stream(stream, gpu)
         ws, nb = None, 0
         if dgain is not None:
             if self._nbytes is None:
@@ -526,21 +608,20 @@ class RMSNorm:
             nb = self._nbytes
             ws = self._ws.get("bwd", stream, nb, sum.device)
         check(self._lib.nnconv_rmsnorm_bwd(
-            self._ref, sum.data_ptr(), dy.data_ptr(), _ptr(dsum), gain.data_ptr(), rstd.data_ptr(),
-            dx.data_ptr(), _ptr(dgain), inv_loss_scale, accumulate, _ptr(overflow_flag), _ptr(ws),
-            nb, stream), "nnconv_rmsnorm_bwd")
+            self._ref, sum.data_ptr(), _ptr(dy), _ptr(dsum), _ptr(gain), _ptr(rstd), _ptr(dx), _ptr(dgain),
+            inv_loss_scale, accumulate, _ptr(overflow_flag), _ptr(ws), nb, stream), "nnconv_rmsnorm_bwd")
 
 
-class GatedRecurrence:
+class GatedRecurrence(_Handle):
     """Gated linear recurrence over n sequences of t tokens with c channels:
     nnconv_recurrence_*.  ld and ldy: elements between the tokens of x, f, g (3 * c for the
     thirds of one projection's output, passed as views) and of y.  `n` and `t` may be changed
-    between calls."""
+    between calls.  Tensors that do not fit are refused with a ValueError: x, f, g, y and their
+    gradients may have any shape that ends in c and whose strides are those of n * t tokens."""
 
     def __init__(self, n, t, c, ld=None, ldy=None, dtype=NNCONV_F16):
-        self.desc = nnconv_recurrence_desc(n, t, c, dtype, c if ld is None else ld,
-                                           c if ldy is None else ldy)
-        self._lib, self._ref = load(), ctypes.byref(self.desc)
+        super().__init__(nnconv_recurrence_desc(n, t, c, dtype, c if ld is None else ld,
+                                                c if ldy is None else ldy))
         self._ws = _Workspaces()
         self._sizes = {}  # pass -> workspace bytes of the present n and t
 
@@ -569,30 +650,100 @@ class GatedRecurrence:
         check(st, "nnconv_recurrence_saved_size")
         return torch.empty(max(nb // 4, 1), dtype=torch.float32, device=device)
 
-    def _workspace(self, pass_, stream, device):
+    def _workspace(self, pass_, stream, x):
         nb = self._sizes.get(pass_)
         if nb is None:
             st, nb = nnconv_recurrence_workspace_size(self.desc, pass_)
             check(st, "nnconv_recurrence_workspace_size")
             self._sizes[pass_] = nb
-        return (None, 0) if nb == 0 else (self._ws.get(pass_, stream, nb, device).data_ptr(), nb)
+        return (None if nb == 0 else self._ws.get(pass_, stream, nb, x.device)), nb
+
+    def _fits(self, gpu, inputs, outputs, dense):
+        """Whether tensors of tokens ld and ldy elements apart, and dense ones of (type, elements), are these."""
+        d, dtype = self.desc, self._dtype
+        n, t, c = d.n, d.t, d.c
+        try:
+            for tensors, ld in ((inputs, d.ld), (outputs, d.ldy)):
+                # as most calls have them: [n][t][c] and [n * t][c]
+                shape, strides = ((n, t, c), (t * ld, ld, 1)) if tensors[0].dim() == 3 else ((n * t, c), (ld, 1))
+                for v in tensors:
+                    if v is not None and not (v.dtype is dtype and v.shape == shape and v.stride() == strides
+                                              and v.get_device() == gpu):
+                        return False
+            for kind, count, tensors in dense:
+                if not _all_dense(tensors, kind, count, gpu):
+                    return False
+            return True
+        except AttributeError:  # an object that is no tensor
+            return False
+
+    def _tokens(self, ld, gpu, **tensors):
+        """One by one: any shape that ends in c, with the strides of tokens ld elements apart."""
+        d = self.desc
+        for name, t in tensors.items():
+            if isinstance(t, self._tensor) and not (
+                    t.dtype is self._dtype and t.get_device() == gpu and self._laid_out(t, ld)):
+                self._refuse(name, t, "%d * %d tokens of %d channels, %d elements apart, of %s on device %d" % (
+                    d.n, d.t, d.c, ld, self._dtype, gpu))
+
+    def _laid_out(self, t, ld):
+        d, shape, strides = self.desc, t.shape, t.stride()
+        if len(shape) == 0 or shape[-1] != d.c or t.numel() != d.n * d.t * d.c:
+            return False
+        if t.numel() == 0:
+            return True
+        if d.c > 1 and strides[-1] != 1:
+            return False
+        for size, stride in zip(shape[-2::-1], strides[-2::-1]):
+            if size > 1 and stride != ld:
+                return False
+            ld *= size
+        return True
+
+    def _saved_count(self):
+        d = self.desc
+        return d.n * -(-d.t // NNCONV_RECURRENCE_SAVE) * d.c
 
     def fwd(self, x, f, bias, y, g=None, lengths=None, h0=None, ht=None, saved=None, stream=None):
-        stream = current_stream() if stream is None else stream
-        ws, nb = self._workspace(NNCONV_FWD, stream, x.device)
+        d, f32, gpu = self.desc, self._f32, self._gpu("x", x)
+        n, c = d.n, d.c
+        if not self._fits(gpu, (x, f, g), (y,), ((f32, c, (bias,)), (f32, n * c, (h0, ht)), (self._i32, n, (lengths,)))):
+            self._tokens(d.ld, gpu, x=x, f=f, g=g)
+            self._tokens(d.ldy, gpu, y=y)
+            self._dense(f32, c, gpu, bias=bias)
+            self._dense(f32, n * c, gpu, h0=h0, ht=ht)
+            self._dense(self._i32, n, gpu, lengths=lengths)
+        if saved is not None:
+            self._dense(f32, self._saved_count(), gpu, more=True, saved=saved)
+        stream = self._stream(stream, gpu)
+        ws, nb = self._workspace(NNCONV_FWD, stream, x)
         check(self._lib.nnconv_recurrence_fwd(
-            self._ref, x.data_ptr(), f.data_ptr(), _ptr(bias), _ptr(g), _ptr(lengths), _ptr(h0),
-            y.data_ptr(), _ptr(ht), _ptr(saved), ws, nb, stream), "nnconv_recurrence_fwd")
+            self._ref, x.data_ptr(), _ptr(f), None if bias is None else bias.data_ptr(),
+            None if g is None else g.data_ptr(), None if lengths is None else lengths.data_ptr(),
+            None if h0 is None else h0.data_ptr(), _ptr(y), None if ht is None else ht.data_ptr(),
+            None if saved is None else saved.data_ptr(), None if ws is None else ws.data_ptr(), nb, stream),
+            "nnconv_recurrence_fwd")
 
     def bwd(self, x, f, bias, saved, dy, dx, df, g=None, dg=None, lengths=None, dht=None, dh0=None,
             dbias=None, inv_loss_scale=1.0, accumulate=0, overflow_flag=None, stream=None):
-        stream = current_stream() if stream is None else stream
-        ws, nb = self._workspace(NNCONV_DGRAD, stream, x.device)
+        d, f32, gpu = self.desc, self._f32, self._gpu("x", x)
+        n, c = d.n, d.c
+        if not self._fits(gpu, (x, f, g, dx, df, dg), (dy,),
+                          ((f32, c, (bias, dbias)), (f32, n * c, (dht, dh0)), (self._i32, n, (lengths,)))):
+            self._tokens(d.ld, gpu, x=x, f=f, g=g, dx=dx, df=df, dg=dg)
+            self._tokens(d.ldy, gpu, dy=dy)
+            self._dense(f32, c, gpu, bias=bias, dbias=dbias)
+            self._dense(f32, n * c, gpu, dht=dht, dh0=dh0)
+            self._dense(self._i32, n, gpu, lengths=lengths)
+        self._dense(f32, self._saved_count(), gpu, more=True, saved=saved)
+        if overflow_flag is not None:
+            self._dense(self._i32, 1, gpu, more=True, overflow_flag=overflow_flag)
+        stream = self._stream(stream, gpu)
+        ws, nb = self._workspace(NNCONV_DGRAD, stream, x)
         check(self._lib.nnconv_recurrence_bwd(
-            self._ref, x.data_ptr(), f.data_ptr(), _ptr(bias), _ptr(g), _ptr(lengths),
-            saved.data_ptr(), dy.data_ptr(), _ptr(dht), dx.data_ptr(), df.data_ptr(), _ptr(dg),
-            _ptr(dh0), _ptr(dbias), inv_loss_scale, accumulate, _ptr(overflow_flag), ws, nb,
-            stream), "nnconv_recurrence_bwd")
+            self._ref, x.data_ptr(), _ptr(f), _ptr(bias), _ptr(g), _ptr(lengths), _ptr(saved), _ptr(dy),
+            _ptr(dht), _ptr(dx), _ptr(df), _ptr(dg), _ptr(dh0), _ptr(dbias), inv_loss_scale, accumulate,
+            _ptr(overflow_flag), _ptr(ws), nb, stream), "nnconv_recurrence_bwd")
 
 
 class AdamW:
