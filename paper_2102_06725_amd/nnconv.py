@@ -500,11 +500,11 @@ class _Handle:
     A call looks its tensors over in one expression (a third of a microsecond each); only where
     that fails are they looked at one by one, for the name of the one to refuse."""
 
-    def __init__(self, desc):
+    def __init__(self, desc, dtype=None):
         import torch
         self.desc, self._lib, self._ref = desc, load(), ctypes.byref(desc)
         self._tensor, self._f32, self._i32 = torch.Tensor, torch.float32, torch.int32
-        self._dtype = {NNCONV_F16: torch.float16, NNCONV_BF16: torch.bfloat16, NNCONV_F32: torch.float32}.get(desc.dtype)
+        self._dtype = {NNCONV_F16: torch.float16, NNCONV_BF16: torch.bfloat16, NNCONV_F32: torch.float32}.get(dtype)
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         self._get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
@@ -542,7 +542,7 @@ class RMSNorm(_Handle):
     program's batch).  Tensors that do not fit are refused with a ValueError."""
 
     def __init__(self, rows, c, dtype=NNCONV_F16, eps=1e-6, group=0):
-        super().__init__(nnconv_rmsnorm_desc(rows, c, dtype, group, eps))
+        super().__init__(nnconv_rmsnorm_desc(rows, c, dtype, group, eps), dtype)
         self._ws = _Workspaces()
         self._nbytes = None
 
@@ -621,7 +621,7 @@ class GatedRecurrence(_Handle):
 
     def __init__(self, n, t, c, ld=None, ldy=None, dtype=NNCONV_F16):
         super().__init__(nnconv_recurrence_desc(n, t, c, dtype, c if ld is None else ld,
-                                                c if ldy is None else ldy))
+                                                c if ldy is None else ldy), dtype)
         self._ws = _Workspaces()
         self._sizes = {}  # pass -> workspace bytes of the present n and t
 
@@ -746,28 +746,37 @@ class GatedRecurrence(_Handle):
             _ptr(overflow_flag), _ptr(ws), nb, stream), "nnconv_recurrence_bwd")
 
 
-class AdamW:
+class AdamW(_Handle):
     """AdamW over a list of tensors: nnconv_adamw_*.
 
     Each entry of `tensors` is a dict with master, grad, m, v (and w16; m_scale and v_scale with
-    8-bit moments) as dense torch tensors on one device, and weight_decay.  Moments in 8 bits are
-    torch.float8_e4m3fn (m) and torch.float8_e5m2 (v), or uint8, with a byte of scale for every
-    NNCONV_ADAMW_BLOCK elements.  The tensors are kept: the list holds their addresses."""
+    8-bit moments) as dense torch tensors on the current device, and weight_decay.  Moments in 8
+    bits are torch.float8_e4m3fn (m) and torch.float8_e5m2 (v), or uint8, with a byte of scale for
+    every NNCONV_ADAMW_BLOCK elements.
+
+    The plan holds the tensors' addresses, and the handle keeps the tensors: every step reads the
+    gradients from the tensors that are in the list, so a backward pass has to write them there
+    (a gradient tensor that is replaced, or set to None and made anew, is not seen).  Making the
+    plan queues kernels and waits for them."""
 
     def __init__(self, tensors, seed=0):
         import torch
+        super().__init__(nnconv_adamw_plan())
         codes = {torch.float32: NNCONV_F32, torch.float16: NNCONV_F16, torch.bfloat16: NNCONV_BF16}
         self.tensors, self.seed = list(tensors), seed
         n = len(self.tensors)
         arr = (nnconv_adamw_tensor * max(n, 1))()
         fp32, scale = {torch.float32}, {torch.uint8, torch.float8_e8m0fnu}
         m8, v8 = {torch.float8_e4m3fn, torch.uint8}, {torch.float8_e5m2, torch.uint8}
+        gpu = self.tensors[0]["master"].get_device() if n else self._get_device()
 
         def address(key, v, size, types):
             if v.numel() != size or not v.is_contiguous():
                 raise ValueError("AdamW: %s has another size than the master, or is not dense" % key)
             if v.dtype not in types:
                 raise ValueError("AdamW: %s has type %s" % (key, v.dtype))
+            if v.get_device() != gpu:
+                raise ValueError("AdamW: %s is on %s, the first master on device %d" % (key, v.device, gpu))
             return v.data_ptr()
 
         for a, t in zip(arr, self.tensors):
@@ -784,17 +793,21 @@ class AdamW:
                 a.m_scale, a.v_scale = (address(k, t[k], blocks, scale) for k in ("m_scale", "v_scale"))
             a.count, a.weight_decay = count, t.get("weight_decay", 0.0)
             a.grad_dtype, a.state_dtype = codes.get(grad.dtype, -1), NNCONV_F8 if f8 else NNCONV_F32
+        stream = self._stream(None, gpu)
         st, nb = nnconv_adamw_plan_size(arr, n)
         check(st, "nnconv_adamw_plan_size")
-        device = self.tensors[0]["master"].device if n else "cuda"
-        self._table = torch.empty(max(nb, 1), dtype=torch.uint8, device=device)
-        self.plan = nnconv_adamw_plan()
-        check(nnconv_adamw_plan_init(arr, n, self._table.data_ptr(), nb, self.plan,
-                                     current_stream()), "nnconv_adamw_plan_init")
+        self._table = torch.empty(max(nb, 1), dtype=torch.uint8, device=torch.device("cuda", gpu))
+        self.plan, self._device = self.desc, gpu
+        check(nnconv_adamw_plan_init(arr, n, self._table.data_ptr(), nb, self.plan, stream), "nnconv_adamw_plan_init")
         torch.cuda.current_stream().synchronize()  # the plan is there for steps on any stream
 
     def step(self, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, state=None, overflow_flag=None,
              stream=None):
-        check(nnconv_adamw_update(self.plan, step.data_ptr(), lr, beta1, beta2, eps, self.seed,
-                                  _ptr(state), _ptr(overflow_flag), Conv2d._stream(stream)),
-              "nnconv_adamw_update")
+        """step, overflow_flag: int32 tensors of one element; state: the loss scaler's."""
+        gpu = self._device
+        self._dense(self._i32, 1, gpu, more=True, step=step, overflow_flag=overflow_flag)
+        if isinstance(state, self._tensor) and not (
+                state.nbytes >= ctypes.sizeof(nnconv_loss_scaler) and state.is_contiguous() and state.get_device() == gpu):
+            self._refuse("state", state, "the loss scaler's %d bytes on device %d" % (ctypes.sizeof(nnconv_loss_scaler), gpu))
+        check(nnconv_adamw_update(self.plan, _ptr(step), lr, beta1, beta2, eps, self.seed, _ptr(state),
+                                  _ptr(overflow_flag), self._stream(stream, gpu)), "nnconv_adamw_update")
