@@ -378,7 +378,7 @@ void launch_recurrence_bwd_short(int dtype, const RecParams &p, hipStream_t st) 
 
 void launch_recurrence_bwd_single(int dtype, const RecParams &p, hipStream_t st) {
     with_kind(dtype, true, [&](auto t, auto) {
-        hipLaunchKernelGGL((recurrence_bwd_single_kernel<decltype(t)>), dim3((p.n + 63) / 64), dim3(64), 0, st, p);
+        hipLaunchKernelGGL((recurrence_bwd_single_kernel<decltype(t)>), dim3((uint32_t)(((int64_t)p.n + 63) / 64)), dim3(64), 0, st, p);
     });
 }
 

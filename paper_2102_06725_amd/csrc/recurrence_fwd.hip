@@ -265,7 +265,7 @@ void launch_recurrence_fwd_short(int dtype, const RecParams &p, hipStream_t st) 
 
 void launch_recurrence_fwd_single(int dtype, const RecParams &p, hipStream_t st) {
     with_kind(dtype, true, [&](auto t, auto) {
-        hipLaunchKernelGGL((recurrence_fwd_single_kernel<decltype(t)>), dim3((p.n + 63) / 64), dim3(64), 0, st, p);
+        hipLaunchKernelGGL((recurrence_fwd_single_kernel<decltype(t)>), dim3((uint32_t)(((int64_t)p.n + 63) / 64)), dim3(64), 0, st, p);
     });
 }
 
