@@ -4,6 +4,10 @@
 
 Compiles every ``csrc/*.hip`` file to an object under ``_build/`` in
 parallel and links them into ``paper_2102_06725_amd/libnnconv.so``.
+
+``libnnconv_recompute.so`` is the same library for tests, with recurrence
+kernels whose workgroups do not wait for each other's words and compute all
+of them again instead: the path that a wait takes when it gives up.
 """
 from __future__ import annotations
 
@@ -19,6 +23,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libnnconv.so")
+RECOMPUTE_LIB = os.path.join(PKG, "libnnconv_recompute.so")
+RECOMPUTE = {"recurrence_fwd.hip": ["-DNNCONV_RECURRENCE_LOOKS=0"], "recurrence_bwd.hip": ["-DNNCONV_RECURRENCE_LOOKS=0"]}
 ARCH = "gfx950"
 
 CXXFLAGS = [
@@ -42,19 +48,31 @@ def sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.hip")))
 
 
+def link(objs, lib) -> None:
+    tmp = lib + ".tmp%d" % os.getpid()
+    subprocess.run([hipcc(), "--offload-arch=" + ARCH, "-shared", "-fPIC", "-o", tmp] + objs, check=True)
+    os.replace(tmp, lib)
+
+
 def build(verbose: bool = False) -> str:
     """Compile and link; always rebuilds.  Returns the library path."""
     cc = hipcc()
     os.makedirs(BUILD, exist_ok=True)
     procs = []
-    objs = []
-    for src in sources():
-        obj = os.path.join(BUILD, os.path.basename(src)[:-4] + ".o")
-        objs.append(obj)
-        cmd = [cc] + CXXFLAGS + ["-c", src, "-o", obj]
+    objs, again = [], []
+
+    def compile_to(src, name, flags):
+        obj = os.path.join(BUILD, name + ".o")
+        cmd = [cc] + CXXFLAGS + flags + ["-c", src, "-o", obj]
         if verbose:
             print(" ".join(cmd), flush=True)
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
+        return obj
+
+    for src in sources():
+        base = os.path.basename(src)
+        objs.append(compile_to(src, base[:-4], []))
+        again.append(compile_to(src, base[:-4] + "_recompute", RECOMPUTE[base]) if base in RECOMPUTE else objs[-1])
     failed = []
     for src, p in procs:
         out, _ = p.communicate()
@@ -67,10 +85,8 @@ def build(verbose: bool = False) -> str:
     if failed:
         msg = "\n".join("%s:\n%s" % (s, t) for s, t in failed)
         raise RuntimeError("libnnconv build failed:\n" + msg)
-    tmp = LIB + ".tmp%d" % os.getpid()
-    cmd = [cc, "--offload-arch=" + ARCH, "-shared", "-fPIC", "-o", tmp] + objs
-    subprocess.run(cmd, check=True)
-    os.replace(tmp, LIB)
+    link(objs, LIB)
+    link(again, RECOMPUTE_LIB)
     return LIB
 
 

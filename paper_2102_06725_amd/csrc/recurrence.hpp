@@ -209,7 +209,13 @@ struct Team {
 // depend on which workgroup came first.
 constexpr int GROUP = 32;  // places of a group at most
 constexpr int ROUND = 16;  // rows of words that a workgroup has on their way at once
-constexpr int POLLS = 4096;
+// Looks at a word that is not there before it is computed.  0 (a build for tests): no word is ever
+// looked at but the first group's state, which is there before the call, so that every pair and
+// state is computed again.
+#ifndef NNCONV_RECURRENCE_LOOKS
+#define NNCONV_RECURRENCE_LOOKS 4096
+#endif
+constexpr int POLLS = NNCONV_RECURRENCE_LOOKS;
 
 __device__ __forceinline__ uint64_t word(float a, float h) {
     return (uint64_t)__builtin_bit_cast(uint32_t, a) |
@@ -234,12 +240,12 @@ struct Words {
     }
 
     // Whether the whole wave has its words.
-    __device__ __forceinline__ bool there() const { return !__any(v0 == NO_WORD || v1 == NO_WORD); }
+    __device__ __forceinline__ bool there() const { return POLLS > 0 && !__any(v0 == NO_WORD || v1 == NO_WORD); }
 
     // Looks again until they are there, POLLS times at most.
     __device__ __forceinline__ bool wait(const uint64_t *row, const Lane &L) {
         for (int k = 0; !there(); ++k) {
-            if (k == POLLS) return false;
+            if (k >= POLLS) return false;
             __builtin_amdgcn_s_sleep(1);
             load(row, L);
         }
