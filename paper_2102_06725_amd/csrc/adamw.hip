@@ -114,7 +114,7 @@ __device__ __forceinline__ float max16(float v) {
 }
 
 struct Step {
-    float inv_scale, beta1, beta2, rest1, rest2, rate, c2, eps, lr;
+    float inv_scale, beta1, beta2, rest1, rest2, rate, root, eps, lr;
     uint32_t key;  // of the hash, without the tensor
 };
 
@@ -123,8 +123,11 @@ __device__ __forceinline__ void adamw_one(const Step &k, float decay, float g, f
     g *= k.inv_scale;
     m = k.beta1 * m + k.rest1 * g;
     v = k.beta2 * v + (k.rest2 * g) * g;
-    // instructions of one unit in the last place are enough for the change
-    w -= k.rate * m * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v * k.c2) + k.eps) + decay * w;
+    // instructions of one unit in the last place are enough for the change; the root's takes a
+    // subnormal number for 0, and v / (1 - beta2^t) may pass the range that its root is far from
+    const bool small = v < 0x1p-96f;
+    const float root = __builtin_amdgcn_sqrtf(small ? v * 0x1p64f : v) * (small ? k.root * 0x1p-32f : k.root);
+    w -= k.rate * m * __builtin_amdgcn_rcpf(root + k.eps) + decay * w;
     asm volatile("" : "+v"(w));  // the 16-bit copy is the rounding of the stored master
 }
 
@@ -279,7 +282,7 @@ struct Lanes {
                     const uint32_t bits = dither_bits(key, (uint32_t)c.first + at + e);
                     const float um = __builtin_fmaf((float)(bits & 0xFFFFu), 0x1p-16f, 0x1p-17f);
                     const float uv = __builtin_fmaf((float)(bits >> 16), 0x1p-16f, 0x1p-17f);
-qm[e] = copysignf(round_random<-6, 3, false>(fabsf(mk[e]), km, um), mk[e]);
+                    qm[e] = copysignf(round_random<-6, 3, false>(fabsf(mk[e]), km, um), mk[e]);
                     qv[e] = round_random<-14, 2, true>(vk[e], kv, uv);
                 }
                 int cm = __builtin_amdgcn_cvt_pk_fp8_f32(qm[0], qm[1], 0, false);
@@ -340,7 +343,7 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(const AdamwTable tab, in
         s.rest1 = 1.0f - beta1;
         s.rest2 = 1.0f - beta2;
         s.rate = (float)(lr / (1.0 - power(beta1, now)));
-        s.c2 = (float)(1.0 / (1.0 - power(beta2, now)));
+        s.root = (float)(1.0 / sqrt(1.0 - power(beta2, now)));
         s.eps = eps;
         s.lr = lr;
         s.key = (uint32_t)now * 0xB5297A4Du + seed * 0x68E31DA4u;
