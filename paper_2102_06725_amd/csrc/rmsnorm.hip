@@ -123,19 +123,25 @@ __device__ __forceinline__ void load_gain(const float *g, const Slot &s, float o
     }
 }
 
-// Division by a group's scale, max |y| / 448.  y * inv is off by an ulp or two, which moves a code
-// that lies near a tie; the correction by the product's remainder makes it the fp32 quotient y / scale
-// (three instructions an element where a division takes ten).  With a tiny scale y and the scale are
-// multiplied by 2^64 first, which keeps the remainder above the smallest fp32 number.
+// Division by a group's scale, max |y| / 448.  A product with a rounded reciprocal is off by an ulp
+// or two, which moves a code that lies near a tie; corrected by the product's remainder it is the
+// fp32 quotient (three instructions where a division takes ten; 0.7 % of the time at 16384 x 4096, 3 %
+// with divisions for the scale and its reciprocal).  The numbers of a tiny group are multiplied
+// by 2^64 first, which keeps remainders above the smallest fp32 number.
 struct Scale {
     float value, by, inv, up;
     __device__ __forceinline__ explicit Scale(float most) {
-        value = most / 448.0f;
+        constexpr float part = 1.0f / 448.0f;
+        up = most < 0x1p-55f ? 0x1p64f : 1.0f;
+        const float m = most * up;
+        by = m * part;
+        by = __builtin_fmaf(__builtin_fmaf(-by, 448.0f, m), part, by);
+        value = up == 1.0f ? by : by * 0x1p-64f;
+        if (__builtin_isinf(most)) value = most;
         if (value < 0x1p-126f) value = 0.f;
-        up = value < 0x1p-64f ? 0x1p64f : 1.0f;
-        by = value * up;
-        inv = value > 0.f ? 1.0f / by : 0.f;
-        if (inv == 0.f) by = 0.f;  // no scale, or an infinite one: the quotients are 0 or NaN
+        inv = __builtin_amdgcn_rcpf(by);
+        inv = __builtin_fmaf(__builtin_fmaf(-by, inv, 1.0f), inv, inv);
+        if (value == 0.f || __builtin_isinf(value)) by = inv = 0.f;  // the quotients are 0 or NaN
     }
     // y[k] = y[k] / value
     template <int N>
