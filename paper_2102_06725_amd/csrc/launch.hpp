@@ -420,6 +420,9 @@ hipError_t launch_sgd_update(int64_t count, float *master, float *mom, void *w16
 
 // --- operators of a gated sequence block ------------------------------------
 
+// Channels of the norm and the recurrence at most, so that counts of them stay in 32 bits.
+constexpr int32_t MOST_CHANNELS = 1 << 28;
+
 // Root-mean-square norm of dense rows [rows][c].
 struct NormParams {
     int64_t rows;
@@ -473,9 +476,6 @@ hipError_t launch_recurrence_fwd(int dtype, const RecParams &p, hipStream_t st);
 hipError_t launch_recurrence_bwd(int dtype, const RecParams &p, hipStream_t st);
 
 // AdamW over a list of tensors, cut into chunks of ADAMW_CHUNK elements.
-// Channels of the operators of this section at most, so that counts of them stay in 32 bits.
-constexpr int32_t MOST_CHANNELS = 1 << 28;
-
 constexpr int64_t ADAMW_CHUNK = 2048;
 constexpr int ADAMW_LINE = 32;       // words from a counter to the next: a cache line
 constexpr size_t ADAMW_HEAD = 4096;  // bytes of counters in front of the chunks

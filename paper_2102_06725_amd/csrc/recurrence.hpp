@@ -22,8 +22,10 @@
 // their launches and one exchange between workgroups: 6 us for one chunk, 10 for two.
 //
 // Chunks: forward 8 waves of 16 tokens, backward 4 of 16, the most that leave two workgroups to
-// a compute unit (123 and 254 registers): what is on its way and what waits for its
-// predecessors are then never the same.  16 waves of 8 tokens, 4 of 32 and 16 of 16 took 103,
+// a compute unit: what is on its way and what waits for its predecessors are then never the
+// same.  With one team a wave the kernels take 123 and 253 registers; with several, whose
+// addresses are a lane's own, all 128 and 256, and 7 to 10 (forward) and 2 (backward, from four
+// teams on) are kept in memory.  16 waves of 8 tokens, 4 of 32 and 16 of 16 took 103,
 // 102 and 98 us where 8 of 16 take 97, chunks of half the tokens 115; backward, 8 waves of 8
 // and 16 of 4 took 65 and 66 us where 4 of 16 take 55.
 #pragma once
@@ -71,9 +73,12 @@ typedef uint32_t __attribute__((aligned(2))) u32_any;  // 4-byte access at any e
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float Z_MAX = 80.f * LOG2E;
 
-// The gate a = sigma(z) and b = 1 - a = sigma(-z), each to full relative precision: with a near
-// 1 the difference 1 - a would keep few bits of the long memories' rates.  bias is the negated
-// bias times log2(e): -z log2(e) is one multiply-add.  The limits let a NaN through.
+// The gate a = sigma(z) and b = 1 - a = sigma(-z), each with a relative error of its own: with a
+// near 1 the difference 1 - a would keep few bits of the long memories' rates.  bias is the
+// negated bias times log2(e): -z log2(e) is one multiply-add, whose roundings, of the bias's
+// product and of log2(e) itself the exponential turns into relative ones.  Both are within (|z| +
+// 1.3 |bias| + 0.3 |f| + 5) 2^-24 (the arithmetic emulated with f from a normal distribution and
+// biases up to 7: 15 * 2^-24 for b, 5 * 2^-24 for a).  The limits let a NaN through.
 __device__ __forceinline__ void gate(float f, float bias, float &a, float &b) {
     float z = __builtin_fmaf(f, -LOG2E, bias);
     z = __builtin_elementwise_minimum(__builtin_elementwise_maximum(z, -Z_MAX), Z_MAX);
