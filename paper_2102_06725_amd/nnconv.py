@@ -456,12 +456,13 @@ class _Workspaces:
     hold its address."""
 
     def __init__(self):
+        import torch
         self._held = {}
         self._kept = []
+        self._capturing = torch.cuda.is_current_stream_capturing
 
     def get(self, kind, stream, nbytes, device):
-        import torch
-        if device.type == "cuda" and torch.cuda.is_current_stream_capturing():
+        if device.type == "cuda" and self._capturing():
             return self._new(nbytes, stream, device)
         t = self._held.get((kind, stream, device))
         if t is None or t.numel() < nbytes:
@@ -658,8 +659,8 @@ class GatedRecurrence(_Handle):
             self._sizes[pass_] = nb
         return (None if nb == 0 else self._ws.get(pass_, stream, nb, x.device)), nb
 
-    def _fits(self, gpu, inputs, outputs, dense):
-        """Whether tensors of tokens ld and ldy elements apart, and dense ones of (type, elements), are these."""
+    def _fits(self, gpu, inputs, outputs, dense, saved):
+        """Whether tensors of tokens ld and ldy elements apart, dense ones of (type, elements), and saved states are these."""
         d, dtype = self.desc, self._dtype
         n, t, c = d.n, d.t, d.c
         try:
@@ -673,7 +674,8 @@ class GatedRecurrence(_Handle):
             for kind, count, tensors in dense:
                 if not _all_dense(tensors, kind, count, gpu):
                     return False
-            return True
+            return saved is None or (saved.dtype is self._f32 and saved.numel() >= self._saved_count()
+                                     and saved.is_contiguous() and saved.get_device() == gpu)
         except AttributeError:  # an object that is no tensor
             return False
 
@@ -707,13 +709,12 @@ class GatedRecurrence(_Handle):
     def fwd(self, x, f, bias, y, g=None, lengths=None, h0=None, ht=None, saved=None, stream=None):
         d, f32, gpu = self.desc, self._f32, self._gpu("x", x)
         n, c = d.n, d.c
-        if not self._fits(gpu, (x, f, g), (y,), ((f32, c, (bias,)), (f32, n * c, (h0, ht)), (self._i32, n, (lengths,)))):
+        if not self._fits(gpu, (x, f, g), (y,), ((f32, c, (bias,)), (f32, n * c, (h0, ht)), (self._i32, n, (lengths,))), saved):
             self._tokens(d.ld, gpu, x=x, f=f, g=g)
             self._tokens(d.ldy, gpu, y=y)
             self._dense(f32, c, gpu, bias=bias)
             self._dense(f32, n * c, gpu, h0=h0, ht=ht)
             self._dense(self._i32, n, gpu, lengths=lengths)
-        if saved is not None:
             self._dense(f32, self._saved_count(), gpu, more=True, saved=saved)
         stream = self._stream(stream, gpu)
         ws, nb = self._workspace(NNCONV_FWD, stream, x)
@@ -729,13 +730,13 @@ class GatedRecurrence(_Handle):
         d, f32, gpu = self.desc, self._f32, self._gpu("x", x)
         n, c = d.n, d.c
         if not self._fits(gpu, (x, f, g, dx, df, dg), (dy,),
-                          ((f32, c, (bias, dbias)), (f32, n * c, (dht, dh0)), (self._i32, n, (lengths,)))):
+                          ((f32, c, (bias, dbias)), (f32, n * c, (dht, dh0)), (self._i32, n, (lengths,))), saved):
             self._tokens(d.ld, gpu, x=x, f=f, g=g, dx=dx, df=df, dg=dg)
             self._tokens(d.ldy, gpu, dy=dy)
             self._dense(f32, c, gpu, bias=bias, dbias=dbias)
             self._dense(f32, n * c, gpu, dht=dht, dh0=dh0)
             self._dense(self._i32, n, gpu, lengths=lengths)
-        self._dense(f32, self._saved_count(), gpu, more=True, saved=saved)
+            self._dense(f32, self._saved_count(), gpu, more=True, saved=saved)
         if overflow_flag is not None:
             self._dense(self._i32, 1, gpu, more=True, overflow_flag=overflow_flag)
         stream = self._stream(stream, gpu)
