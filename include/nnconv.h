@@ -386,7 +386,8 @@ typedef struct {
 
 /* Forward: y and, where the pointers are not NULL, sum (= r) and rstd
  * (fp32, [rows], for the backward pass).  A row whose mean square passes fp32's
- * range has rstd 0.  residual: NULL or [rows][c].
+ * range has rstd 0, one below it with eps = 0 an infinite rstd.
+ * residual: NULL or [rows][c].
  * gain: fp32, [c].  sum may be x or residual itself (updated in place);
  * nothing else may overlap an output.  A row of zeros with eps = 0 gives NaN,
  * as the formula does.  Any alignment of at least one element; 16-byte aligned
@@ -435,7 +436,8 @@ nnconv_status nnconv_rmsnorm_bwd(const nnconv_rmsnorm_desc *desc, const void *su
  *   h_t = a_t * h_(t-1) + (1 - a_t) * x_t,   h_0 = h0
  *   y_t = h_t * g_t / (1 + exp(-g_t))        (y_t = h_t without g)
  * The limit keeps both a and 1 - a above 0, so that a gate never makes a NaN
- * of an infinite state; a NaN passes through. */
+ * of an infinite state; a NaN passes through.  One channel (c = 1) is walked
+ * token by token, a sequence a lane. */
 typedef struct {
     int32_t n;      /* sequences, >= 0 */
     int32_t t;      /* tokens of each, >= 0 */
@@ -501,7 +503,8 @@ nnconv_status nnconv_recurrence_bwd(const nnconv_recurrence_desc *desc, const vo
  *   master -= lr (m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps)
  *                 + weight_decay * master)
  *   w16 = round-to-nearest-even(master)
- * in fp32, with m and v unrounded in the master's update.
+ * in fp32, with m and v unrounded in the master's update (0 / 0, with eps = 0
+ * and a v of 0, is NaN).
  *
  * state_dtype F32: m and v are fp32 arrays.  F8: m is e4m3 (largest 448) and
  * v e5m2 (largest 57344) codes, with one power of two for every
