@@ -498,7 +498,7 @@ class _Handle:
     device than the call's are refused, since it would read or write past their end.  Other
     objects with data_ptr() are taken as they are.
 
-    A call looks its tensors over in one expression (a third of a microsecond each); only where
+    A call looks its tensors over in one go (a quarter of a microsecond each); only where
     that fails are they looked at one by one, for the name of the one to refuse."""
 
     def __init__(self, desc, dtype=None):
