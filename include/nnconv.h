@@ -2,7 +2,8 @@
  * nnconv.h -- C ABI of libnnconv: mixed-precision 2-D convolution in the
  * three training passes (forward, backward-data, backward-weight) on one
  * AMD Instinct MI355X (gfx950); and, after it, the operators of gated sequence blocks on
- * channel-last tokens (norm, recurrence) and the solver they are trained with.
+ * channel-last tokens (norm, recurrence), the solver they are trained with, and both
+ * ends of a model over a vocabulary (embedding, cross entropy, distillation).
  *
  * The operation is the paper's convolution call (Sec. 3.2, Listings 4-5:
  * convolution(x, base_axis=1, outmaps, kernel, ...)), trained by
@@ -565,6 +566,108 @@ nnconv_status nnconv_adamw_update(const nnconv_adamw_plan *plan, int32_t *step, 
                                   float beta1, float beta2, float eps, uint32_t seed,
                                   const nnconv_loss_scaler *state, const int32_t *overflow_flag,
                                   void *hip_stream);
+
+/* Both ends of a model over a vocabulary of v tokens: the rows of a table that
+ * token numbers name, and the softmax cross entropy of the last rows against
+ * the table of a head, with the gradients of both.  Token numbers are device
+ * int32; one outside 0..v-1 (such as -1) is padding.  Calls without rows take
+ * null pointers for what has none. */
+
+typedef struct {
+    int64_t rows;   /* tokens, 0 to 2^29 */
+    int32_t c;      /* channels, 1 to 2^28 */
+    int32_t v;      /* rows of the table, >= 1 */
+    int32_t dtype;  /* F16 or BF16: table, y, dy */
+    float scale;    /* finite: what a row is multiplied by */
+} nnconv_embedding_desc;
+
+/* y[r] = scale * table[ids[r]], zeros for padding.  ids: [rows], table: [v][c],
+ * y: [rows][c], dense.  16-byte aligned tables and outputs with c a multiple
+ * of 8 are the fast ones.
+ * INVALID_ARG: rows < 0, c < 1, v < 1, scale not finite, bad dtype, null
+ * pointers; UNSUPPORTED: dtype F32, more tokens or channels; MISALIGNED:
+ * pointers below their element size. */
+nnconv_status nnconv_embedding_fwd(const nnconv_embedding_desc *desc, const int32_t *ids,
+                                   const void *table, void *y, void *hip_stream);
+
+/* Bytes of workspace of nnconv_embedding_bwd. */
+nnconv_status nnconv_embedding_workspace_size(const nnconv_embedding_desc *desc, size_t *bytes);
+
+/* The table's gradient:
+ *   dtable[j] = (accumulate ? dtable[j] : 0)
+ *               + inv_loss_scale * scale * sum over r with ids[r] = j of dy[r]
+ * The tokens are sorted by number first, so that every sum has a fixed order.
+ * Without accumulate every row is written, those that no token names with
+ * zeros; with it these rows are neither read nor written, so that the call may
+ * add to the gradient of a head that shares the table.  dy of padding is not
+ * read.  dtable_dtype: F32 or desc->dtype.
+ * Errors as nnconv_embedding_fwd's and as nnconv_wgrad's for accumulate and
+ * ws (16-byte aligned); UNSUPPORTED for another dtable_dtype. */
+nnconv_status nnconv_embedding_bwd(const nnconv_embedding_desc *desc, const int32_t *ids,
+                                   const void *dy, void *dtable, int32_t dtable_dtype,
+                                   float inv_loss_scale, int32_t accumulate,
+                                   int32_t *overflow_flag, void *ws, size_t ws_bytes,
+                                   void *hip_stream);
+
+/* Softmax cross entropy over a vocabulary, without the logits in memory:
+ *   z[r][j] = logit_scale * sum over c of x[r][c] * w[j][c]
+ *   lse[r]  = log sum over j of exp(z[r][j])
+ *   loss[r] = sum over i < k of q[r][i] * (log q[r][i] + lse[r] - z[r][targets[r][i]])
+ * With labels (teacher NULL, k = 1) q is 1: loss = lse - z[target].  With a
+ * teacher q is the softmax of logit_scale * teacher[r][.] over the row's k
+ * entries, the teacher's largest logits as a rule, and the loss the divergence
+ * of the student from it; entries whose target is padding or whose logit is
+ * -inf are left out, and a target that is named twice counts with both shares.
+ * A row without an entry does not count: its loss, lse and gradients are 0, and
+ * its x is not read. */
+typedef struct {
+    int64_t rows;          /* 0 to 2^23 */
+    int32_t c;             /* channels, 1 to 2^20 */
+    int32_t v;             /* vocabulary, 1 to 2^21 */
+    int32_t dtype;         /* F16 or BF16: x, w, dx */
+    int32_t k;             /* targets of a row, 1 to 1024; 1 with labels */
+    int32_t teacher_dtype; /* F32 or dtype (ignored without a teacher) */
+    float logit_scale;     /* finite: 1 / temperature */
+} nnconv_xent_desc;
+
+/* Bytes of workspace of nnconv_xent_fwd (NNCONV_FWD) or nnconv_xent_train
+ * (NNCONV_DGRAD).  Training keeps 16 bits for each logit of a piece of the
+ * rows, 1 GiB of them at most (256 rows at least), and fp32 sums of dw where
+ * there is more than one piece. */
+nnconv_status nnconv_xent_workspace_size(const nnconv_xent_desc *desc, nnconv_pass pass,
+                                         size_t *bytes);
+
+/* loss and, where lse is not NULL, lse: fp32, [rows].  x: [rows][c], w: [v][c],
+ * targets: [rows][k], teacher: NULL or [rows][k], dense.  w has to be 16-byte
+ * aligned where c is a multiple of 8; other channel counts are copied into the
+ * workspace.  ws: 16-byte aligned.
+ * INVALID_ARG: sizes below the limits above, logit_scale not finite, bad
+ * dtypes, null x, w, targets or loss, k other than 1 without a teacher;
+ * UNSUPPORTED: larger sizes, other types; WORKSPACE; MISALIGNED. */
+nnconv_status nnconv_xent_fwd(const nnconv_xent_desc *desc, const void *x, const void *w,
+                              const int32_t *targets, const void *teacher, float *loss, float *lse,
+                              void *ws, size_t ws_bytes, void *hip_stream);
+
+/* The same and the gradients of alpha * (*grad_scale) * sum over r of loss[r]
+ * (grad_scale: a device fp32, or NULL for 1: the loss scale over the number of
+ * rows that count, say):
+ *   dz = softmax(z) - q
+ *   dx[r] = G * logit_scale * sum over j of dz[r][j] * w[j],   G = alpha * (*grad_scale)
+ *   dw[j] = (accumulate ? dw[j] : 0)
+ *           + inv_loss_scale * G * logit_scale * sum over r of dz[r][j] * x[r]
+ * dz is rounded once to the operands' type, as an operand of both products
+ * (2^15 dz, so that fp16 keeps its 11 bits down to a dz of 2^-29).  dx:
+ * [rows][c], it may be x itself; dw: [v][c] of dw_dtype, F32 or desc->dtype,
+ * or NULL: then it is left out.  overflow_flag is set where an element of dx
+ * or dw is inf or NaN.  16-byte aligned dx and dw with c a multiple of 8 are the
+ * fast ones.
+ * Errors as nnconv_xent_fwd's and as nnconv_wgrad's for accumulate; null dx:
+ * INVALID_ARG; another dw_dtype: UNSUPPORTED. */
+nnconv_status nnconv_xent_train(const nnconv_xent_desc *desc, const void *x, const void *w,
+                                const int32_t *targets, const void *teacher, float alpha,
+                                const float *grad_scale, float *loss, float *lse, void *dx, void *dw,
+                                int32_t dw_dtype, float inv_loss_scale, int32_t accumulate,
+                                int32_t *overflow_flag, void *ws, size_t ws_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -2238,3 +2238,184 @@ NNCONV_API nnconv_status nnconv_adamw_update(const nnconv_adamw_plan *plan, int3
                                    beta1, beta2, eps, seed, state, overflow_flag,
                                    (hipStream_t)hip_stream));
 }
+
+// ---------------------------------------------------------------------------
+// both ends of a model over a vocabulary
+// ---------------------------------------------------------------------------
+
+// The gradient of a parameter may be fp32 or of the operands' type.
+static nnconv_status grad_dtype(int32_t kind, int32_t dtype) {
+    if (kind == NNCONV_F32 || kind == dtype) return NNCONV_OK;
+    return kind == NNCONV_F16 || kind == NNCONV_BF16 || kind == NNCONV_F8 ? NNCONV_ERR_UNSUPPORTED
+                                                                          : NNCONV_ERR_INVALID_ARG;
+}
+
+static nnconv_status embedding_check(const nnconv_embedding_desc *d) {
+    if (!d || d->rows < 0 || d->c < 1 || d->v < 1 || !__builtin_isfinite(d->scale))
+        return NNCONV_ERR_INVALID_ARG;
+    if (d->rows > MAX_ELEMS / d->c || d->v > MAX_ELEMS / d->c) return NNCONV_ERR_INVALID_ARG;
+    if (d->c > MOST_CHANNELS || d->rows > MOST_IDS) return NNCONV_ERR_UNSUPPORTED;
+    return half_dtype(d->dtype);
+}
+
+static EmbeddingParams embedding_params(const nnconv_embedding_desc *d, const int32_t *ids) {
+    EmbeddingParams p;
+    memset(&p, 0, sizeof(p));
+    p.rows = d->rows;
+    p.c = d->c;
+    p.v = d->v;
+    p.scale = d->scale;
+    p.ids = ids;
+    return p;
+}
+
+NNCONV_API nnconv_status nnconv_embedding_fwd(const nnconv_embedding_desc *desc, const int32_t *ids,
+                                              const void *table, void *y, void *hip_stream) {
+    const nnconv_status st = embedding_check(desc);
+    if (st != NNCONV_OK) return st;
+    if (desc->rows > 0 && (!ids || !table || !y)) return NNCONV_ERR_INVALID_ARG;
+    if (!aligned(ids, 4) || !aligned(table, 2) || !aligned(y, 2)) return NNCONV_ERR_MISALIGNED;
+    if (desc->rows == 0) return NNCONV_OK;
+    EmbeddingParams p = embedding_params(desc, ids);
+    p.table = table;
+    p.y = y;
+    clear_stale_error();
+    return hip_status(launch_embedding_fwd(desc->dtype, p, (hipStream_t)hip_stream));
+}
+
+NNCONV_API nnconv_status nnconv_embedding_workspace_size(const nnconv_embedding_desc *desc,
+                                                         size_t *bytes) {
+    const nnconv_status st = embedding_check(desc);
+    if (st != NNCONV_OK) return st;
+    if (!bytes) return NNCONV_ERR_INVALID_ARG;
+    *bytes = embedding_ws(desc->rows, desc->c);
+    return NNCONV_OK;
+}
+
+// A workspace of `need` bytes, 16-byte aligned.
+static nnconv_status workspace_check(size_t need, const void *ws, size_t ws_bytes) {
+    if (need == 0) return NNCONV_OK;
+    if (!ws) return NNCONV_ERR_INVALID_ARG;
+    if (ws_bytes < need) return NNCONV_ERR_WORKSPACE;
+    return aligned(ws, 16) ? NNCONV_OK : NNCONV_ERR_MISALIGNED;
+}
+
+NNCONV_API nnconv_status nnconv_embedding_bwd(const nnconv_embedding_desc *desc, const int32_t *ids,
+                                              const void *dy, void *dtable, int32_t dtable_dtype,
+                                              float inv_loss_scale, int32_t accumulate,
+                                              int32_t *overflow_flag, void *ws, size_t ws_bytes,
+                                              void *hip_stream) {
+    nnconv_status st = embedding_check(desc);
+    if (st == NNCONV_OK) st = grad_dtype(dtable_dtype, desc->dtype);
+    if (st != NNCONV_OK) return st;
+    if ((desc->rows > 0 && (!ids || !dy)) || !dtable || (accumulate != 0 && accumulate != 1))
+        return NNCONV_ERR_INVALID_ARG;
+    if (!aligned(ids, 4) || !aligned(dy, 2) || !aligned(dtable, dtable_dtype == NNCONV_F32 ? 4 : 2) ||
+        (overflow_flag && !aligned(overflow_flag, 4)))
+        return NNCONV_ERR_MISALIGNED;
+    st = workspace_check(embedding_ws(desc->rows, desc->c), ws, ws_bytes);
+    if (st != NNCONV_OK) return st;
+    EmbeddingParams p = embedding_params(desc, ids);
+    p.dy = dy;
+    p.dtable = dtable;
+    p.dtable_dtype = dtable_dtype;
+    p.accumulate = accumulate;
+    p.inv_loss_scale = inv_loss_scale;
+    p.flag = overflow_flag;
+    p.ws = ws;
+    clear_stale_error();
+    return hip_status(launch_embedding_bwd(desc->dtype, p, (hipStream_t)hip_stream));
+}
+
+static nnconv_status xent_check(const nnconv_xent_desc *d, XentParams *p) {
+    if (!d || d->rows < 0 || d->c < 1 || d->v < 1 || d->k < 1 || !__builtin_isfinite(d->logit_scale))
+        return NNCONV_ERR_INVALID_ARG;
+    if (d->rows > MAX_ELEMS / d->c || d->rows > MAX_ELEMS / d->v || d->v > MAX_ELEMS / d->c)
+        return NNCONV_ERR_INVALID_ARG;
+    if (d->teacher_dtype != NNCONV_F32 && d->teacher_dtype != NNCONV_F16 && d->teacher_dtype != NNCONV_BF16)
+        return d->teacher_dtype == NNCONV_F8 ? NNCONV_ERR_UNSUPPORTED : NNCONV_ERR_INVALID_ARG;
+    const nnconv_status st = half_dtype(d->dtype);
+    if (st != NNCONV_OK) return st;
+    if (d->teacher_dtype != NNCONV_F32 && d->teacher_dtype != d->dtype) return NNCONV_ERR_UNSUPPORTED;
+    memset(p, 0, sizeof(*p));
+    p->rows = d->rows;
+    p->c = d->c;
+    p->v = d->v;
+    p->k = d->k;
+    p->dtype = d->dtype;
+    p->teacher_dtype = d->teacher_dtype;
+    p->logit_scale = d->logit_scale;
+    return xent_fits(*p) ? NNCONV_OK : NNCONV_ERR_UNSUPPORTED;
+}
+
+NNCONV_API nnconv_status nnconv_xent_workspace_size(const nnconv_xent_desc *desc, nnconv_pass pass,
+                                                    size_t *bytes) {
+    XentParams p;
+    const nnconv_status st = xent_check(desc, &p);
+    if (st != NNCONV_OK) return st;
+    if (!bytes || (pass != NNCONV_FWD && pass != NNCONV_DGRAD)) return NNCONV_ERR_INVALID_ARG;
+    *bytes = xent_ws(p, pass == NNCONV_DGRAD);
+    return NNCONV_OK;
+}
+
+// What both calls take: the operands, and the loss.
+static nnconv_status xent_common(XentParams *p, const void *x, const void *w, const int32_t *targets,
+                                 const void *teacher, float *loss, float *lse, bool train, void *ws,
+                                 size_t ws_bytes) {
+    if (p->rows > 0 && (!x || !w || !targets || !loss || (!teacher && p->k != 1)))
+        return NNCONV_ERR_INVALID_ARG;
+    // rows of whole 16-byte vectors are read where they lie, others copied
+    if (!aligned(x, 2) || !aligned(w, p->c % 8 == 0 ? 16 : 2) || !aligned(targets, 4) ||
+        (teacher && !aligned(teacher, p->teacher_dtype == NNCONV_F32 ? 4 : 2)) || !aligned(loss, 4) ||
+        (lse && !aligned(lse, 4)))
+        return NNCONV_ERR_MISALIGNED;
+    p->x = x;
+    p->w = w;
+    p->targets = targets;
+    p->teacher = teacher;
+    p->loss = loss;
+    p->lse = lse;
+    p->ws = ws;
+    return workspace_check(xent_ws(*p, train), ws, ws_bytes);
+}
+
+NNCONV_API nnconv_status nnconv_xent_fwd(const nnconv_xent_desc *desc, const void *x, const void *w,
+                                         const int32_t *targets, const void *teacher, float *loss,
+                                         float *lse, void *ws, size_t ws_bytes, void *hip_stream) {
+    XentParams p;
+    nnconv_status st = xent_check(desc, &p);
+    if (st == NNCONV_OK) st = xent_common(&p, x, w, targets, teacher, loss, lse, false, ws, ws_bytes);
+    if (st != NNCONV_OK) return st;
+    clear_stale_error();
+    return hip_status(launch_xent(p, false, (hipStream_t)hip_stream));
+}
+
+NNCONV_API nnconv_status nnconv_xent_train(const nnconv_xent_desc *desc, const void *x, const void *w,
+                                           const int32_t *targets, const void *teacher, float alpha,
+                                           const float *grad_scale, float *loss, float *lse, void *dx,
+                                           void *dw, int32_t dw_dtype, float inv_loss_scale,
+                                           int32_t accumulate, int32_t *overflow_flag, void *ws,
+                                           size_t ws_bytes, void *hip_stream) {
+    XentParams p;
+    nnconv_status st = xent_check(desc, &p);
+    if (st != NNCONV_OK) return st;
+    if (dw) st = grad_dtype(dw_dtype, desc->dtype);
+    if (st != NNCONV_OK) return st;
+    if ((desc->rows > 0 && !dx) || (accumulate != 0 && accumulate != 1)) return NNCONV_ERR_INVALID_ARG;
+    if ((grad_scale && !aligned(grad_scale, 4)) || !aligned(dx, 2) ||
+        (dw && !aligned(dw, dw_dtype == NNCONV_F32 ? 4 : 2)) ||
+        (overflow_flag && !aligned(overflow_flag, 4)))
+        return NNCONV_ERR_MISALIGNED;
+    st = xent_common(&p, x, w, targets, teacher, loss, lse, true, ws, ws_bytes);
+    if (st != NNCONV_OK) return st;
+    p.alpha = alpha;
+    p.grad_scale = grad_scale;
+    p.dx = dx;
+    p.dw = dw;
+    p.dw_dtype = dw_dtype;
+    p.inv_loss_scale = inv_loss_scale;
+    p.accumulate = accumulate;
+    p.flag = overflow_flag;
+    clear_stale_error();
+    return hip_status(launch_xent(p, true, (hipStream_t)hip_stream));
+}

@@ -499,4 +499,49 @@ hipError_t launch_adamw(const AdamwTable &tab, int64_t chunks, int32_t *step, fl
                         float beta2, float eps, uint32_t seed, const nnconv_loss_scaler *state,
                         const int32_t *flag, hipStream_t st);
 
+// --- both ends of a model over a vocabulary ------------------------------------
+
+// Tokens of a lookup at most: workgroups of 256 threads for every 64 of them.
+constexpr int64_t MOST_IDS = 1 << 29;
+
+// Rows of a table by token number (embedding.hip).
+struct EmbeddingParams {
+    int64_t rows;
+    int32_t c, v;
+    float scale;
+    const int32_t *ids;
+    const void *table;   // forward
+    void *y;
+    const void *dy;      // backward
+    void *dtable;
+    int32_t dtable_dtype, accumulate;
+    float inv_loss_scale;
+    int32_t *flag;
+    void *ws;
+};
+size_t embedding_ws(int64_t rows, int32_t c);
+hipError_t launch_embedding_fwd(int dtype, const EmbeddingParams &p, hipStream_t st);
+hipError_t launch_embedding_bwd(int dtype, const EmbeddingParams &p, hipStream_t st);
+
+// Softmax cross entropy over a vocabulary (xent.hip).
+struct XentParams {
+    int64_t rows;
+    int32_t c, v, k, dtype, teacher_dtype;
+    float logit_scale;
+    const void *x, *w;
+    const int32_t *targets;
+    const void *teacher;      // null: labels
+    float *loss, *lse;        // lse may be null
+    const float *grad_scale;  // training
+    float alpha, inv_loss_scale;
+    void *dx, *dw;            // dw may be null
+    int32_t dw_dtype, accumulate;
+    int32_t *flag;
+    void *ws;
+    bool sizes_only;          // the workspace of a call with every output
+};
+bool xent_fits(const XentParams &p);
+size_t xent_ws(const XentParams &p, bool train);
+hipError_t launch_xent(const XentParams &p, bool train, hipStream_t st);
+
 }  // namespace nnconv

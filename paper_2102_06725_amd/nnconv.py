@@ -78,7 +78,9 @@ EXPORTS = ("nnconv_version", "nnconv_last_hip_error", "nnconv_status_string", "n
            "nnconv_rmsnorm_fwd", "nnconv_rmsnorm_fwd_q8", "nnconv_rmsnorm_workspace_size",
            "nnconv_rmsnorm_bwd", "nnconv_recurrence_saved_size",
            "nnconv_recurrence_workspace_size", "nnconv_recurrence_fwd", "nnconv_recurrence_bwd",
-           "nnconv_adamw_plan_size", "nnconv_adamw_plan_init", "nnconv_adamw_update")
+           "nnconv_adamw_plan_size", "nnconv_adamw_plan_init", "nnconv_adamw_update",
+           "nnconv_embedding_fwd", "nnconv_embedding_workspace_size", "nnconv_embedding_bwd",
+           "nnconv_xent_workspace_size", "nnconv_xent_fwd", "nnconv_xent_train")
 
 
 class nnconv_desc(ctypes.Structure):
@@ -115,6 +117,17 @@ class nnconv_adamw_tensor(ctypes.Structure):
 class nnconv_adamw_plan(ctypes.Structure):
     _fields_ = [("table", ctypes.c_void_p), ("chunks", ctypes.c_int64),
                 ("tensors", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class nnconv_embedding_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("c", ctypes.c_int32), ("v", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class nnconv_xent_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("c", ctypes.c_int32), ("v", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("k", ctypes.c_int32), ("teacher_dtype", ctypes.c_int32),
+                ("logit_scale", ctypes.c_float)]
 
 
 class NNConvError(RuntimeError):
@@ -193,6 +206,13 @@ def load(path: str | None = None):
     lib.nnconv_adamw_plan_init.argtypes = [tens, _I32, _VP, _SZ, plan, _VP]
     lib.nnconv_adamw_update.argtypes = [plan, _VP, _F32, _F32, _F32, _F32, ctypes.c_uint32, _VP,
                                         _VP, _VP]
+    emb, xent = ctypes.POINTER(nnconv_embedding_desc), ctypes.POINTER(nnconv_xent_desc)
+    lib.nnconv_embedding_fwd.argtypes = [emb] + [_VP] * 4
+    lib.nnconv_embedding_workspace_size.argtypes = [emb, _SZP]
+    lib.nnconv_embedding_bwd.argtypes = [emb] + [_VP] * 3 + [_I32, _F32, _I32, _VP, _VP, _SZ, _VP]
+    lib.nnconv_xent_workspace_size.argtypes = [xent, ctypes.c_int, _SZP]
+    lib.nnconv_xent_fwd.argtypes = [xent] + [_VP] * 7 + [_SZ, _VP]
+    lib.nnconv_xent_train.argtypes = [xent] + [_VP] * 4 + [_F32] + [_VP] * 5 + [_I32, _F32, _I32, _VP, _VP, _SZ, _VP]
     for f in EXPORTS[3:]:
         getattr(lib, f).restype = ctypes.c_int
     if path is None:
@@ -372,6 +392,42 @@ def nnconv_adamw_update(plan, step, lr, beta1, beta2, eps, seed, state, overflow
                                       stream)
 
 
+def nnconv_embedding_fwd(desc, ids, table, y, stream) -> int:
+    return load().nnconv_embedding_fwd(ctypes.byref(desc), ids, table, y, stream)
+
+
+def nnconv_embedding_workspace_size(desc):
+    b = ctypes.c_size_t()
+    st = load().nnconv_embedding_workspace_size(ctypes.byref(desc), ctypes.byref(b))
+    return st, b.value
+
+
+def nnconv_embedding_bwd(desc, ids, dy, dtable, dtable_dtype, inv_loss_scale, accumulate,
+                         overflow_flag, ws, ws_bytes, stream) -> int:
+    return load().nnconv_embedding_bwd(ctypes.byref(desc), ids, dy, dtable, int(dtable_dtype),
+                                       float(inv_loss_scale), int(accumulate), overflow_flag, ws,
+                                       ws_bytes, stream)
+
+
+def nnconv_xent_workspace_size(desc, pass_: int):
+    b = ctypes.c_size_t()
+    st = load().nnconv_xent_workspace_size(ctypes.byref(desc), int(pass_), ctypes.byref(b))
+    return st, b.value
+
+
+def nnconv_xent_fwd(desc, x, w, targets, teacher, loss, lse, ws, ws_bytes, stream) -> int:
+    return load().nnconv_xent_fwd(ctypes.byref(desc), x, w, targets, teacher, loss, lse, ws,
+                                  ws_bytes, stream)
+
+
+def nnconv_xent_train(desc, x, w, targets, teacher, alpha, grad_scale, loss, lse, dx, dw, dw_dtype,
+                      inv_loss_scale, accumulate, overflow_flag, ws, ws_bytes, stream) -> int:
+    return load().nnconv_xent_train(ctypes.byref(desc), x, w, targets, teacher, float(alpha),
+                                    grad_scale, loss, lse, dx, dw, int(dw_dtype),
+                                    float(inv_loss_scale), int(accumulate), overflow_flag, ws,
+                                    ws_bytes, stream)
+
+
 def check(status: int, what: str = "") -> None:
     if status != NNCONV_OK:
         raise NNConvError(status, what)
@@ -535,6 +591,17 @@ class _Handle:
                     t.dtype is dtype and t.is_contiguous() and t.get_device() == gpu
                     and (t.numel() == count or more and t.numel() > count)):
                 self._refuse(name, t, "%d%s dense elements of %s on device %d" % (count, " or more" if more else "", dtype, gpu))
+
+
+    def _gradient(self, name, t, count, gpu):
+        """The type code of a parameter's gradient: fp32, or as the operands."""
+        if not isinstance(t, self._tensor):
+            if t is None:
+                raise ValueError("%s: %s is needed" % (type(self).__name__, name))
+            return NNCONV_F32
+        wide = t.dtype is self._f32
+        self._dense(self._f32 if wide else self._dtype, count, gpu, **{name: t})
+        return NNCONV_F32 if wide else self.desc.dtype
 
 
 class RMSNorm(_Handle):
@@ -812,3 +879,119 @@ class AdamW(_Handle):
             self._refuse("state", state, "the loss scaler's %d bytes on device %d" % (ctypes.sizeof(nnconv_loss_scaler), gpu))
         check(nnconv_adamw_update(self.plan, _ptr(step), lr, beta1, beta2, eps, self.seed, _ptr(state),
                                   _ptr(overflow_flag), self._stream(stream, gpu)), "nnconv_adamw_update")
+
+
+class Embedding(_Handle):
+    """Rows of a table [v][c] by token number, times `scale`: nnconv_embedding_*.  `rows`, the
+    tokens of a call, may be changed between calls.  Tensors are dense and on the current device,
+    token numbers int32; others are refused with a ValueError."""
+
+    def __init__(self, rows, c, v, dtype=NNCONV_F16, scale=1.0):
+        super().__init__(nnconv_embedding_desc(rows, c, v, dtype, scale), dtype)
+        self._ws = _Workspaces()
+        self._nbytes = None
+
+    @property
+    def rows(self):
+        return self.desc.rows
+
+    @rows.setter
+    def rows(self, rows):
+        self.desc.rows = rows
+        self._nbytes = None
+
+    def fwd(self, ids, table, y, stream=None):
+        d, gpu = self.desc, self._gpu("ids", ids)
+        self._dense(self._i32, d.rows, gpu, ids=ids)
+        self._dense(self._dtype, d.v * d.c, gpu, table=table)
+        self._dense(self._dtype, d.rows * d.c, gpu, y=y)
+        check(self._lib.nnconv_embedding_fwd(self._ref, ids.data_ptr(), _ptr(table), _ptr(y), self._stream(stream, gpu)),
+              "nnconv_embedding_fwd")
+
+    def bwd(self, ids, dy, dtable, inv_loss_scale=1.0, accumulate=0, overflow_flag=None, stream=None):
+        """dtable: fp32 or of the table's type."""
+        d, gpu = self.desc, self._gpu("ids", ids)
+        self._dense(self._i32, d.rows, gpu, ids=ids)
+        self._dense(self._dtype, d.rows * d.c, gpu, dy=dy)
+        kind = self._gradient("dtable", dtable, d.v * d.c, gpu)
+        if overflow_flag is not None:
+            self._dense(self._i32, 1, gpu, more=True, overflow_flag=overflow_flag)
+        stream = self._stream(stream, gpu)
+        if self._nbytes is None:
+            st, self._nbytes = nnconv_embedding_workspace_size(d)
+            check(st, "nnconv_embedding_workspace_size")
+        ws = self._ws.get("bwd", stream, self._nbytes, ids.device)
+        check(self._lib.nnconv_embedding_bwd(
+            self._ref, ids.data_ptr(), _ptr(dy), _ptr(dtable), kind, inv_loss_scale, accumulate, _ptr(overflow_flag),
+            ws.data_ptr(), self._nbytes, stream), "nnconv_embedding_bwd")
+
+
+class CrossEntropy(_Handle):
+    """Softmax cross entropy of logit_scale * x w^T over a vocabulary of v rows of w:
+    nnconv_xent_*.  With labels each row has one target; with `k` each row has k targets and a
+    teacher's logits for them, fp32 or of x's type (teacher_dtype).  `rows` may be changed between
+    calls.  Tensors are dense and on the current device, targets int32; others are refused with a
+    ValueError."""
+
+    def __init__(self, rows, c, v, dtype=NNCONV_F16, logit_scale=1.0, k=None, teacher_dtype=NNCONV_F32):
+        import torch
+        super().__init__(nnconv_xent_desc(rows, c, v, dtype, 1 if k is None else k, teacher_dtype, logit_scale), dtype)
+        self._teacher = None if k is None else {
+            NNCONV_F16: torch.float16, NNCONV_BF16: torch.bfloat16}.get(teacher_dtype, torch.float32)
+        self._ws = _Workspaces()
+        self._sizes = {}  # pass -> workspace bytes of the present rows
+
+    @property
+    def rows(self):
+        return self.desc.rows
+
+    @rows.setter
+    def rows(self, rows):
+        self.desc.rows = rows
+        self._sizes.clear()
+
+    def _workspace(self, pass_, stream, x):
+        nb = self._sizes.get(pass_)
+        if nb is None:
+            st, nb = nnconv_xent_workspace_size(self.desc, pass_)
+            check(st, "nnconv_xent_workspace_size")
+            self._sizes[pass_] = nb
+        return self._ws.get(pass_, stream, nb, x.device), nb
+
+    def _operands(self, gpu, x, w, targets, teacher, loss, lse):
+        d = self.desc
+        if (teacher is None) != (self._teacher is None):
+            raise ValueError("CrossEntropy: teacher: %s" % ("made with labels" if self._teacher is None else "is needed"))
+        self._dense(self._dtype, d.rows * d.c, gpu, x=x)
+        self._dense(self._dtype, d.v * d.c, gpu, w=w)
+        self._dense(self._i32, d.rows * d.k, gpu, targets=targets)
+        if teacher is not None:
+            self._dense(self._teacher, d.rows * d.k, gpu, teacher=teacher)
+        self._dense(self._f32, d.rows, gpu, loss=loss, lse=lse)
+
+    def fwd(self, x, w, targets, loss, lse=None, teacher=None, stream=None):
+        gpu = self._gpu("x", x)
+        self._operands(gpu, x, w, targets, teacher, loss, lse)
+        stream = self._stream(stream, gpu)
+        ws, nb = self._workspace(NNCONV_FWD, stream, x)
+        check(self._lib.nnconv_xent_fwd(
+            self._ref, x.data_ptr(), _ptr(w), _ptr(targets), _ptr(teacher), _ptr(loss), _ptr(lse), ws.data_ptr(), nb, stream),
+            "nnconv_xent_fwd")
+
+    def train(self, x, w, targets, loss, dx, dw=None, lse=None, teacher=None, alpha=1.0, grad_scale=None, inv_loss_scale=1.0,
+              accumulate=0, overflow_flag=None, stream=None):
+        """dw: fp32 or of w's type; grad_scale: an fp32 tensor of one element."""
+        d, gpu = self.desc, self._gpu("x", x)
+        self._operands(gpu, x, w, targets, teacher, loss, lse)
+        self._dense(self._dtype, d.rows * d.c, gpu, dx=dx)
+        kind = NNCONV_F32 if dw is None else self._gradient("dw", dw, d.v * d.c, gpu)
+        if grad_scale is not None:
+            self._dense(self._f32, 1, gpu, more=True, grad_scale=grad_scale)
+        if overflow_flag is not None:
+            self._dense(self._i32, 1, gpu, more=True, overflow_flag=overflow_flag)
+        stream = self._stream(stream, gpu)
+        ws, nb = self._workspace(NNCONV_DGRAD, stream, x)
+        check(self._lib.nnconv_xent_train(
+            self._ref, x.data_ptr(), _ptr(w), _ptr(targets), _ptr(teacher), alpha, _ptr(grad_scale), _ptr(loss), _ptr(lse),
+            _ptr(dx), _ptr(dw), kind, inv_loss_scale, accumulate, _ptr(overflow_flag), ws.data_ptr(), nb, stream),
+            "nnconv_xent_train")

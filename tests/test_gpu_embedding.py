@@ -1,0 +1,160 @@
+"""nnconv_embedding_* against the fp64 oracle.
+
+Bounds: a row is one fp32 product and one rounding.  A gradient row of n tokens is a chain of n fp32 additions (fewer
+where spans are joined), one product with a factor that is itself rounded, and the addition to what is there."""
+import numpy as np
+import pytest
+
+from oracle import vocabulary as V
+from paper_2102_06725_amd import nnconv as nc
+
+import sequence_util as U
+import vocabulary_util as W
+
+pytestmark = pytest.mark.gpu
+
+SIZES = [  # rows, c, v, dtype, padding, elements past 16-byte alignment
+    (1, 1, 1, "f16", 0.0, 0), (1, 8, 3, "bf16", 0.0, 0), (7, 9, 5, "f16", 0.3, 1), (64, 16, 300, "bf16", 0.2, 0),
+    (65, 255, 17, "f16", 0.0, 0), (200, 771, 1000, "bf16", 0.3, 3), (513, 264, 70000, "f16", 0.1, 0),
+    (4096, 24, 256, "bf16", 0.0, 0), (4097, 33, 257, "f16", 0.5, 0), (9001, 40, 65537, "bf16", 0.05, 0),
+    (300, 2056, 11, "f16", 0.0, 0), (12000, 8, 1, "bf16", 0.0, 0), (40, 520, 4000, "f16", 1.0, 0),
+]
+
+
+def ids_of(rng, rows, v, pad):
+    return W.tokens(rng, rows, v, pad)
+
+
+def desc(rows, c, v, dtype, scale):
+    return nc.nnconv_embedding_desc(rows, c, v, U.CODE[dtype], scale)
+
+
+@pytest.mark.parametrize("rows,c,v,dtype,pad,shift", SIZES)
+def test_fwd(nnlib, rows, c, v, dtype, pad, shift):
+    rng = np.random.default_rng(rows + c)
+    ids, table, scale = ids_of(rng, rows, v, pad), U.normal(rng, (v, c), dtype), float(np.float32(np.sqrt(c)))
+    I, T, Y = W.Ints(ids), U.Buf(table, dtype, shift=shift), U.Buf(dtype=dtype, shape=(rows, c), shift=shift)
+    nc.check(nc.nnconv_embedding_fwd(desc(rows, c, v, dtype, scale), I.data_ptr(), T.data_ptr(), Y.data_ptr(), nc.current_stream()))
+    ref = V.embedding_fwd(ids, table, scale)
+    U.close16(Y.f64(), ref, dtype, W.U32 * (1 + U.HALF_ULP[dtype]) * np.abs(ref))
+    T.host()
+
+
+def backward(ids, dy, v, dtype, scale, kind, old=None, inv=1.0, shift=0, flag=None, stream=None):
+    rows, c = dy.shape
+    d = desc(rows, c, v, dtype, scale)
+    I, D = W.Ints(ids), U.Buf(dy, dtype, shift=shift)
+    G = U.Buf(old, kind, shift=shift) if old is not None else U.Buf(dtype=kind, shape=(v, c), shift=shift)
+    st, nb = nc.nnconv_embedding_workspace_size(d)
+    nc.check(st)
+    ws = W.workspace(nb)
+    nc.check(nc.nnconv_embedding_bwd(d, I.data_ptr(), D.data_ptr(), G.data_ptr(), dict(U.CODE, f32=nc.NNCONV_F32)[kind], inv,
+                                     int(old is not None), None if flag is None else flag.data_ptr(), ws.data_ptr(), nb,
+                                     nc.current_stream() if stream is None else stream))
+    U.torch().cuda.synchronize()
+    return G
+
+
+def check(G, ids, dy, v, scale, kind, old=None, inv=1.0):
+    d, mag, n = V.embedding_bwd(ids, dy, v, scale)
+    ref = inv * d + (0.0 if old is None else old)
+    slack = (n[:, None] + 4) * W.U32 * inv * mag + 2 * W.U32 * np.abs(ref)
+    got = G.f64()
+    if kind == "f32":
+        U.close32(got, ref, slack)
+    else:
+        U.close16(got, ref, kind, slack * (1 + U.HALF_ULP[kind]))
+    idle = n == 0
+    assert np.array_equal(got[idle], np.zeros_like(got[idle]) if old is None else old[idle])
+    return got
+
+
+@pytest.mark.parametrize("wide", [True, False], ids=["f32", "16 bits"])
+@pytest.mark.parametrize("tied", [False, True], ids=["new", "added"])
+@pytest.mark.parametrize("rows,c,v,dtype,pad,shift", SIZES)
+def test_bwd(nnlib, rows, c, v, dtype, pad, shift, tied, wide):
+    if v * c > 2e7:
+        v //= 8
+    rng = np.random.default_rng(rows + c)
+    kind = "f32" if wide else dtype
+    ids, dy = ids_of(rng, rows, v, pad), U.normal(rng, (rows, c), dtype)
+    old = None if not tied else rng.standard_normal((v, c)).astype(np.float32).astype(np.float64) if wide else U.normal(rng, (v, c), dtype)
+    # loss scales are powers of two
+    check(backward(ids, dy, v, dtype, 1.5, kind, old, 2.0 ** -4, shift), ids, dy, v, 1.5, kind, old, 2.0 ** -4)
+
+
+@pytest.mark.parametrize("rows,v", [(1, 100000), (64, 64), (128, 2), (129, 2), (20000, 3), (8192, 2 ** 21)])
+def test_orders(nnlib, rows, v):
+    """All tokens alike, in rising and falling order, and numbers of every width."""
+    rng = np.random.default_rng(rows)
+    c = 4
+    for ids in (np.full(rows, v - 1), np.arange(rows) % v, (np.arange(rows)[::-1]) % v, (np.arange(rows) * 7919) % v,
+                np.repeat(np.arange(-(-rows // 64)), 64)[:rows] % v):
+        dy = U.normal(rng, (rows, c), "f16")
+        if v <= 100000:
+            check(backward(ids, dy, v, "f16", 1.0, "f32"), ids, dy, v, 1.0, "f32")
+        else:
+            old = np.zeros((v, c))
+            got = backward(ids, dy, v, "f16", 1.0, "f32", old).f64()
+            want = np.zeros((v, c))
+            np.add.at(want, ids, dy)
+            assert np.array_equal(np.nonzero(got.any(1))[0], np.nonzero(want.any(1))[0])
+            assert np.abs(got - want).max() <= rows * W.U32 * np.abs(dy).sum() / max(1, rows // 4)
+
+
+def test_padding_holds_anything(nnlib):
+    rng = np.random.default_rng(5)
+    ids = W.tokens(rng, 300, 50, 0.4)
+    dy = U.normal(rng, (300, 20), "bf16")
+    dy[(ids < 0) | (ids >= 50)] = np.nan
+    clean = np.where(np.isnan(dy), 0.0, dy)
+    got = check(backward(ids, dy, 50, "bf16", 1.0, "f32"), ids, clean, 50, 1.0, "f32")
+    assert np.isfinite(got).all()
+
+
+def test_same_bits(nnlib):
+    rng = np.random.default_rng(6)
+    ids, dy = W.tokens(rng, 30000, 4000), U.normal(rng, (30000, 24), "f16")
+    first = backward(ids, dy, 4000, "f16", 1.0, "f32").host()
+    for _ in range(3):
+        assert U.torch().equal(backward(ids, dy, 4000, "f16", 1.0, "f32").host(), first)
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16"])
+def test_flag(nnlib, kind):
+    t = U.torch()
+    flag = t.zeros(1, dtype=t.int32, device="cuda")
+    ids, dy = np.array([1, 1, 2]), np.full((3, 9), 60000.0)
+    backward(ids[2:], dy[2:], 4, "f16", 1.0, kind, flag=flag)
+    assert int(flag) == 0
+    backward(ids, dy, 4, "f16", 1.0, kind, flag=flag)  # 120000 passes fp16's range, not fp32's
+    assert int(flag) == (kind == "f16")
+    dy[0, 3] = np.inf
+    backward(ids, dy, 4, "f16", 1.0, kind, flag=flag)
+    assert int(flag) == 1
+
+
+def test_nothing(nnlib):
+    """No tokens: a gradient of zeros, or what is there."""
+    old = np.ones((5, 7))
+    none = np.zeros((0, 7))
+    assert np.all(backward(np.zeros(0), none, 5, "f16", 1.0, "f16").f64() == 0)
+    assert np.all(backward(np.zeros(0), none, 5, "f16", 1.0, "f32", old).f64() == 1)
+
+
+def test_handle(nnlib):
+    t = U.torch()
+    rng = np.random.default_rng(8)
+    op = nc.Embedding(50, 16, 30, dtype=nc.NNCONV_BF16, scale=2.0)
+    ids = t.from_numpy(W.tokens(rng, 50, 30, 0.2).astype(np.int32)).cuda()
+    table = t.randn((30, 16), device="cuda").bfloat16()
+    y, d = t.empty((50, 16), dtype=t.bfloat16, device="cuda"), t.empty((30, 16), device="cuda")
+    for rows in (50, 0, 1, 33):
+        op.rows = rows
+        op.fwd(ids[:rows], table, y[:rows])
+        op.bwd(ids[:rows], y[:rows], d)
+        host = ids[:rows].cpu().numpy()
+        ref = V.embedding_fwd(host, table.double().cpu().numpy(), 2.0)
+        assert np.array_equal(y[:rows].double().cpu().numpy(), ref)
+        grad, _, _ = V.embedding_bwd(host, ref, 30, 2.0)
+        assert np.allclose(d.double().cpu().numpy(), grad, rtol=1e-5, atol=1e-6)
