@@ -2328,7 +2328,7 @@ NNCONV_API nnconv_status nnconv_embedding_bwd(const nnconv_embedding_desc *desc,
 }
 
 static nnconv_status xent_check(const nnconv_xent_desc *d, XentParams *p) {
-    if (!d || d->rows < 0 || d->c < 1 || d->v < 1 || d->k < 1 || !__builtin_isfinite(d->logit_scale))
+    if (!d || d->rows < 0 || d->c < 1 || d->v < 1 || d->k < 1 || !__builtin_isfinite(d->logit_scale) || d->logit_scale == 0.0f)
         return NNCONV_ERR_INVALID_ARG;
     if (d->rows > MAX_ELEMS / d->c || d->rows > MAX_ELEMS / d->v || d->v > MAX_ELEMS / d->c)
         return NNCONV_ERR_INVALID_ARG;

@@ -14,21 +14,24 @@ namespace xent {
 
 constexpr int MOST_TARGETS = 1024;
 
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
 struct Rows {
     int64_t rows;
     int32_t c, ldx, v, k;
     const uint16_t *x, *w;
     int64_t ldw;
     const int32_t *targets;
-    const void *teacher;
+    const void *teacher;  // or null: labels
     float scale;
     uint16_t *xc;    // [rows][ldx]: x with zeros behind its channels and in rows that do not count
-    float *zt, *qt;  // [rows][k]: the targets' logits; what is taken from their softmax
-    float *base;     // [rows]: sum q (log q - z); NaN bits NOT_COUNTED in rows that do not count
+    float *zt, *qt;  // [rows][k]: the targets' logits, in units of log 2; what is taken from their softmax
+    float *base;     // [rows]: sum q (log q - z); the bits NOT_COUNTED in rows that do not count
 };
 
-// What `base` holds for a row that does not count.  Arithmetic makes no NaN with these bits.
+// What stands for a row that does not count.  Arithmetic makes no NaN with these bits.
 constexpr uint32_t NOT_COUNTED = 0x7FC0DEADu;
+__device__ __forceinline__ bool counted(float v) { return __builtin_bit_cast(uint32_t, v) != NOT_COUNTED; }
 
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
@@ -36,9 +39,52 @@ __device__ __forceinline__ float wave_sum(float v) {
     return v;
 }
 
-// A workgroup a row: the row's copy, the logits of its targets in fp32 (their own sums, since the
-// gradient takes q from a softmax value close to it), and the teacher's softmax.
+// 8 channels from `c` on of a row of n, zeros behind it.
+template <bool VEC>
+__device__ __forceinline__ u32x4 channels(const uint16_t *row, int c, int n) {
+    if constexpr (VEC) return *(const u32x4 *)(row + c);
+    u32x4 v = {};
+#pragma unroll
+    for (int d = 0; d < 8; ++d)
+        if (c + d < n) v[d >> 1] |= (uint32_t)row[c + d] << (16 * (d & 1));
+    return v;
+}
+
+// Labels: the copy of x, a thread 8 channels.
+template <bool VEC>
+__global__ __launch_bounds__(256) void copy_kernel(const Rows P) {
+    const uint32_t per = (uint32_t)P.ldx / 8;
+    const int64_t count = P.rows * per;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / per;
+        const int c = (int)(i - r * per) * 8;
+        const bool in = (uint32_t)P.targets[r] < (uint32_t)P.v;
+        *(u32x4 *)(P.xc + r * P.ldx + c) = in ? channels<VEC>(P.x + r * P.c, c, P.c) : u32x4{};
+    }
+}
+
+template <class T>
+__device__ __forceinline__ float dot8(u32x4 a, u32x4 b, float s) {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+        s = fmaf(from16<T>(a[d]), from16<T>(b[d]), s);
+        s = fmaf(from16<T>(a[d] >> 16), from16<T>(b[d] >> 16), s);
+    }
+    return s;
+}
+
 template <class T, class S>
+__device__ __forceinline__ float teacher_logit(const void *p, int64_t i) {
+    if constexpr (sizeof(S) == 4)
+        return ((const float *)p)[i];
+    else
+        return from16<T>(((const uint16_t *)p)[i]);
+}
+
+// A teacher: a workgroup a row.  The row's copy, the logits of its targets in fp32 (their own sums:
+// the products' tiles have them in many places), and the teacher's softmax.  A quarter wave has a
+// target: 16 lanes of 8 channels each.
+template <class T, class S, bool VEC>
 __global__ __launch_bounds__(256) void rows_kernel(const Rows P) {
     const int64_t r = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -46,20 +92,12 @@ __global__ __launch_bounds__(256) void rows_kernel(const Rows P) {
     __shared__ float part[4];
     const int k = P.k;
     const int32_t *t = P.targets + r * k;
-    const S *teacher = (const S *)P.teacher + r * k;
-    // the largest teacher's logit that counts
+    // the largest of the teacher's logits that count
     float most = -INFINITY;
     bool any = false, nan = false;
     for (int i = lane; i < k; i += 64) {
-        const bool in = (uint32_t)t[i] < (uint32_t)P.v;
-        float a = 0.f;
-        if (P.teacher) {
-            if constexpr (sizeof(S) == 4)
-                a = teacher[i] * P.scale;
-            else
-                a = from16<T>(teacher[i]) * P.scale;
-        }
-        if (!in || a == -INFINITY) continue;
+        const float a = teacher_logit<T, S>(P.teacher, r * k + i) * P.scale;
+        if ((uint32_t)t[i] >= (uint32_t)P.v || a == -INFINITY) continue;
         any = true;
         nan |= !(a == a);
         most = fmaxf(most, a);
@@ -71,37 +109,32 @@ __global__ __launch_bounds__(256) void rows_kernel(const Rows P) {
     uint16_t *xc = P.xc + r * P.ldx;
     const uint16_t *x = P.x + r * P.c;
     if (!any) {
-        for (int c = tid; c < P.ldx; c += 256) xc[c] = 0;
+        for (int c = tid * 8; c < P.ldx; c += 2048) *(u32x4 *)(xc + c) = u32x4{};
         for (int i = tid; i < k; i += 256) P.zt[r * k + i] = P.qt[r * k + i] = 0.f;
         if (tid == 0) P.base[r] = __builtin_bit_cast(float, NOT_COUNTED);
         return;
     }
-    for (int c = tid; c < P.ldx; c += 256) xc[c] = c < P.c ? x[c] : (uint16_t)0;
-    // q before its division, and the logits
+    for (int c = tid * 8; c < P.ldx; c += 2048) *(u32x4 *)(xc + c) = channels<VEC>(x, c, P.c);
     float sum = 0.f;
-    for (int i = wave; i < k; i += 4) {
-        const int32_t j = t[i];
-        const bool in = (uint32_t)j < (uint32_t)P.v;
-        float a = 0.f;
-        if (P.teacher) {
-            if constexpr (sizeof(S) == 4)
-                a = teacher[i] * P.scale;
-            else
-                a = from16<T>(teacher[i]) * P.scale;
-        }
-        const float e = !in || a == -INFINITY ? 0.f : expf(a - most);
-        float dot = 0.f;
-        if (in) {
-            const uint16_t *w = P.w + (int64_t)j * P.ldw;
-            for (int c = lane; c < P.c; c += 64) dot = fmaf(from16<T>(x[c]), from16<T>(w[c]), dot);
-        }
-        dot = wave_sum(dot) * P.scale;
-        if (lane == 0) {
-            q[i] = e;
-            z[i] = dot;
-        }
+    for (int i = tid; i < k; i += 256) {
+        const float a = teacher_logit<T, S>(P.teacher, r * k + i) * P.scale;
+        const float e = (uint32_t)t[i] >= (uint32_t)P.v || a == -INFINITY ? 0.f : expf(a - most);
+        q[i] = e;
         sum += e;
     }
+    const int l16 = lane & 15;
+    for (int i = tid >> 4; i < k; i += 16) {
+        const int32_t j = t[i];
+        float dot = 0.f;
+        if ((uint32_t)j < (uint32_t)P.v) {
+            const uint16_t *w = P.w + (int64_t)j * P.ldw;  // whole vectors, zeros behind the channels
+            for (int c = l16 * 8; c < P.ldx; c += 128) dot = dot8<T>(channels<VEC>(x, c, P.c), *(const u32x4 *)(w + c), dot);
+        }
+#pragma unroll
+        for (int d = 8; d > 0; d >>= 1) dot += __shfl_xor(dot, d);
+        if (l16 == 0) z[i] = dot * P.scale;
+    }
+    sum = wave_sum(sum);
     if (lane == 0) part[wave] = sum;
     __syncthreads();
     sum = part[0] + part[1] + part[2] + part[3];
@@ -111,16 +144,9 @@ __global__ __launch_bounds__(256) void rows_kernel(const Rows P) {
         const float e = q[i];
         float taken = 0.f;  // a target that is named twice is taken from once, with both shares
         for (int j = 0; j < k; ++j) taken += t[j] == t[i] ? q[j] : 0.f;
-        P.zt[r * k + i] = z[i];
+        P.zt[r * k + i] = z[i] * LOG2E;
         P.qt[r * k + i] = taken / sum;
-        float a = 0.f;
-        if (P.teacher) {
-            if constexpr (sizeof(S) == 4)
-                a = teacher[i] * P.scale;
-            else
-                a = from16<T>(teacher[i]) * P.scale;
-        }
-        if (e != 0.f) base += e / sum * (a - most - log_sum - z[i]);
+        if (e != 0.f) base += e / sum * (teacher_logit<T, S>(P.teacher, r * k + i) * P.scale - most - log_sum - z[i]);
     }
     __syncthreads();
     base = wave_sum(base);
@@ -128,40 +154,51 @@ __global__ __launch_bounds__(256) void rows_kernel(const Rows P) {
     __syncthreads();
     if (tid == 0) {
         base = part[0] + part[1] + part[2] + part[3];
-        if (nan) base = __builtin_nanf("");
-        P.base[r] = base;
+        P.base[r] = nan ? __builtin_nanf("") : base;
     }
 }
 
-// A wave a row: lse and loss; the tiles' largest logits become the factors of their exponentials.
-__global__ __launch_bounds__(256) void join_kernel(int64_t rows, int32_t tiles, float2 *stats, const float *base,
-                                                   float *lse, float *loss, float *lse_out, bool train) {
+struct Join {
+    int64_t rows;
+    int32_t tiles, v;
+    float2 *stats;
+    const int32_t *labels;  // or null
+    const float *zt, *base; // of labels; of a teacher
+    float *lse;             // in units of log 2, for scale_kernel; the bits NOT_COUNTED in rows that do not count
+    float *loss, *lse_out;
+};
+
+// A wave a row: lse and loss; in training the tiles' largest logits become the factors of their
+// exponentials.
+template <bool TRAIN>
+__global__ __launch_bounds__(256) void join_kernel(const Join P) {
     const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
-    if (r >= rows) return;
-    float2 *s = stats + r * tiles;
+    if (r >= P.rows) return;
+    float2 *s = P.stats + r * P.tiles;
     float most = -INFINITY;
-    for (int i = lane; i < tiles; i += 64) most = fmaxf(most, s[i].x);
+    for (int i = lane; i < P.tiles; i += 64) most = fmaxf(most, s[i].x);
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
     float sum = 0.f;
-    for (int i = lane; i < tiles; i += 64) {
+    for (int i = lane; i < P.tiles; i += 64) {
         const float2 v = s[i];
-        sum += v.y * expf(v.x == most ? 0.f : v.x - most);
+        sum += v.y * exp2f(v.x == most ? 0.f : v.x - most);
     }
     sum = wave_sum(sum);
-    const float b = base[r];
-    const bool counts = __builtin_bit_cast(uint32_t, b) != NOT_COUNTED;
-    const float total = most + logf(sum);
+    const bool counts = P.labels ? (uint32_t)P.labels[r] < (uint32_t)P.v : counted(P.base[r]);
     if (lane == 0) {
-        loss[r] = counts ? b + total : 0.f;
-        if (lse_out) lse_out[r] = counts ? total : 0.f;
-        if (train) lse[r] = total;
+        const float log_sum = log2f(sum);
+        // a label's logit is subtracted before the logarithm joins: near 0 both are small
+        const float loss = P.labels ? (most - P.zt[r] + log_sum) * LN2 : P.base[r] + (most + log_sum) * LN2;
+        P.loss[r] = counts ? loss : 0.f;
+        if (P.lse_out) P.lse_out[r] = counts ? (most + log_sum) * LN2 : 0.f;
+        if (TRAIN) P.lse[r] = counts ? most + log_sum : __builtin_bit_cast(float, NOT_COUNTED);
     }
-    if (!train) return;
+    if (!TRAIN) return;
     const float over = GRAD_UNIT / sum;
-    for (int i = lane; i < tiles; i += 64)
-        s[i].x = counts ? over * expf(s[i].x == most ? 0.f : s[i].x - most) : 0.f;
+    for (int i = lane; i < P.tiles; i += 64)
+        s[i].x = counts ? over * exp2f(s[i].x == most ? 0.f : s[i].x - most) : 0.f;
 }
 
 struct Scale {
@@ -170,7 +207,7 @@ struct Scale {
     uint16_t *e;
     const float2 *stats;
     const int32_t *targets;
-    const float *zt, *qt, *base, *lse;
+    const float *zt, *qt, *lse;  // qt null: 1
 };
 
 constexpr int SCALE_VECTORS = 4;  // of 8 elements a thread
@@ -183,7 +220,8 @@ __global__ __launch_bounds__(256) void scale_kernel(const Scale P) {
     const int64_t n0 = (int64_t)blockIdx.x * 256 * 8 * SCALE_VECTORS;
     uint16_t *e = P.e + r * P.lde;
     const float2 *s = P.stats + r * P.tiles;
-    const bool counts = __builtin_bit_cast(uint32_t, P.base[r]) != NOT_COUNTED;
+    const float lse = P.lse[r];
+    const bool counts = counted(lse);
 #pragma unroll
     for (int i = 0; i < SCALE_VECTORS; ++i) {
         const int64_t n = n0 + (i * 256 + threadIdx.x) * 8;
@@ -198,11 +236,11 @@ __global__ __launch_bounds__(256) void scale_kernel(const Scale P) {
     }
     if (!counts) return;
     __syncthreads();
-    const float lse = P.lse[r];
     for (int i = threadIdx.x; i < P.k; i += 256) {
         const int32_t j = P.targets[r * P.k + i];
         if ((uint32_t)j >= (uint32_t)P.v || j < n0 || j >= n0 + 256 * 8 * SCALE_VECTORS) continue;
-        e[j] = (uint16_t)to16<T>(GRAD_UNIT * (expf(P.zt[r * P.k + i] - lse) - P.qt[r * P.k + i]));
+        const float q = P.qt ? P.qt[r * P.k + i] : 1.f;
+        e[j] = (uint16_t)to16<T>(GRAD_UNIT * (exp2f(P.zt[r * P.k + i] - lse) - q));
     }
 }
 
@@ -219,29 +257,38 @@ struct Shape {
     int64_t k_split;
 };
 
-// 256-row tiles from one tile a compute unit up, else 128-row ones with the reduction split.
+// By an estimate of the time in us: rounds of workgroups (one 256 x 256 tile a compute unit, or two
+// 128 x 128 ones) of what a reduction element and a tile take, and the sums of the splits.  The
+// rates are those of long products, 1200 and 960 TFLOP/s over all units.
 static Shape shape_of(int64_t m, int64_t n, int64_t k, bool split) {
-    auto tiles = [&](int b) { return ((m + b - 1) / b) * ((n + b - 1) / b); };
-    Shape s = {TILE_256, 1, (k + 63) / 64 * 64};
-    if (tiles(256) >= CUS) return s;
-    s.cfg = TILE_128;
-    const int64_t t = tiles(128);
-    if (!split || t >= 2 * CUS) return s;
-    int64_t splits = 2 * CUS / t;
-    const int64_t most = (k + 511) / 512;  // of no less than 512 elements each
-    if (splits > most) splits = most;
-    if (splits > 16) splits = 16;
-    if (splits < 1) splits = 1;
-    s.k_split = ((k + splits - 1) / splits + 63) / 64 * 64;
-    s.splits = (int32_t)((k + s.k_split - 1) / s.k_split);
-    return s;
+    Shape best = {TILE_256, 1, (k + 63) / 64 * 64};
+    double least = 1e300;
+    for (int c = TILE_256; c <= TILE_128; ++c) {
+        const int64_t b = tile_rows((Config)c), slots = c == TILE_256 ? CUS : 2 * CUS;
+        const double per_k = c == TILE_256 ? 0.028 : 0.0175, per_tile = c == TILE_256 ? 6.0 : 4.0;
+        const int64_t tiles = ((m + b - 1) / b) * ((n + b - 1) / b);
+        for (int64_t s = 1; s <= (split ? 16 : 1); ++s) {
+            const int64_t ks = ((k + s - 1) / s + 63) / 64 * 64, splits = (k + ks - 1) / ks;
+            if (splits != s || (s > 1 && ks < 256)) continue;
+            const int64_t rounds = (tiles * splits + slots - 1) / slots;
+            // a 128 x 128 tile alone on its unit is faster than beside another
+            const double alone = c == TILE_128 && tiles * splits <= CUS ? 0.7 : 1.0;
+            double t = (double)rounds * ((double)ks * per_k * alone + per_tile);
+            if (splits > 1) t += 3.0 + (double)(m * n) * (8.0 * (double)splits + 4.0) / 5e6;
+            if (t < least) {
+                least = t;
+                best = {(Config)c, (int32_t)splits, ks};
+            }
+        }
+    }
+    return best;
 }
 
 struct Plan {
     int64_t ldx, ldw, lde, piece;
     Shape logits, dx, dw;
     int32_t tiles;  // stats a row
-    bool copy_w;
+    bool copy_w, copy_x;
     size_t xc, wc, zt, qt, base, lse, stats, e, part, acc, bytes;
 };
 
@@ -249,6 +296,9 @@ static Plan plan_of(const XentParams &p, bool train) {
     Plan q;
     q.ldx = q.ldw = (p.c + 7) / 8 * 8;
     q.copy_w = p.c % 8 != 0;
+    // rows that do not count may hold NaN, which the product for dw would meet; a teacher's rows are
+    // copied beside its softmax
+    q.copy_x = q.copy_w || p.sizes_only || p.teacher || (train && p.dw) || ((uintptr_t)p.x & 15) != 0;
     q.lde = ((int64_t)p.v + 63) / 64 * 64;
     q.piece = p.rows;
     if (train) {
@@ -267,7 +317,7 @@ static Plan plan_of(const XentParams &p, bool train) {
         at += align256(bytes);
         return was;
     };
-    q.xc = take((size_t)p.rows * q.ldx * 2);
+    q.xc = take(q.copy_x ? (size_t)p.rows * q.ldx * 2 : 0);
     q.wc = take(q.copy_w ? (size_t)p.v * q.ldw * 2 : 0);
     q.zt = take((size_t)p.rows * p.k * 4);
     q.qt = take((size_t)p.rows * p.k * 4);
@@ -287,12 +337,30 @@ static Plan plan_of(const XentParams &p, bool train) {
     return q;
 }
 
-template <class T>
-static void launch_rows(const Rows &r, int teacher_dtype, hipStream_t st) {
-    if (r.teacher && teacher_dtype != NNCONV_F32)
-        hipLaunchKernelGGL((rows_kernel<T, uint16_t>), dim3((uint32_t)r.rows), dim3(256), 0, st, r);
+template <class T, class S>
+static void launch_rows(const Rows &r, bool vec, hipStream_t st) {
+    if (vec)
+        hipLaunchKernelGGL((rows_kernel<T, S, true>), dim3((uint32_t)r.rows), dim3(256), 0, st, r);
     else
-        hipLaunchKernelGGL((rows_kernel<T, float>), dim3((uint32_t)r.rows), dim3(256), 0, st, r);
+        hipLaunchKernelGGL((rows_kernel<T, S, false>), dim3((uint32_t)r.rows), dim3(256), 0, st, r);
+}
+
+static void launch_rows(int dtype, int teacher_dtype, const Rows &r, hipStream_t st) {
+    const bool vec = r.c % 8 == 0 && ((uintptr_t)r.x & 15) == 0;
+    if (!r.teacher) {
+        const int64_t n = (r.rows * (r.ldx / 8) + 255) / 256;
+        const dim3 grid((uint32_t)(n < (1 << 20) ? n : (1 << 20)));
+        if (vec)
+            hipLaunchKernelGGL((copy_kernel<true>), grid, dim3(256), 0, st, r);
+        else
+            hipLaunchKernelGGL((copy_kernel<false>), grid, dim3(256), 0, st, r);
+        return;
+    }
+    const bool wide = teacher_dtype == NNCONV_F32;
+    if (dtype == Half::id)
+        wide ? launch_rows<Half, float>(r, vec, st) : launch_rows<Half, uint16_t>(r, vec, st);
+    else
+        wide ? launch_rows<BFloat, float>(r, vec, st) : launch_rows<BFloat, uint16_t>(r, vec, st);
 }
 
 }  // namespace xent
@@ -345,26 +413,42 @@ hipError_t launch_xent(const XentParams &p, bool train, hipStream_t st) {
     r.zt = at(q.zt);
     r.qt = at(q.qt);
     r.base = at(q.base);
-    if (p.dtype == Half::id)
-        launch_rows<Half>(r, p.teacher_dtype, st);
-    else
-        launch_rows<BFloat>(r, p.teacher_dtype, st);
+    const uint16_t *x = (const uint16_t *)p.x;
+    if (q.copy_x) {
+        launch_rows(p.dtype, p.teacher_dtype, r, st);
+        x = r.xc;
+    }
 
     const int tile = tile_rows(q.logits.cfg);
     for (int64_t r0 = 0; r0 < p.rows; r0 += q.piece) {
         const int64_t n = p.rows - r0 < q.piece ? p.rows - r0 : q.piece;
         Logits l;
-        l.x = {r.xc + r0 * q.ldx, q.ldx, (int32_t)n};
+        l.x = {x + r0 * q.ldx, q.ldx, (int32_t)n};
         l.w = {w, q.ldw, p.v};
         l.k = (int32_t)q.ldx;
-        l.scale = p.logit_scale;
+        l.unit = p.logit_scale * LOG2E;
+        l.labels = p.teacher ? nullptr : p.targets + r0;
+        l.zt = r.zt + r0;
         l.stats = (float2 *)(ws + q.stats);
         l.e = train ? (uint16_t *)(ws + q.e) : nullptr;
         l.lde = q.lde;
         hipError_t e = launch_logits(p.dtype, q.logits.cfg, l, st);
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL(join_kernel, dim3((uint32_t)((n + 3) / 4)), dim3(256), 0, st, n, q.tiles, l.stats, r.base + r0,
-                           at(q.lse), p.loss + r0, p.lse ? p.lse + r0 : nullptr, train);
+        Join j;
+        j.rows = n;
+        j.tiles = q.tiles;
+        j.v = p.v;
+        j.stats = l.stats;
+        j.labels = l.labels;
+        j.zt = l.zt;
+        j.base = r.base + r0;
+        j.lse = at(q.lse);
+        j.loss = p.loss + r0;
+        j.lse_out = p.lse ? p.lse + r0 : nullptr;
+        if (train)
+            hipLaunchKernelGGL((join_kernel<true>), dim3((uint32_t)((n + 3) / 4)), dim3(256), 0, st, j);
+        else
+            hipLaunchKernelGGL((join_kernel<false>), dim3((uint32_t)((n + 3) / 4)), dim3(256), 0, st, j);
         if (!train) continue;
         Scale s;
         s.v = p.v;
@@ -376,8 +460,7 @@ hipError_t launch_xent(const XentParams &p, bool train, hipStream_t st) {
         s.stats = l.stats;
         s.targets = p.targets + r0 * p.k;
         s.zt = r.zt + r0 * p.k;
-        s.qt = r.qt + r0 * p.k;
-        s.base = r.base + r0;
+        s.qt = p.teacher ? r.qt + r0 * p.k : nullptr;
         s.lse = at(q.lse);
         constexpr int64_t STRETCH = 256 * 8 * SCALE_VECTORS;
         for (int64_t y0 = 0; y0 < n; y0 += 32768) {  // rows of one launch
@@ -387,8 +470,7 @@ hipError_t launch_xent(const XentParams &p, bool train, hipStream_t st) {
             t.stats += y0 * q.tiles;
             t.targets += y0 * p.k;
             t.zt += y0 * p.k;
-            t.qt += y0 * p.k;
-            t.base += y0;
+            if (t.qt) t.qt += y0 * p.k;
             t.lse += y0;
             const dim3 grid((uint32_t)((q.lde + STRETCH - 1) / STRETCH), (uint32_t)ny);
             if (p.dtype == Half::id)

@@ -37,8 +37,10 @@ __device__ __forceinline__ float unpack_exp(uint32_t bits) {
 struct Logits {
     gemm::Operand x, w;  // [rows][k], [v][k]
     int32_t k;           // reduction elements
-    float scale;
-    float2 *stats;       // [rows][tiles_n]: largest, sum
+    float unit;          // logit_scale / log 2: what a product counts in units of log 2
+    const int32_t *labels;  // [rows] or null
+    float *zt;           // [rows]: the labels' logits, in units of log 2
+    float2 *stats;       // [rows][tiles_n]: largest, in units of log 2, and sum
     uint16_t *e;         // [rows][lde] or null
     int64_t lde;         // a multiple of 64, >= v
     int32_t tiles_m, tiles_n;

@@ -147,8 +147,8 @@ static hipError_t launch(bool atr, Grad p, hipStream_t st) {
 
 template <class T>
 static hipError_t launch_t(Config cfg, bool atr, const Grad &p, hipStream_t st) {
-    if (cfg == TILE_256) return launch<T, 256, 256, 2, 2, 32, 4, 1>(atr, p, st);
-    return launch<T, 128, 128, 2, 2, 32, 4, 2>(atr, p, st);
+    if (cfg == TILE_256) return launch<T, 256, 256, 2, 4, 64, 2, 2>(atr, p, st);
+    return launch<T, 128, 128, 2, 2, 64, 2, 2>(atr, p, st);
 }
 
 hipError_t launch_grad(int dtype, Config cfg, bool atr, Grad p, hipStream_t st) {

@@ -3,13 +3,15 @@
 // A tile's logits stay in registers: of each row the largest (in the lane's 16 values of each
 // block, then its other half's, then the other waves' through LDS) and the sum of the exponentials
 // against it go to memory, and in training the exponentials themselves, at most 1, in 16 bits.
+// Logits are counted in units of log 2, as the exponential instruction takes them: the largest is
+// rounded to fp32 in these units, and each exponential's argument is one fused step from it, so
+// that the sums belong to the very number that is stored.  The label's logit is taken from the
+// same product, so that a loss near 0 is the difference of equal numbers.
 #include "xent.hpp"
 
 namespace nnconv {
 
 namespace xent {
-
-constexpr float LOG2E = 1.4426950408889634f;
 
 template <class T, int BM, int BN, int WM, int WN, int BK, int STAGES, int OCC, bool KEEP>
 __global__ __launch_bounds__(WM * WN * 64, OCC) void logits_kernel(const Logits P) {
@@ -20,33 +22,67 @@ __global__ __launch_bounds__(WM * WN * 64, OCC) void logits_kernel(const Logits 
     __shared__ __attribute__((aligned(16))) char lds[LDS];
     __shared__ float red[2][WN][BM];
 
-    int tm, tn;
-    tile_of((int)xcd_remap(blockIdx.x, gridDim.x), P.tiles_m, P.tiles_n, tm, tn);
-    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
-    G g;
-    g.run(P.x, P.w, m0, n0, 0, P.k, lds);
-
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WM, wn = wave / WM;
     const int l32 = lane & 31, half = lane >> 5;
-    const int cols = P.w.extent - n0 < BN ? (int)(P.w.extent - n0) : BN;  // of the tile
-    const int c0 = wn * G::WTN + 4 * half;
+    int tm, tn;
+    tile_of((int)xcd_remap(blockIdx.x, gridDim.x), P.tiles_m, P.tiles_n, tm, tn);
+    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+    const int c0 = wn * G::WTN + 4 * half;  // the lane's first column
+    // where the label's logit is among the lane's, if it is
+    int label[FM];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        const int64_t m = m0 + wm * G::WTM + i * 32 + l32;
+        label[i] = P.labels && m < P.x.extent ? P.labels[m] : -1;
+    }
+    G g;
+    g.run(P.x, P.w, m0, n0, 0, P.k, lds);
 
-    float most[FM];
+    const int cols = P.w.extent - n0 < BN ? (int)(P.w.extent - n0) : BN;  // of the tile
+    if (P.unit < 0.f) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int u = 0; u < 16; ++u) g.acc[j][i][u] = -g.acc[j][i][u];
+    }
+    if (cols < BN) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int u = 0; u < 16; ++u)
+                if (c0 + j * 32 + 8 * (u >> 2) + (u & 3) >= cols) {
+#pragma unroll
+                    for (int i = 0; i < FM; ++i) g.acc[j][i][u] = -INFINITY;
+                }
+    }
+    const float unit = fabsf(P.unit);
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
         float v = -INFINITY;
 #pragma unroll
         for (int j = 0; j < FN; ++j)
 #pragma unroll
-            for (int u = 0; u < 16; ++u) {
-                float z = g.acc[j][i][u] * P.scale;
-                if (cols < BN && c0 + j * 32 + 8 * (u >> 2) + (u & 3) >= cols) z = -INFINITY;
-                g.acc[j][i][u] = z;
-                v = fmaxf(v, z);
-            }
-        most[i] = fmaxf(v, __shfl_xor(v, 32));
-        if (half == 0) red[0][wn][wm * G::WTM + i * 32 + l32] = most[i];
+            for (int u = 0; u < 16; ++u) v = fmaxf(v, g.acc[j][i][u]);
+        v = fmaxf(v, __shfl_xor(v, 32));
+        const int r = wm * G::WTM + i * 32 + l32;
+        if (half == 0) red[0][wn][r] = v;
+        const int64_t at = label[i] - n0 - c0;
+        if (!__any(label[i] >= 0 && at >= 0 && at < G::WTN)) continue;
+        bool mine = false;
+        float z = 0.f;
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int u = 0; u < 16; ++u)
+                if (at == j * 32 + 8 * (u >> 2) + (u & 3)) {
+                    mine = true;
+                    z = g.acc[j][i][u];
+                }
+        // another padding than -1 may lie in the tile's empty columns
+        if (mine && label[i] < P.w.extent && m0 + r < P.x.extent) P.zt[m0 + r] = z * unit;
     }
     barrier_lds();
 #pragma unroll
@@ -55,14 +91,13 @@ __global__ __launch_bounds__(WM * WN * 64, OCC) void logits_kernel(const Logits 
         float v = red[0][0][r];
 #pragma unroll
         for (int w = 1; w < WN; ++w) v = fmaxf(v, red[0][w][r]);
-        most[i] = v;
-        const float from = v == -INFINITY ? 0.f : v;  // a row of infinitely low logits
+        v = v == -INFINITY ? 0.f : v * unit;  // a row of infinitely low logits has sum 0
         float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < FN; ++j)
 #pragma unroll
             for (int u = 0; u < 16; ++u) {
-                const float e = __builtin_amdgcn_exp2f((g.acc[j][i][u] - from) * LOG2E);
+                const float e = __builtin_amdgcn_exp2f(fmaf(g.acc[j][i][u], unit, -v));
                 g.acc[j][i][u] = e;
                 sum += e;
             }
@@ -78,7 +113,7 @@ __global__ __launch_bounds__(WM * WN * 64, OCC) void logits_kernel(const Logits 
             v = fmaxf(v, red[0][w][r]);
             s += red[1][w][r];
         }
-        P.stats[(m0 + r) * P.tiles_n + tn] = float2{v, s};
+        P.stats[(m0 + r) * P.tiles_n + tn] = float2{v == -INFINITY ? v : v * unit, s};
     }
     if constexpr (KEEP) {
         // through LDS, 16-byte chunks swizzled by row, so that whole lines are stored
@@ -125,8 +160,8 @@ static hipError_t launch(Logits p, hipStream_t st) {
 
 template <class T>
 static hipError_t launch_t(Config cfg, const Logits &p, hipStream_t st) {
-    if (cfg == TILE_256) return launch<T, 256, 256, 2, 2, 32, 4, 1>(p, st);
-    return launch<T, 128, 128, 2, 2, 32, 4, 2>(p, st);
+    if (cfg == TILE_256) return launch<T, 256, 256, 2, 4, 64, 2, 2>(p, st);
+    return launch<T, 128, 128, 2, 2, 64, 2, 2>(p, st);
 }
 
 hipError_t launch_logits(int dtype, Config cfg, Logits p, hipStream_t st) {

@@ -203,3 +203,55 @@ def test_handle(nnlib, rows, c, v):
         assert t.equal(a.cpu(), ref[key].host())
     op.fwd(X, Wt, T, loss, teacher=Q)
     assert t.allclose(loss.cpu(), ref["loss"].host(), rtol=1e-5, atol=1e-5)
+
+
+@pytest.mark.parametrize("rows,c,v,dtype,k", [(600, 520, 20000, "bf16", None), (2100, 1100, 8300, "f16", None), (1500, 300, 3000, "f16", 9)])
+def test_large_tiles(nnlib, rows, c, v, dtype, k):
+    """Sizes whose products take 256 x 256 tiles, one and several a compute unit, and split reductions."""
+    rng = np.random.default_rng(rows)
+    x, w, targets, teacher = W.loss_inputs(rng, rows, c, v, dtype, k=k, pad=0.1)
+    got = W.loss_call(x, w, targets, teacher, dtype, 1.0)
+    W.check_loss(got, x, w, targets, teacher, dtype, 1.0)
+    again = W.loss_call(x, w, targets, teacher, dtype, 1.0, train=False)
+    assert np.allclose(again["loss"].f64(), got["loss"].f64(), rtol=1e-6, atol=1e-5)
+
+
+@pytest.mark.parametrize("scale", [-0.75, 2.0 ** -20, 3.0])
+def test_logit_scales(nnlib, scale):
+    rng = np.random.default_rng(14)
+    x, w, targets, teacher = W.loss_inputs(rng, 60, 40, 300, "f16", k=4)
+    W.check_loss(W.loss_call(x, w, targets, teacher, "f16", scale), x, w, targets, teacher, "f16", scale)
+    W.check_loss(W.loss_call(x, w, targets[:, :1], None, "f16", scale), x, w, targets[:, :1], None, "f16", scale)
+
+
+def test_pieces(nnlib):
+    """A vocabulary of which 256 rows fill the workspace's exponentials: dw joins over two pieces."""
+    t = U.torch()
+    g = t.Generator(device="cuda").manual_seed(3)
+    rows, c, v = 300, 8, 2 ** 21
+    w = t.randn((v, c), generator=g, device="cuda").half()
+    x = t.randn((rows, c), generator=g, device="cuda").half()
+    target = t.randint(0, v, (rows,), generator=g, device="cuda", dtype=t.int32)
+    target[7], target[299] = -1, v - 1
+    op = nc.CrossEntropy(rows, c, v)
+    loss, lse, dx = t.empty(rows, device="cuda"), t.empty(rows, device="cuda"), t.empty_like(x)
+    dw, dw32 = t.empty_like(w), t.full((v, c), 0.25, device="cuda")
+    op.train(x, w, target, loss, dx, dw, lse=lse, alpha=2.0 ** 12)
+    op.train(x, w, target, loss, dx, dw32, alpha=2.0 ** 12, accumulate=1)
+    live = target >= 0
+    z = x.double() @ w.double().t()
+    ref_lse = t.logsumexp(z, 1) * live
+    at = target.clamp(min=0).long()
+    ref_loss = (ref_lse - z.gather(1, at[:, None])[:, 0]) * live
+    # 2^-24 of a logit of 8 products and of lse, sums of 2^21 terms in chains of at most 400
+    assert float((lse - ref_lse).abs().max()) < 500 * 2.0 ** -24 + 20 * 2.0 ** -24 * float(z.abs().max())
+    assert float((loss - ref_loss).abs().max()) < 500 * 2.0 ** -24 + 40 * 2.0 ** -24 * float(z.abs().max())
+    p = z.sub_(ref_lse[:, None]).exp_().mul_(live[:, None])
+    p[t.arange(rows, device="cuda"), at] -= live.double()
+    p *= 2.0 ** 12
+    ref_dx, ref_dw = p @ w.double(), p.t() @ x.double()
+    # one rounding of each gradient of a logit, its storage before, and one of the result
+    for got, ref, mag in ((dx, ref_dx, p.abs() @ w.double().abs()), (dw, ref_dw, p.abs().t() @ x.double().abs()),
+                          (dw32 - 0.25, ref_dw, p.abs().t() @ x.double().abs() + 2.0 ** -12)):
+        bound = (2.0 ** -11 + 2.0 ** -12 + 2.0 ** -15) * mag + 2.0 ** -11 * ref.abs() + 2.0 ** -23 + 2.0 ** 12 * 2.0 ** -28
+        assert bool(((got.double() - ref).abs() <= bound).all())
