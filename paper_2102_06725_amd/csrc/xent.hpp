@@ -43,6 +43,7 @@ struct Logits {
     float2 *stats;       // [rows][tiles_n]: largest, in units of log 2, and sum
     uint16_t *e;         // [rows][lde] or null
     int64_t lde;         // a multiple of 64, >= v
+    bool stream;         // e past the caches
     int32_t tiles_m, tiles_n;
 };
 

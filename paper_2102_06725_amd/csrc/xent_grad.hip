@@ -39,8 +39,7 @@ template <class T, int BM, int BN, int WM, int WN, int BK, int STAGES, int OCC, 
 __global__ __launch_bounds__(WM * WN * 64, OCC) void grad_kernel(const Grad P) {
     typedef gemm::Tile<T, BM, BN, WM, WN, BK, STAGES, ATR, true> G;
     constexpr int FM = G::FM, FN = G::FN;
-    constexpr int ROWB = BN * 2;
-    constexpr int LDS = G::LDS_BYTES < BM * ROWB ? BM * ROWB : G::LDS_BYTES;
+    constexpr int LDS = G::LDS_BYTES < BM * BN * 2 ? BM * BN * 2 : G::LDS_BYTES;
     __shared__ __attribute__((aligned(16))) char lds[LDS];
 
     const int per = P.tiles_m * P.tiles_n;
@@ -81,34 +80,36 @@ __global__ __launch_bounds__(WM * WN * 64, OCC) void grad_kernel(const Grad P) {
         }
         return;
     }
-    barrier_lds();
-    constexpr int CPR = BN / 8;
-    bool bad = false;
+    barrier_lds();  // no wave reads operands any more
+    constexpr int CPR = G::WTN / 8, ROWB = G::WTN * 2;
+    char *own = lds + wave * (G::WTM * ROWB);
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
-        const int r = wm * G::WTM + i * 32 + l32;
+        const int r = i * 32 + l32;
 #pragma unroll
         for (int j = 0; j < FN; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int c = (wn * G::WTN + j * 32) / 8 + q;
                 const f32x16 &a = g.acc[j][i];
                 const u32x2 pk = {pack16<T>(a[4 * q] * factor, a[4 * q + 1] * factor),
                                   pack16<T>(a[4 * q + 2] * factor, a[4 * q + 3] * factor)};
-                *(u32x2 *)(lds + r * ROWB + ((c ^ (r & 15)) * 16) + half * 8) = pk;
+                *(u32x2 *)(own + r * ROWB + (((j * 4 + q) ^ (r & (CPR - 1))) * 16) + half * 8) = pk;
             }
     }
-    barrier_lds();
-    constexpr int PASS = WM * WN * 64 / CPR;
-    const int c = threadIdx.x % CPR;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int c = lane % CPR;
+    const int64_t n = n0 + wn * G::WTN + c * 8;
+    bool bad = false;
     constexpr uint32_t TOP = T::id == Half::id ? 0x7C00u : 0x7F80u;
-    for (int r = threadIdx.x / CPR; r < BM; r += PASS) {
-        if (m0 + r >= o.m || n0 + c * 8 >= o.n) continue;
-        const u32x4 v = *(const u32x4 *)(lds + r * ROWB + (c ^ (r & 15)) * 16);
+#pragma unroll 4
+    for (int r = lane / CPR; r < G::WTM; r += 64 / CPR) {
+        const int64_t m = m0 + wm * G::WTM + r;
+        const u32x4 v = *(const u32x4 *)(own + r * ROWB + (c ^ (r & (CPR - 1))) * 16);
+        if (m >= o.m || n >= o.n) continue;
 #pragma unroll
         for (int d = 0; d < 4; ++d)
             bad |= (v[d] & TOP) == TOP || ((v[d] >> 16) & TOP) == TOP;
-        __builtin_nontemporal_store(v, (u32x4 *)((uint16_t *)o.out + (m0 + r) * o.n + n0 + c * 8));
+        __builtin_nontemporal_store(v, (u32x4 *)((uint16_t *)o.out + m * o.n + n));
     }
     if (o.flag && bad) *o.flag = 1;
 }

@@ -17,8 +17,7 @@ template <class T, int BM, int BN, int WM, int WN, int BK, int STAGES, int OCC, 
 __global__ __launch_bounds__(WM * WN * 64, OCC) void logits_kernel(const Logits P) {
     typedef gemm::Tile<T, BM, BN, WM, WN, BK, STAGES, false, false> G;
     constexpr int FM = G::FM, FN = G::FN;
-    constexpr int ROWB = BN * 2;
-    constexpr int LDS = KEEP && G::LDS_BYTES < BM * ROWB ? BM * ROWB : G::LDS_BYTES;
+    constexpr int LDS = KEEP && G::LDS_BYTES < BM * BN * 2 ? BM * BN * 2 : G::LDS_BYTES;
     __shared__ __attribute__((aligned(16))) char lds[LDS];
     __shared__ float red[2][WN][BM];
 
@@ -116,28 +115,35 @@ __global__ __launch_bounds__(WM * WN * 64, OCC) void logits_kernel(const Logits 
         P.stats[(m0 + r) * P.tiles_n + tn] = float2{v == -INFINITY ? v : v * unit, s};
     }
     if constexpr (KEEP) {
-        // through LDS, 16-byte chunks swizzled by row, so that whole lines are stored
-        constexpr int CPR = BN / 8;
+        // through the wave's own part of LDS (behind the barriers above no wave reads operands there
+        // any more), 16-byte chunks swizzled by row, so that whole lines are stored
+        constexpr int CPR = G::WTN / 8, ROWB = G::WTN * 2;
+        char *own = lds + wave * (G::WTM * ROWB);
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
-            const int r = wm * G::WTM + i * 32 + l32;
+            const int r = i * 32 + l32;
 #pragma unroll
             for (int j = 0; j < FN; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int c = (wn * G::WTN + j * 32) / 8 + q;
                     const f32x16 &a = g.acc[j][i];
                     const u32x2 pk = {pack_exp<T>(a[4 * q], a[4 * q + 1]), pack_exp<T>(a[4 * q + 2], a[4 * q + 3])};
-                    *(u32x2 *)(lds + r * ROWB + ((c ^ (r & 15)) * 16) + half * 8) = pk;
+                    *(u32x2 *)(own + r * ROWB + (((j * 4 + q) ^ (r & (CPR - 1))) * 16) + half * 8) = pk;
                 }
         }
-        barrier_lds();
-        constexpr int PASS = WM * WN * 64 / CPR;
-        const int c = threadIdx.x % CPR;
-        for (int r = threadIdx.x / CPR; r < BM; r += PASS) {
-            if (m0 + r >= P.x.extent || n0 + c * 8 >= P.lde) continue;
-            const u32x4 v = *(const u32x4 *)(lds + r * ROWB + (c ^ (r & 15)) * 16);
-            *(u32x4 *)(P.e + (m0 + r) * P.lde + n0 + c * 8) = v;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const int c = lane % CPR;
+        const int64_t n = n0 + wn * G::WTN + c * 8;
+#pragma unroll 4
+        for (int r = lane / CPR; r < G::WTM; r += 64 / CPR) {
+            const int64_t m = m0 + wm * G::WTM + r;
+            const u32x4 v = *(const u32x4 *)(own + r * ROWB + (c ^ (r & (CPR - 1))) * 16);
+            if (m >= P.x.extent || n >= P.lde) continue;
+            u32x4 *to = (u32x4 *)(P.e + m * P.lde + n);
+            if (P.stream)
+                __builtin_nontemporal_store(v, to);
+            else
+                *to = v;
         }
     }
 }
