@@ -574,9 +574,9 @@ nnconv_status nnconv_adamw_update(const nnconv_adamw_plan *plan, int32_t *step, 
  * null pointers for what has none. */
 
 typedef struct {
-    int64_t rows;   /* tokens, 0 to 2^29 */
-    int32_t c;      /* channels, 1 to 2^28 */
-    int32_t v;      /* rows of the table, >= 1 */
+    int64_t rows;   /* tokens, 0 to 2^27 */
+    int32_t c;      /* channels, 1 to 2^24 */
+    int32_t v;      /* rows of the table, 1 to 2^29 */
     int32_t dtype;  /* F16 or BF16: table, y, dy */
     float scale;    /* finite: what a row is multiplied by */
 } nnconv_embedding_desc;
@@ -585,7 +585,7 @@ typedef struct {
  * y: [rows][c], dense.  16-byte aligned tables and outputs with c a multiple
  * of 8 are the fast ones.
  * INVALID_ARG: rows < 0, c < 1, v < 1, scale not finite, bad dtype, null
- * pointers; UNSUPPORTED: dtype F32, more tokens or channels; MISALIGNED:
+ * pointers; UNSUPPORTED: dtype F32, larger sizes; MISALIGNED:
  * pointers below their element size. */
 nnconv_status nnconv_embedding_fwd(const nnconv_embedding_desc *desc, const int32_t *ids,
                                    const void *table, void *y, void *hip_stream);

@@ -2,13 +2,18 @@
 //
 // Forward: a copy with a factor, bound by the bytes.  Backward: the tokens are sorted by number
 // (stable, so that the tokens of a row are added in their order and results are the same bits
-// every time), stretches of SPAN sorted tokens are summed by a workgroup each, and rows whose
-// tokens reach over several stretches are joined from their parts.
+// every time), spans of sorted tokens are summed by a team of threads each, and rows whose tokens
+// reach over several spans are joined from their parts.  The launches that sort wait for their own
+// loads and barriers mostly; further workgroups of theirs clear the table meanwhile, the rows that
+// tokens name too (32768 tokens of 1152 channels, 32768 rows in fp32: 75 us a backward pass, 84 with rows looked up and cleared beside the sums).
 #include "launch.hpp"
 
 namespace nnconv {
 
 namespace embedding {
+
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;  // 16 bytes at any element
+typedef f32x4 __attribute__((aligned(4))) f32x4_any;
 
 template <class T>
 __device__ __forceinline__ uint32_t scaled(uint32_t two, float f) {
@@ -39,13 +44,35 @@ __global__ __launch_bounds__(256) void fwd_kernel(const EmbeddingParams P) {
     }
 }
 
+// Bytes to clear by the workgroups behind the first `blocks` of a launch, CLEAR_BYTES each.
+struct Clear {
+    char *p;
+    int64_t bytes;  // even
+    uint32_t blocks;
+};
+constexpr int CLEAR_BYTES = 65536;
+
+// Whether this workgroup is one of them.
+__device__ __forceinline__ bool cleared(const Clear &c) {
+    if (blockIdx.x < c.blocks) return false;
+    const int64_t at = (int64_t)(blockIdx.x - c.blocks) * CLEAR_BYTES;
+    const int64_t left = c.bytes - at;
+    const int n = left < CLEAR_BYTES ? (int)left : CLEAR_BYTES;
+    for (int i = threadIdx.x * 16; i + 16 <= n; i += blockDim.x * 16)
+        __builtin_nontemporal_store(u32x4{}, (u32x4_any *)(c.p + at + i));
+    for (int i = n / 16 * 16 + threadIdx.x * 2; i < n; i += blockDim.x * 2) *(uint16_t *)(c.p + at + i) = 0;
+    return true;
+}
+
+__global__ __launch_bounds__(256) void clear_kernel(const Clear c) { cleared(c); }
+
 // --- sorting ---------------------------------------------------------------------------
 //
-// Passes over 8 bits of the number, least first.  A workgroup has TILE tokens, a wave a quarter
-// of them in their order; lanes with equal digits find each other by ballots, so that a token's
-// place among its equals is its order.
+// Passes over 8 bits of the number, least first.  A wave takes its tokens in their order; lanes
+// with equal digits find each other by ballots, so that a token's place among its equals is its
+// order.
 
-constexpr int BITS = 8, BINS = 1 << BITS, WAVES = 16, TILE = 4096, PER_WAVE = TILE / WAVES;
+constexpr int BITS = 8, BINS = 1 << BITS;
 
 // Number of the token that sorts; padding last.
 __device__ __forceinline__ uint32_t key_of(int32_t id, int32_t v) { return (uint32_t)id < (uint32_t)v ? (uint32_t)id : (uint32_t)v; }
@@ -62,211 +89,413 @@ __device__ __forceinline__ uint64_t equals(uint32_t digit, bool live) {
     return m;
 }
 
-struct Sort {
-    int64_t rows;
-    int32_t v, shift, blocks;
-    const int32_t *ids;          // first pass
-    const uint32_t *key, *row;   // later passes
-    uint32_t *key_out, *row_out;
-    uint32_t *counts;            // [BINS][blocks]
-};
-
-// COUNT: the digits of each workgroup's tokens; else their places (counts are running sums then).
-template <bool FIRST, bool COUNT>
-__global__ __launch_bounds__(64 * WAVES) void sort_kernel(const Sort P) {
-    __shared__ uint32_t seen[WAVES][BINS];
+// Each token's place among the workgroup's of its digit; `seen` is, behind a barrier, for each wave
+// and digit the tokens of the waves before, and `sum` the digit's in all (of thread = digit).
+template <int WAVES, int R>
+__device__ __forceinline__ uint32_t rank(const uint32_t (&key)[R], const bool (&live)[R], int shift, uint32_t (&place)[R],
+                                         uint32_t (*seen)[BINS]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int i = threadIdx.x; i < WAVES * BINS; i += 64 * WAVES) seen[i / BINS][i % BINS] = 0;
     __syncthreads();
-    const int64_t first = (int64_t)blockIdx.x * TILE + wave * PER_WAVE;
-    uint32_t key[PER_WAVE / 64], place[PER_WAVE / 64];
 #pragma unroll
-    for (int s = 0; s < PER_WAVE / 64; ++s) {
-        const int64_t i = first + s * 64 + lane;
-        const bool live = i < P.rows;
-        key[s] = live ? (FIRST ? key_of(P.ids[i], P.v) : P.key[i]) : 0;
-        const uint32_t digit = (key[s] >> P.shift) & (BINS - 1);
-        const uint64_t m = equals(digit, live);
+    for (int s = 0; s < R; ++s) {
+        const uint32_t digit = (key[s] >> shift) & (BINS - 1);
+        const uint64_t m = equals(digit, live[s]);
         const uint32_t before = __popcll(m & (((uint64_t)1 << lane) - 1));
-        // every lane reads the count before the first of its equals adds to it (one wave, in order)
+        // every lane reads the count before the first of its equals adds to it
         place[s] = seen[wave][digit] + before;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (live && before == 0) seen[wave][digit] += (uint32_t)__popcll(m);
+        if (live[s] && before == 0) seen[wave][digit] += (uint32_t)__popcll(m);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
     __syncthreads();
+    uint32_t sum = 0;
     if (threadIdx.x < BINS) {
-        uint32_t sum = 0;
         for (int w = 0; w < WAVES; ++w) {
             const uint32_t n = seen[w][threadIdx.x];
             seen[w][threadIdx.x] = sum;
             sum += n;
         }
-        if constexpr (COUNT)
-            P.counts[(int64_t)threadIdx.x * P.blocks + blockIdx.x] = sum;
-        else {
-            const uint32_t base = P.counts[(int64_t)threadIdx.x * P.blocks + blockIdx.x];
-            for (int w = 0; w < WAVES; ++w) seen[w][threadIdx.x] += base;
-        }
     }
-    if constexpr (!COUNT) {
+    return sum;
+}
+
+// Sum over the threads before (256 of them), of all of them in `all`.
+__device__ __forceinline__ uint32_t scan256(uint32_t n, uint32_t *waves) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t scan = n;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t o = __shfl_up(scan, d);
+        if (lane >= d) scan += o;
+    }
+    if (lane == 63 && wave < 4) waves[wave] = scan;
+    __syncthreads();
+    uint32_t before = scan - n;
+#pragma unroll
+    for (int w = 0; w < 3; ++w)
+        if (w < wave) before += waves[w];
+    return before;
+}
+
+// Up to ONE tokens: all passes by one workgroup, through LDS (5003 tokens: 15 us).
+constexpr int ONE_ROUNDS = 8, ONE = 1024 * ONE_ROUNDS;
+
+template <int R>
+__global__ __launch_bounds__(1024) void sort_one_kernel(const int32_t *ids, int32_t rows, int32_t v, int bits, uint32_t *key_out,
+                                                        uint32_t *row_out, const Clear clear) {
+    __shared__ uint32_t seen[16][BINS], waves[4];
+    __shared__ uint32_t keys[1024 * R];
+    __shared__ uint16_t from[1024 * R];
+    if (cleared(clear)) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t key[R], row[R], place[R];
+    bool live[R];
+#pragma unroll
+    for (int s = 0; s < R; ++s) {
+        const int i = wave * 64 * R + s * 64 + lane;
+        live[s] = i < rows;
+        key[s] = live[s] ? key_of(ids[i], v) : 0;
+        row[s] = (uint32_t)i;
+    }
+    for (int shift = 0; shift < bits; shift += BITS) {
+        const uint32_t sum = rank<16, R>(key, live, shift, place, seen);
+        const uint32_t base = scan256(sum, waves);
+        if (threadIdx.x < BINS)
+            for (int w = 0; w < 16; ++w) seen[w][threadIdx.x] += base;
         __syncthreads();
 #pragma unroll
-        for (int s = 0; s < PER_WAVE / 64; ++s) {
-            const int64_t i = first + s * 64 + lane;
-            if (i >= P.rows) continue;
-            const uint32_t to = seen[wave][(key[s] >> P.shift) & (BINS - 1)] + place[s];
-            P.key_out[to] = key[s];
-            P.row_out[to] = FIRST ? (uint32_t)i : P.row[i];
+        for (int s = 0; s < R; ++s)
+            if (live[s]) {
+                const uint32_t to = seen[wave][(key[s] >> shift) & (BINS - 1)] + place[s];
+                keys[to] = key[s];
+                from[to] = (uint16_t)row[s];
+            }
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < R; ++s) {
+            const int i = wave * 64 * R + s * 64 + lane;
+            if (live[s]) {
+                key[s] = keys[i];
+                row[s] = from[i];
+            }
         }
+    }
+#pragma unroll
+    for (int s = 0; s < R; ++s) {
+        const int i = wave * 64 * R + s * 64 + lane;
+        if (!live[s]) continue;
+        key_out[i] = key[s];
+        row_out[i] = row[s];
     }
 }
 
-// counts -> running sums over (digit, workgroup), by one workgroup.
-__global__ __launch_bounds__(1024) void sort_scan_kernel(uint32_t *counts, int64_t n) {
-    __shared__ uint32_t wave_sums[16];
+// More: a pass counts the digits of each workgroup's tokens and moves them in a second launch, whose
+// workgroups add up the counts in front of theirs themselves (32768 tokens, 2 passes: 21 us).
+// From MANY workgroups on they would read too much, and a launch between adds the counts up.
+constexpr int ROUNDS = 4, MANY = 128;
+
+struct Sort {
+    int64_t rows;
+    int32_t v, shift, blocks;
+    bool summed;                 // counts are places already
+    const int32_t *ids;          // first pass
+    const uint32_t *key, *row;   // later passes
+    uint32_t *key_out, *row_out;
+    uint32_t *counts;            // [blocks][BINS]
+    Clear clear;
+};
+
+template <bool FIRST>
+__device__ __forceinline__ uint32_t key_at(const Sort &P, int64_t i) {
+    return FIRST ? key_of(P.ids[i], P.v) : P.key[i];
+}
+
+template <int WAVES, bool FIRST>
+__global__ __launch_bounds__(64 * WAVES) void count_kernel(const Sort P) {
+    __shared__ uint32_t seen[WAVES][BINS];
+    if (cleared(P.clear)) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint32_t carry = 0;
-    for (int64_t i0 = 0; i0 < n; i0 += 4096) {
-        const int64_t i = i0 + threadIdx.x * 4;
-        uint32_t c[4];
+    const int64_t first = (int64_t)blockIdx.x * (64 * WAVES * ROUNDS) + wave * 64 * ROUNDS;
+    uint32_t key[ROUNDS], place[ROUNDS];
+    bool live[ROUNDS];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) c[u] = i + u < n ? counts[i + u] : 0;
-        uint32_t sum = c[0] + c[1] + c[2] + c[3], scan = sum;
+    for (int s = 0; s < ROUNDS; ++s) {
+        const int64_t i = first + s * 64 + lane;
+        live[s] = i < P.rows;
+        key[s] = live[s] ? key_at<FIRST>(P, i) : 0;
+    }
+    const uint32_t sum = rank<WAVES, ROUNDS>(key, live, P.shift, place, seen);
+    if (threadIdx.x < BINS) P.counts[(int64_t)blockIdx.x * BINS + threadIdx.x] = sum;
+}
+
+// counts -> places, by one workgroup of a thread a digit.
+__global__ __launch_bounds__(256) void place_kernel(uint32_t *counts, int32_t blocks) {
+    __shared__ uint32_t waves[4];
+    uint32_t sum = 0;
+#pragma unroll 8
+    for (int b = 0; b < blocks; ++b) sum += counts[(int64_t)b * BINS + threadIdx.x];
+    uint32_t at = scan256(sum, waves);
+#pragma unroll 8
+    for (int b = 0; b < blocks; ++b) {
+        const uint32_t n = counts[(int64_t)b * BINS + threadIdx.x];
+        counts[(int64_t)b * BINS + threadIdx.x] = at;
+        at += n;
+    }
+}
+
+template <int WAVES, bool FIRST>
+__global__ __launch_bounds__(64 * WAVES) void sort_kernel(const Sort P) {
+    __shared__ uint32_t seen[WAVES][BINS], waves[4];
+    if (cleared(P.clear)) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t first = (int64_t)blockIdx.x * (64 * WAVES * ROUNDS) + wave * 64 * ROUNDS;
+    uint32_t key[ROUNDS], row[ROUNDS], place[ROUNDS];
+    bool live[ROUNDS];
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t o = __shfl_up(scan, d);
-            if (lane >= d) scan += o;
+    for (int s = 0; s < ROUNDS; ++s) {
+        const int64_t i = first + s * 64 + lane;
+        live[s] = i < P.rows;
+        key[s] = live[s] ? key_at<FIRST>(P, i) : 0;
+        row[s] = live[s] ? (FIRST ? (uint32_t)i : P.row[i]) : 0;
+    }
+    uint32_t before = 0, total = 0;
+    if (threadIdx.x < BINS) {
+        if (P.summed)
+            before = P.counts[(int64_t)blockIdx.x * BINS + threadIdx.x];
+        else {
+#pragma unroll 8
+            for (int b = 0; b < P.blocks; ++b) {
+                const uint32_t n = P.counts[(int64_t)b * BINS + threadIdx.x];
+                total += n;
+                before += b < (int)blockIdx.x ? n : 0;
+            }
         }
-        if (lane == 63) wave_sums[wave] = scan;
-        __syncthreads();
-        uint32_t before = carry, all = 0;
+    }
+    rank<WAVES, ROUNDS>(key, live, P.shift, place, seen);
+    before += scan256(total, waves);
+    if (threadIdx.x < BINS)
+        for (int w = 0; w < WAVES; ++w) seen[w][threadIdx.x] += before;
+    __syncthreads();
 #pragma unroll
-        for (int w = 0; w < 16; ++w) {
-            if (w < wave) before += wave_sums[w];
-            all += wave_sums[w];
-        }
-        before += scan - sum;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (i + u < n) counts[i + u] = before;
-            before += c[u];
-        }
-        carry += all;
-        __syncthreads();
+    for (int s = 0; s < ROUNDS; ++s) {
+        if (!live[s]) continue;
+        const uint32_t to = seen[wave][(key[s] >> P.shift) & (BINS - 1)] + place[s];
+        P.key_out[to] = key[s];
+        P.row_out[to] = row[s];
     }
 }
 
 // --- sums ------------------------------------------------------------------------------
 
-constexpr int SPAN = 64;  // sorted tokens of a workgroup
+// Sorted tokens of a team, a multiple of 8: 32, and 8 where there are few, since each row's end is a
+// round trip to memory where it is added to what is there (5003 tokens of 771 channels: 39 us a
+// backward pass with 8, 52 with 16, 81 with 32; 32768 of 1152: 95 with 8, 86 with 16, 84 with 32).
+constexpr int SPAN = 32, SMALL_SPAN = 8;
+constexpr int64_t FEW_TOKENS = 16384;
+constexpr int LEAST_TEAM = 4;   // threads of one, of 8 channels each
 
 struct Sums {
     int64_t rows;
-    int32_t c, v, kind;     // kind: Half::id, BFloat::id or 2: fp32
+    int32_t c, cp, v, kind;  // cp: c in whole vectors; kind: Half::id, BFloat::id or 2: fp32
+    int32_t team, span;      // threads, a power of two; tokens
     const uint32_t *key, *row;
     const uint16_t *dy;
     void *dtable;
     float factor;
     int32_t accumulate;
     int32_t *flag;
-    float *part;            // [2 * spans][c]: of a span, what belongs to the row of the span before, and to the next's
+    float *part;             // [2 * spans][cp]: of a span, what belongs to the row of the span before, and to the next's
 };
 
-__device__ __forceinline__ void put(const Sums &P, int64_t i, float v) {
-    v *= P.factor;
+// 8 values of row `j` from channel c on to the gradient.
+__device__ __forceinline__ void put8(const Sums &P, int64_t j, int c, const float (&s)[8]) {
+    const int64_t i = j * P.c + c;
+    const int n = P.c - c < 8 ? P.c - c : 8;
+    float v[8];
+    bool bad = false;
+#pragma unroll
+    for (int d = 0; d < 8; ++d) v[d] = s[d] * P.factor;
     if (P.kind == 2) {
         float *o = (float *)P.dtable + i;
-        if (P.accumulate) v += *o;
-        *o = v;
-        if (P.flag && !__builtin_isfinite(v)) *P.flag = 1;
-        return;
+        if (n == 8) {
+            f32x4 lo = {v[0], v[1], v[2], v[3]}, hi = {v[4], v[5], v[6], v[7]};
+            if (P.accumulate) {
+                lo += *(const f32x4_any *)o;
+                hi += *(const f32x4_any *)(o + 4);
+            }
+            *(f32x4_any *)o = lo;
+            *(f32x4_any *)(o + 4) = hi;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) bad |= !__builtin_isfinite(lo[d]) || !__builtin_isfinite(hi[d]);
+        } else
+            for (int d = 0; d < n; ++d) {
+                float x = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x = e == d ? v[e] : x;
+                if (P.accumulate) x += o[d];
+                o[d] = x;
+                bad |= !__builtin_isfinite(x);
+            }
+    } else {
+        uint16_t *o = (uint16_t *)P.dtable + i;
+        const bool half = P.kind == Half::id;
+        u32x4 old = {}, out;
+        if (P.accumulate) {
+            if (n == 8)
+                old = *(const u32x4_any *)o;
+            else
+#pragma unroll
+                for (int d = 0; d < 8; ++d)
+                    if (d < n) old[d >> 1] |= (uint32_t)o[d] << (16 * (d & 1));
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                v[2 * d] += half ? from16<Half>(old[d]) : from16<BFloat>(old[d]);
+                v[2 * d + 1] += half ? from16<Half>(old[d] >> 16) : from16<BFloat>(old[d] >> 16);
+            }
+        }
+        const uint32_t top = half ? 0x7C00u : 0x7F80u;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+            out[d] = half ? pack16<Half>(v[2 * d], v[2 * d + 1]) : pack16<BFloat>(v[2 * d], v[2 * d + 1]);
+            bad |= (2 * d < n && (out[d] & top) == top) || (2 * d + 1 < n && ((out[d] >> 16) & top) == top);
+        }
+        if (n == 8)
+            *(u32x4_any *)o = out;
+        else
+#pragma unroll
+            for (int d = 0; d < 8; ++d)
+                if (d < n) o[d] = (uint16_t)(out[d >> 1] >> (16 * (d & 1)));
     }
-    uint16_t *o = (uint16_t *)P.dtable + i;
-    if (P.accumulate) v += P.kind == Half::id ? from16<Half>(*o) : from16<BFloat>(*o);
-    *o = (uint16_t)(P.kind == Half::id ? to16<Half>(v) : to16<BFloat>(v));
-    if (P.flag && !__builtin_isfinite(P.kind == Half::id ? from16<Half>(*o) : from16<BFloat>(*o))) *P.flag = 1;
+    if (bad && P.flag) *P.flag = 1;
 }
 
-// Workgroup (span, 256 channels): runs of equal numbers.  A run that begins in this span and ends
-// in it is a row's whole sum.
+// Workgroups of teams, a span each: runs of equal numbers.  A run that begins and ends in its span
+// is a row's whole sum.  Loads of 8 tokens are on their way at once.
 template <class T>
 __global__ __launch_bounds__(256) void sum_kernel(const Sums P) {
-    __shared__ uint32_t key[SPAN + 2], row[SPAN];  // key[0] and key[SPAN + 1]: the neighbours'
-    const int64_t at = (int64_t)blockIdx.x * SPAN;
-    const int n = P.rows - at < SPAN ? (int)(P.rows - at) : SPAN;
-    if (threadIdx.x < (uint32_t)n) {
-        key[threadIdx.x + 1] = P.key[at + threadIdx.x];
-        row[threadIdx.x] = P.row[at + threadIdx.x];
+    __shared__ uint32_t key[256 / LEAST_TEAM * SPAN + 2], row[256 / LEAST_TEAM * SPAN];  // key[0]: the one before
+    const int teams = 256 / P.team;
+    const int64_t first = (int64_t)blockIdx.x * teams * P.span;
+    const int all = P.rows - first < teams * P.span ? (int)(P.rows - first) : teams * P.span;
+    for (int i = threadIdx.x; i < all; i += 256) {
+        key[i + 1] = P.key[first + i];
+        row[i] = P.row[first + i];
     }
-    if (threadIdx.x == 64) key[0] = at > 0 ? P.key[at - 1] : ~0u;
-    if (threadIdx.x == 65) key[n + 1] = at + n < P.rows ? P.key[at + n] : ~0u;
+    if (threadIdx.x == 0) {
+        key[0] = first > 0 ? P.key[first - 1] : ~0u;
+        key[all + 1] = first + all < P.rows ? P.key[first + all] : ~0u;
+    }
     __syncthreads();
-    for (int64_t c = (int64_t)blockIdx.y * 256 + threadIdx.x; c < P.c; c += (int64_t)gridDim.y * 256) {
-        float sum = 0.f;
-        bool begun = key[0] == key[1];  // the run reaches in from the span before
-        for (int i = 0; i < n; ++i) {
-            if (key[i + 1] >= (uint32_t)P.v) break;  // padding is sorted last
-            sum += from16<T>(P.dy[(int64_t)row[i] * P.c + c]);
-            if (key[i + 1] == key[i + 2] && i + 1 < n) continue;
-            if (begun)
-                P.part[(2 * (int64_t)blockIdx.x) * P.c + c] = sum;
-            else if (key[i + 1] == key[i + 2])
-                P.part[(2 * (int64_t)blockIdx.x + 1) * P.c + c] = sum;
+    const int team = threadIdx.x / P.team;
+    const int c = ((int)blockIdx.y * 256 + (threadIdx.x & (P.team - 1))) * 8;
+    const int begin = team * P.span, n = all - begin < P.span ? all - begin : P.span;
+    if (n <= 0 || c >= P.c) return;
+    const int64_t span = (int64_t)blockIdx.x * teams + team;
+    const uint32_t *k = key + 1 + begin;
+    const bool whole = c + 8 <= P.c;
+    float sum[8] = {};
+    bool begun = k[-1] == k[0];  // the run reaches in from the span before
+    for (int i0 = 0; i0 < n; i0 += 8) {
+        u32x4 v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            v[u] = u32x4{};
+            if (i0 + u >= n || k[i0 + u] >= (uint32_t)P.v) continue;  // padding is not read
+            const uint16_t *src = P.dy + (int64_t)row[begin + i0 + u] * P.c + c;
+            if (whole)
+                v[u] = *(const u32x4_any *)src;
             else
-                put(P, (int64_t)key[i + 1] * P.c + c, sum);
-            sum = 0.f;
+#pragma unroll
+                for (int d = 0; d < 7; ++d)
+                    if (c + d < P.c) v[u][d >> 1] |= (uint32_t)src[d] << (16 * (d & 1));
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int i = i0 + u;
+            if (i >= n || k[i] >= (uint32_t)P.v) break;  // padding is sorted last
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                sum[2 * d] += from16<T>(v[u][d]);
+                sum[2 * d + 1] += from16<T>(v[u][d] >> 16);
+            }
+            const bool on = k[i + 1] == k[i];
+            if (on && i + 1 < n) continue;
+            if (begun || on) {
+                float *to = P.part + (2 * span + (begun ? 0 : 1)) * P.cp + c;
+                *(f32x4 *)to = f32x4{sum[0], sum[1], sum[2], sum[3]};
+                *(f32x4 *)(to + 4) = f32x4{sum[4], sum[5], sum[6], sum[7]};
+            } else
+                put8(P, k[i], c, sum);
+#pragma unroll
+            for (int d = 0; d < 8; ++d) sum[d] = 0.f;
             begun = false;
         }
     }
 }
 
-// Workgroup (span, 256 channels): the row whose run begins in this span and goes on behind it.
-__global__ __launch_bounds__(256) void join_kernel(const Sums P, int64_t spans) {
-    const int64_t s = blockIdx.x, last = s * SPAN + SPAN - 1;
+// A workgroup a span: the row whose run begins in it and goes on behind it.
+__global__ __launch_bounds__(256) void join_kernel(const Sums P) {
+    const int64_t s = blockIdx.x, last = s * P.span + P.span - 1;
     if (last + 1 >= P.rows) return;
     const uint32_t k = P.key[last];
     if (k >= (uint32_t)P.v || P.key[last + 1] != k) return;
-    if (s * SPAN > 0 && P.key[s * SPAN] == k && P.key[s * SPAN - 1] == k) return;  // begins before
-    for (int64_t c = (int64_t)blockIdx.y * 256 + threadIdx.x; c < P.c; c += (int64_t)gridDim.y * 256) {
-        float sum = P.part[(2 * s + 1) * P.c + c];
-        for (int64_t i = s + 1; i < spans && P.key[i * SPAN] == k; ++i) sum += P.part[2 * i * P.c + c];
-        put(P, (int64_t)k * P.c + c, sum);
+    if (s > 0 && P.key[s * P.span] == k && P.key[s * P.span - 1] == k) return;  // begins before
+    int64_t more = 0;  // spans behind this one that it reaches into
+    for (;; more += 64) {
+        const int64_t i = (s + 1 + more + (threadIdx.x & 63)) * P.span;
+        const uint64_t in = __ballot(i < P.rows && P.key[i < P.rows ? i : 0] == k);
+        if (in != ~(uint64_t)0) {
+            more += __builtin_ctzll(~in);
+            break;
+        }
     }
-}
-
-// Rows of the table that no token names.
-__global__ __launch_bounds__(256) void clear_kernel(const Sums P) {
-    for (int64_t j = blockIdx.x; j < P.v; j += gridDim.x) {
-        int64_t lo = 0, hi = P.rows;
-        while (lo < hi) {
-            const int64_t mid = (lo + hi) / 2;
-            if (P.key[mid] < (uint32_t)j)
-                lo = mid + 1;
-            else
-                hi = mid;
+    for (int c = ((int)blockIdx.y * 256 + threadIdx.x) * 8; c < P.c; c += (int)gridDim.y * 256 * 8) {
+        const float *from = P.part + (2 * s + 1) * P.cp + c;
+        f32x4 lo = *(const f32x4 *)from, hi = *(const f32x4 *)(from + 4);
+        const float *next = P.part + 2 * (s + 1) * P.cp + c;
+        const int64_t step = 2 * (int64_t)P.cp;
+        int64_t i = 0;
+        for (; i + 8 <= more; i += 8, next += 8 * step) {
+            f32x4 a[8], b[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                a[u] = *(const f32x4 *)(next + u * step);
+                b[u] = *(const f32x4 *)(next + u * step + 4);
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                lo += a[u];
+                hi += b[u];
+            }
         }
-        if (lo < P.rows && P.key[lo] == (uint32_t)j) continue;
-        for (int64_t c = threadIdx.x; c < P.c; c += 256) {
-            if (P.kind == 2)
-                ((float *)P.dtable)[j * P.c + c] = 0.f;
-            else
-                ((uint16_t *)P.dtable)[j * P.c + c] = 0;
+        for (; i < more; ++i, next += step) {
+            lo += *(const f32x4 *)next;
+            hi += *(const f32x4 *)(next + 4);
         }
+        const float sum[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        put8(P, k, c, sum);
     }
 }
 
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 
 struct Layout {
-    int64_t blocks, spans;
+    int waves;  // of a sorting workgroup; 0: one workgroup sorts
+    int32_t blocks;
+    int64_t spans;
+    int32_t cp, span;
     size_t key[2], row[2], counts, part, bytes;
 };
 
 static Layout layout_of(int64_t rows, int32_t c) {
     Layout l;
-    l.blocks = (rows + TILE - 1) / TILE;
-    l.spans = (rows + SPAN - 1) / SPAN;
+    l.waves = rows <= ONE ? 0 : rows <= (int64_t)MANY * 64 * 4 * ROUNDS ? 4 : 16;
+    const int64_t tile = 64 * l.waves * ROUNDS;
+    l.blocks = l.waves ? (int32_t)((rows + tile - 1) / tile) : 0;
+    l.cp = (c + 7) / 8 * 8;
+    l.span = rows <= FEW_TOKENS ? SMALL_SPAN : SPAN;
+    l.spans = (rows + l.span - 1) / l.span;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t was = at;
@@ -278,9 +507,55 @@ static Layout layout_of(int64_t rows, int32_t c) {
         l.row[i] = take((size_t)rows * 4);
     }
     l.counts = take((size_t)l.blocks * BINS * 4);
-    l.part = take((size_t)l.spans * 2 * c * 4);
+    l.part = take((size_t)l.spans * 2 * l.cp * 4);
     l.bytes = at;
     return l;
+}
+
+// Takes the next of `parts` parts of what is left to clear, behind `blocks` workgroups; the grid.
+static dim3 with_clear(Clear &all, Clear &part, uint32_t blocks, int parts) {
+    int64_t n = (all.bytes / parts + CLEAR_BYTES - 1) / CLEAR_BYTES * CLEAR_BYTES;
+    if (n > all.bytes) n = all.bytes;
+    part = {all.p, n, blocks};
+    all.p += n;
+    all.bytes -= n;
+    return dim3(blocks + (uint32_t)((n + CLEAR_BYTES - 1) / CLEAR_BYTES));
+}
+
+template <int WAVES, bool FIRST>
+static void sort_pass(Sort &q, Clear &all, int parts, hipStream_t st) {
+    const dim3 block(64 * WAVES);
+    const dim3 counting = with_clear(all, q.clear, (uint32_t)q.blocks, parts);
+    hipLaunchKernelGGL((count_kernel<WAVES, FIRST>), counting, block, 0, st, q);
+    if (q.summed) hipLaunchKernelGGL(place_kernel, dim3(1), dim3(256), 0, st, q.counts, q.blocks);
+    const dim3 sorting = with_clear(all, q.clear, (uint32_t)q.blocks, parts - 1);
+    hipLaunchKernelGGL((sort_kernel<WAVES, FIRST>), sorting, block, 0, st, q);
+}
+
+template <int WAVES>
+static void sort_passes(Sort q, Clear &all, const Layout &l, char *ws, int bits, int &from, hipStream_t st) {
+    q.counts = (uint32_t *)(ws + l.counts);
+    q.summed = WAVES == 16;
+    int parts = 2 * ((bits + BITS - 1) / BITS);
+    for (q.shift = 0; q.shift < bits; q.shift += BITS, parts -= 2) {
+        q.key = (const uint32_t *)(ws + l.key[from]);
+        q.row = (const uint32_t *)(ws + l.row[from]);
+        from ^= 1;
+        q.key_out = (uint32_t *)(ws + l.key[from]);
+        q.row_out = (uint32_t *)(ws + l.row[from]);
+        if (q.shift == 0)
+            sort_pass<WAVES, true>(q, all, parts, st);
+        else
+            sort_pass<WAVES, false>(q, all, parts, st);
+    }
+}
+
+template <int R>
+static void sort_one(const Sort &q, Clear &all, const Layout &l, char *ws, int bits, hipStream_t st) {
+    Clear part;
+    const dim3 grid = with_clear(all, part, 1, 1);
+    hipLaunchKernelGGL((sort_one_kernel<R>), grid, dim3(1024), 0, st, q.ids, (int32_t)q.rows, q.v, bits,
+                       (uint32_t *)(ws + l.key[0]), (uint32_t *)(ws + l.row[0]), part);
 }
 
 }  // namespace embedding
@@ -318,48 +593,48 @@ hipError_t launch_embedding_bwd(int dtype, const EmbeddingParams &p, hipStream_t
     s.flag = p.flag;
     char *ws = (char *)p.ws;
     const Layout l = layout_of(p.rows, p.c);
-    int from = 0;
-    if (p.rows > 0) {
-        int bits = 1;  // of the largest key, which is v
-        while (bits < 32 && ((uint32_t)p.v >> bits) != 0) ++bits;
-        Sort q;
-        q.rows = p.rows;
-        q.v = p.v;
-        q.blocks = (int32_t)l.blocks;
-        q.ids = p.ids;
-        q.counts = (uint32_t *)(ws + l.counts);
-        const dim3 grid((uint32_t)l.blocks), block(64 * WAVES);
-        for (int shift = 0; shift < bits; shift += BITS) {
-            q.shift = shift;
-            q.key = (const uint32_t *)(ws + l.key[from]);
-            q.row = (const uint32_t *)(ws + l.row[from]);
-            from ^= 1;
-            q.key_out = (uint32_t *)(ws + l.key[from]);
-            q.row_out = (uint32_t *)(ws + l.row[from]);
-            if (shift == 0)
-                hipLaunchKernelGGL((sort_kernel<true, true>), grid, block, 0, st, q);
-            else
-                hipLaunchKernelGGL((sort_kernel<false, true>), grid, block, 0, st, q);
-            hipLaunchKernelGGL(sort_scan_kernel, dim3(1), dim3(1024), 0, st, q.counts, l.blocks * BINS);
-            if (shift == 0)
-                hipLaunchKernelGGL((sort_kernel<true, false>), grid, block, 0, st, q);
-            else
-                hipLaunchKernelGGL((sort_kernel<false, false>), grid, block, 0, st, q);
-        }
+    Clear all = {(char *)p.dtable, p.accumulate ? 0 : (int64_t)p.v * p.c * (p.dtable_dtype == NNCONV_F32 ? 4 : 2), 0};
+    if (p.rows == 0) {
+        Clear part;
+        const dim3 grid = with_clear(all, part, 0, 1);
+        if (grid.x > 0) hipLaunchKernelGGL(clear_kernel, grid, dim3(256), 0, st, part);
+        return hipGetLastError();
     }
+    int bits = 1;  // of the largest key, which is v
+    while (bits < 32 && ((uint32_t)p.v >> bits) != 0) ++bits;
+    Sort q = {};
+    q.rows = p.rows;
+    q.v = p.v;
+    q.blocks = l.blocks;
+    q.ids = p.ids;
+    int from = 0;
+    if (l.waves == 4)
+        sort_passes<4>(q, all, l, ws, bits, from, st);
+    else if (l.waves == 16)
+        sort_passes<16>(q, all, l, ws, bits, from, st);
+    else if (p.rows <= 1024)
+        sort_one<1>(q, all, l, ws, bits, st);
+    else if (p.rows <= 4096)
+        sort_one<4>(q, all, l, ws, bits, st);
+    else
+        sort_one<ONE_ROUNDS>(q, all, l, ws, bits, st);
     s.key = (const uint32_t *)(ws + l.key[from]);
     s.row = (const uint32_t *)(ws + l.row[from]);
     s.part = (float *)(ws + l.part);
-    if (!p.accumulate)
-        hipLaunchKernelGGL(clear_kernel, dim3((uint32_t)(p.v < 65536 ? p.v : 65536)), dim3(256), 0, st, s);
-    if (p.rows > 0) {
-        const int64_t cols = (p.c + 255) / 256;
-        const dim3 grid((uint32_t)l.spans, (uint32_t)(cols < 64 ? cols : 64));
-        if (dtype == Half::id)
-            hipLaunchKernelGGL((sum_kernel<Half>), grid, dim3(256), 0, st, s);
-        else
-            hipLaunchKernelGGL((sum_kernel<BFloat>), grid, dim3(256), 0, st, s);
-        hipLaunchKernelGGL(join_kernel, grid, dim3(256), 0, st, s, l.spans);
+    s.cp = l.cp;
+    s.span = l.span;
+    const int32_t vectors = l.cp / 8;
+    s.team = LEAST_TEAM;
+    while (s.team < vectors && s.team < 256) s.team *= 2;
+    const int64_t teams = 256 / s.team;
+    const dim3 grid((uint32_t)((l.spans + teams - 1) / teams), (uint32_t)((vectors + 255) / 256));
+    if (dtype == Half::id)
+        hipLaunchKernelGGL((sum_kernel<Half>), grid, dim3(256), 0, st, s);
+    else
+        hipLaunchKernelGGL((sum_kernel<BFloat>), grid, dim3(256), 0, st, s);
+    if (l.spans > 1) {
+        const uint32_t cols = grid.y < 64 ? grid.y : 64;
+        hipLaunchKernelGGL(join_kernel, dim3((uint32_t)l.spans, cols), dim3(256), 0, st, s);
     }
     return hipGetLastError();
 }

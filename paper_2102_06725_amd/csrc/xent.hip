@@ -158,89 +158,111 @@ __global__ __launch_bounds__(256) void rows_kernel(const Rows P) {
     }
 }
 
+// The tiles' statistics of rows, and what becomes of them.
 struct Join {
     int64_t rows;
-    int32_t tiles, v;
-    float2 *stats;
-    const int32_t *labels;  // or null
-    const float *zt, *base; // of labels; of a teacher
-    float *lse;             // in units of log 2, for scale_kernel; the bits NOT_COUNTED in rows that do not count
-    float *loss, *lse_out;
+    int32_t tiles, tile, v, k;  // tile: columns
+    const float2 *stats;
+    const int32_t *targets;     // [rows][k]
+    const float *zt;            // the targets' logits, in units of log 2
+    const float *qt, *base;     // a teacher's shares and sums; null with labels
+    float *loss, *lse;          // lse may be null
+    uint16_t *e;                // training: [rows][lde]
+    int64_t lde, stretch;       // elements of a workgroup
+    int32_t parts;              // workgroups of a row
 };
 
-// A wave a row: lse and loss; in training the tiles' largest logits become the factors of their
-// exponentials.
-template <bool TRAIN>
-__global__ __launch_bounds__(256) void join_kernel(const Join P) {
-    const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+// The largest logit of a row, and the sum of the exponentials against it, by one wave.
+__device__ __forceinline__ void join_row(const float2 *s, int tiles, float &most, float &sum) {
     const int lane = threadIdx.x & 63;
-    if (r >= P.rows) return;
-    float2 *s = P.stats + r * P.tiles;
-    float most = -INFINITY;
-    for (int i = lane; i < P.tiles; i += 64) most = fmaxf(most, s[i].x);
+    most = -INFINITY;
+    for (int i = lane; i < tiles; i += 64) most = fmaxf(most, s[i].x);
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
-    float sum = 0.f;
-    for (int i = lane; i < P.tiles; i += 64) {
+    sum = 0.f;
+    for (int i = lane; i < tiles; i += 64) {
         const float2 v = s[i];
         sum += v.y * exp2f(v.x == most ? 0.f : v.x - most);
     }
     sum = wave_sum(sum);
-    const bool counts = P.labels ? (uint32_t)P.labels[r] < (uint32_t)P.v : counted(P.base[r]);
-    if (lane == 0) {
-        const float log_sum = log2f(sum);
-        // a label's logit is subtracted before the logarithm joins: near 0 both are small
-        const float loss = P.labels ? (most - P.zt[r] + log_sum) * LN2 : P.base[r] + (most + log_sum) * LN2;
-        P.loss[r] = counts ? loss : 0.f;
-        if (P.lse_out) P.lse_out[r] = counts ? (most + log_sum) * LN2 : 0.f;
-        if (TRAIN) P.lse[r] = counts ? most + log_sum : __builtin_bit_cast(float, NOT_COUNTED);
-    }
-    if (!TRAIN) return;
-    const float over = GRAD_UNIT / sum;
-    for (int i = lane; i < P.tiles; i += 64)
-        s[i].x = counts ? over * exp2f(s[i].x == most ? 0.f : s[i].x - most) : 0.f;
 }
 
-struct Scale {
-    int32_t v, k, tile, tiles;
-    int64_t lde;
-    uint16_t *e;
-    const float2 *stats;
-    const int32_t *targets;
-    const float *zt, *qt, *lse;  // qt null: 1
-};
+__device__ __forceinline__ bool row_counts(const Join &P, int64_t r) {
+    return P.base ? counted(P.base[r]) : (uint32_t)P.targets[r] < (uint32_t)P.v;
+}
 
-constexpr int SCALE_VECTORS = 4;  // of 8 elements a thread
+__device__ __forceinline__ void put_loss(const Join &P, int64_t r, bool counts, float most, float log_sum) {
+    // a label's logit is subtracted before the logarithm joins: near 0 both are small
+    const float loss = P.base ? P.base[r] + (most + log_sum) * LN2 : (most - P.zt[r] + log_sum) * LN2;
+    P.loss[r] = counts ? loss : 0.f;
+    if (P.lse) P.lse[r] = counts ? (most + log_sum) * LN2 : 0.f;
+}
 
-// e -> 2^15 (softmax - q), a workgroup a stretch of a row: all of it by the tiles' factors, then
-// the targets from their own logits.
+// A wave a row.
+__global__ __launch_bounds__(256) void join_kernel(const Join P) {
+    const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (r >= P.rows) return;
+    float most, sum;
+    join_row(P.stats + r * P.tiles, P.tiles, most, sum);
+    const bool counts = row_counts(P, r);
+    if ((threadIdx.x & 63) == 0) put_loss(P, r, counts, most, log2f(sum));
+}
+
+// A workgroup a stretch of a row, one or at most SHARE of them: each joins the row's statistics
+// itself (a launch for it took 4 us of a small step's 58), all of the stretch is scaled by its
+// tiles' factors, then the targets are written from their own logits.  Bound by its 4 bytes an
+// element (5.2 TB/s on 1 GiB).
+constexpr int64_t STRETCH = 8192, SHARE = 8;
+
 template <class T>
-__global__ __launch_bounds__(256) void scale_kernel(const Scale P) {
-    const int64_t r = blockIdx.y;
-    const int64_t n0 = (int64_t)blockIdx.x * 256 * 8 * SCALE_VECTORS;
+__global__ __launch_bounds__(256) void scale_kernel(const Join P) {
+    const int64_t r = blockIdx.x / P.parts;
+    const int part = (int)(blockIdx.x - r * P.parts);
+    const int64_t n0 = part * P.stretch, n1 = n0 + P.stretch < P.lde ? n0 + P.stretch : P.lde;
     uint16_t *e = P.e + r * P.lde;
     const float2 *s = P.stats + r * P.tiles;
-    const float lse = P.lse[r];
-    const bool counts = counted(lse);
+    u32x4 v[4];
+    auto load = [&](int64_t i) {
 #pragma unroll
-    for (int i = 0; i < SCALE_VECTORS; ++i) {
-        const int64_t n = n0 + (i * 256 + threadIdx.x) * 8;
-        if (n >= P.lde) continue;
-        u32x4 v = *(const u32x4 *)(e + n);
-        const float f = s[n / P.tile].x;
-        // a row that does not count has zeros, whatever became of its exponentials
+        for (int u = 0; u < 4; ++u)
+            if (i + u * 2048 < n1) v[u] = *(const u32x4 *)(e + i + u * 2048);
+    };
+    int64_t i = n0 + threadIdx.x * 8;
+    load(i);  // on their way meanwhile
+    const bool counts = row_counts(P, r);
+    float most, sum;
+    join_row(s, P.tiles, most, sum);
+    const float log_sum = log2f(sum), over = GRAD_UNIT / sum;
+    if (part == 0 && threadIdx.x == 0) put_loss(P, r, counts, most, log_sum);
+    for (;;) {
+        float f[4];
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
-            v[d] = counts ? pack16<T>(unpack_exp<T>(v[d]) * f, unpack_exp<T>(v[d] >> 16) * f) : 0u;
-        *(u32x4 *)(e + n) = v;
+        for (int u = 0; u < 4; ++u) {
+            const int64_t n = i + u * 2048;
+            const float m = n < n1 ? s[n / P.tile].x : most;
+            f[u] = over * exp2f(m == most ? 0.f : m - most);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int64_t n = i + u * 2048;
+            if (n >= n1) continue;
+            // a row that does not count has zeros, whatever became of its exponentials
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+                v[u][d] = counts ? pack16<T>(unpack_exp<T>(v[u][d]) * f[u], unpack_exp<T>(v[u][d] >> 16) * f[u]) : 0u;
+            *(u32x4 *)(e + n) = v[u];
+        }
+        i += STRETCH;
+        if (i >= n1) break;
+        load(i);
     }
     if (!counts) return;
     __syncthreads();
     for (int i = threadIdx.x; i < P.k; i += 256) {
         const int32_t j = P.targets[r * P.k + i];
-        if ((uint32_t)j >= (uint32_t)P.v || j < n0 || j >= n0 + 256 * 8 * SCALE_VECTORS) continue;
+        if ((uint32_t)j >= (uint32_t)P.v || j < n0 || j >= n1) continue;
         const float q = P.qt ? P.qt[r * P.k + i] : 1.f;
-        e[j] = (uint16_t)to16<T>(GRAD_UNIT * (exp2f(P.zt[r * P.k + i] - lse) - q));
+        e[j] = (uint16_t)to16<T>(GRAD_UNIT * (exp2f(P.zt[r * P.k + i] - most - log_sum) - q));
     }
 }
 
@@ -262,6 +284,7 @@ struct Shape {
 // rates are those of long products, 1200 and 960 TFLOP/s over all units.
 static Shape shape_of(int64_t m, int64_t n, int64_t k, bool split) {
     Shape best = {TILE_256, 1, (k + 63) / 64 * 64};
+    if (!split && m <= 32) return {TILE_32, 1, best.k_split};
     double least = 1e300;
     for (int c = TILE_256; c <= TILE_128; ++c) {
         const int64_t b = tile_rows((Config)c), slots = c == TILE_256 ? CUS : 2 * CUS;
@@ -289,7 +312,7 @@ struct Plan {
     Shape logits, dx, dw;
     int32_t tiles;  // stats a row
     bool copy_w, copy_x;
-    size_t xc, wc, zt, qt, base, lse, stats, e, part, acc, bytes;
+    size_t xc, wc, zt, qt, base, stats, e, part, acc, bytes;
 };
 
 static Plan plan_of(const XentParams &p, bool train) {
@@ -309,7 +332,7 @@ static Plan plan_of(const XentParams &p, bool train) {
     q.logits = shape_of(q.piece, p.v, p.c, false);
     q.dx = shape_of(q.piece, p.c, q.lde, true);
     q.dw = shape_of(p.v, p.c, q.piece, true);
-    const int tile = tile_rows(q.logits.cfg);
+    const int tile = tile_cols(q.logits.cfg);
     q.tiles = (int32_t)(((int64_t)p.v + tile - 1) / tile);
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -323,9 +346,8 @@ static Plan plan_of(const XentParams &p, bool train) {
     q.qt = take((size_t)p.rows * p.k * 4);
     q.base = take((size_t)p.rows * 4);
     q.stats = take((size_t)q.piece * q.tiles * 8);
-    q.lse = q.e = q.part = q.acc = at;
+    q.e = q.part = q.acc = at;
     if (train) {
-        q.lse = take((size_t)q.piece * 4);
         q.e = take((size_t)q.piece * q.lde * 2);
         size_t part = q.dx.splits > 1 ? (size_t)q.dx.splits * q.piece * p.c : 0;
         const size_t w = q.dw.splits > 1 ? (size_t)q.dw.splits * p.v * p.c : 0;
@@ -419,7 +441,7 @@ hipError_t launch_xent(const XentParams &p, bool train, hipStream_t st) {
         x = r.xc;
     }
 
-    const int tile = tile_rows(q.logits.cfg);
+    const int tile = tile_cols(q.logits.cfg);
     for (int64_t r0 = 0; r0 < p.rows; r0 += q.piece) {
         const int64_t n = p.rows - r0 < q.piece ? p.rows - r0 : q.piece;
         Logits l;
@@ -440,47 +462,30 @@ hipError_t launch_xent(const XentParams &p, bool train, hipStream_t st) {
         Join j;
         j.rows = n;
         j.tiles = q.tiles;
+        j.tile = tile;
         j.v = p.v;
+        j.k = p.k;
         j.stats = l.stats;
-        j.labels = l.labels;
-        j.zt = l.zt;
-        j.base = r.base + r0;
-        j.lse = at(q.lse);
+        j.targets = p.targets + r0 * p.k;
+        j.zt = r.zt + r0 * p.k;
+        j.qt = p.teacher ? r.qt + r0 * p.k : nullptr;
+        j.base = p.teacher ? r.base + r0 : nullptr;
         j.loss = p.loss + r0;
-        j.lse_out = p.lse ? p.lse + r0 : nullptr;
-        if (train)
-            hipLaunchKernelGGL((join_kernel<true>), dim3((uint32_t)((n + 3) / 4)), dim3(256), 0, st, j);
-        else
-            hipLaunchKernelGGL((join_kernel<false>), dim3((uint32_t)((n + 3) / 4)), dim3(256), 0, st, j);
-        if (!train) continue;
-        Scale s;
-        s.v = p.v;
-        s.k = p.k;
-        s.tile = tile;
-        s.tiles = q.tiles;
-        s.lde = q.lde;
-        s.e = l.e;
-        s.stats = l.stats;
-        s.targets = p.targets + r0 * p.k;
-        s.zt = r.zt + r0 * p.k;
-        s.qt = p.teacher ? r.qt + r0 * p.k : nullptr;
-        s.lse = at(q.lse);
-        constexpr int64_t STRETCH = 256 * 8 * SCALE_VECTORS;
-        for (int64_t y0 = 0; y0 < n; y0 += 32768) {  // rows of one launch
-            Scale t = s;
-            const int64_t ny = n - y0 < 32768 ? n - y0 : 32768;
-            t.e += y0 * q.lde;
-            t.stats += y0 * q.tiles;
-            t.targets += y0 * p.k;
-            t.zt += y0 * p.k;
-            if (t.qt) t.qt += y0 * p.k;
-            t.lse += y0;
-            const dim3 grid((uint32_t)((q.lde + STRETCH - 1) / STRETCH), (uint32_t)ny);
-            if (p.dtype == Half::id)
-                hipLaunchKernelGGL((scale_kernel<Half>), grid, dim3(256), 0, st, t);
-            else
-                hipLaunchKernelGGL((scale_kernel<BFloat>), grid, dim3(256), 0, st, t);
+        j.lse = p.lse ? p.lse + r0 : nullptr;
+        j.e = l.e;
+        j.lde = q.lde;
+        if (!train) {
+            hipLaunchKernelGGL(join_kernel, dim3((uint32_t)((n + 3) / 4)), dim3(256), 0, st, j);
+            continue;
         }
+        j.stretch = (q.lde + SHARE - 1) / SHARE;
+        j.stretch = (j.stretch + STRETCH - 1) / STRETCH * STRETCH;
+        j.parts = (int32_t)((q.lde + j.stretch - 1) / j.stretch);
+        const dim3 grid((uint32_t)(n * j.parts));  // 2^23 at most: a piece has 2^29 elements, or 256 rows
+        if (p.dtype == Half::id)
+            hipLaunchKernelGGL((scale_kernel<Half>), grid, dim3(256), 0, st, j);
+        else
+            hipLaunchKernelGGL((scale_kernel<BFloat>), grid, dim3(256), 0, st, j);
         const float alpha = p.alpha * p.logit_scale / GRAD_UNIT;
         Grad g;
         g.a = {l.e, q.lde, (int32_t)n};

@@ -3,8 +3,8 @@
 //
 //   logits   z = scale * x w^T by tiles; of each tile's rows the largest z and the sum of
 //            exp(z - largest), and in training e = exp(z - largest) in fp16
-//   join     lse, loss, and a factor of each row and tile that turns its e into 2^15 softmax(z)
-//   scale    e -> 2^15 (softmax(z) - q) in the operand type, in place
+//   join     lse and loss of the tiles' statistics
+//   scale    the same, and e -> 2^15 (softmax(z) - q) in the operand type, in place
 //   grad     dx = d w, dw = d^T x
 #pragma once
 
@@ -71,9 +71,10 @@ struct Grad {
     int32_t tiles_m, tiles_n;
 };
 
-// Tile of a product: rows and columns.
-enum Config { TILE_256 = 0, TILE_128 = 1 };
-inline int tile_rows(Config c) { return c == TILE_256 ? 256 : 128; }
+// Tiles of a product: 256 x 256, 128 x 128, and for the logits of a few rows 32 x 128.
+enum Config { TILE_256 = 0, TILE_128 = 1, TILE_32 = 2 };
+inline int tile_rows(Config c) { return c == TILE_256 ? 256 : c == TILE_128 ? 128 : 32; }
+inline int tile_cols(Config c) { return c == TILE_256 ? 256 : 128; }
 
 hipError_t launch_logits(int dtype, Config cfg, Logits p, hipStream_t st);
 // atr: a is read along its rows (the reduction's elements are p[k * ld + m]).

@@ -166,6 +166,7 @@ static hipError_t launch(Logits p, hipStream_t st) {
 
 template <class T>
 static hipError_t launch_t(Config cfg, const Logits &p, hipStream_t st) {
+    if (cfg == TILE_32) return launch<T, 32, 128, 1, 4, 64, 4, 2>(p, st);
     if (cfg == TILE_256) return launch<T, 256, 256, 2, 4, 64, 2, 2>(p, st);
     return launch<T, 128, 128, 2, 2, 64, 2, 2>(p, st);
 }

@@ -83,7 +83,7 @@ def test_bwd(nnlib, rows, c, v, dtype, pad, shift, tied, wide):
     check(backward(ids, dy, v, dtype, 1.5, kind, old, 2.0 ** -4, shift), ids, dy, v, 1.5, kind, old, 2.0 ** -4)
 
 
-@pytest.mark.parametrize("rows,v", [(1, 100000), (64, 64), (128, 2), (129, 2), (20000, 3), (8192, 2 ** 21)])
+@pytest.mark.parametrize("rows,v", [(1, 100000), (64, 64), (128, 2), (129, 2), (20000, 3), (8192, 2 ** 21), (140001, 70000), (131073, 100), (1025, 300)])
 def test_orders(nnlib, rows, v):
     """All tokens alike, in rising and falling order, and numbers of every width."""
     rng = np.random.default_rng(rows)
