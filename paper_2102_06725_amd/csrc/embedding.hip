@@ -597,7 +597,8 @@ hipError_t launch_embedding_bwd(int dtype, const EmbeddingParams &p, hipStream_t
     if (p.rows == 0) {
         Clear part;
         const dim3 grid = with_clear(all, part, 0, 1);
-        if (grid.x > 0) hipLaunchKernelGGL(clear_kernel, grid, dim3(256), 0, st, part);
+        if (grid.x == 0) return hipSuccess;
+        hipLaunchKernelGGL(clear_kernel, grid, dim3(256), 0, st, part);
         return hipGetLastError();
     }
     int bits = 1;  // of the largest key, which is v

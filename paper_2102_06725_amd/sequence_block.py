@@ -6,8 +6,9 @@ Each block is a pre-norm residual block:
     thirds (value, forget gate, output gate);  x = projection back to c of y
 
 with 1x1 convolutions over NHWC images of height 1 and width t as the projections, and a last norm and
-projection behind the blocks.  `SequenceModel` keeps fp32 masters, 16-bit working weights, gradients and
-moments in flat arrays.  A training step is loss-scaled and stays on the device: forward, backward, AdamW
+projection behind the blocks.  `GatedBlocks` keeps fp32 masters, 16-bit working weights, gradients and
+moments in flat arrays; `SequenceModel` adds projections at both ends (a model over a vocabulary is in
+`token_model.py`).  A training step is loss-scaled and stays on the device: forward, backward, AdamW
 (8-bit moments for the matrices, 32-bit ones for gains and biases), the loss scaler's step.  It
 queues kernels only, so it can be captured into a graph.  `Server` runs one token of every
 sequence at a time, with the recurrence's states updated in place.
@@ -23,20 +24,21 @@ from . import nnconv as nc
 ALIGN = 64  # elements: tensors of the flat arrays start at a block of 8-bit moments
 
 
-class SequenceModel:
-    """c_in input channels, `blocks` blocks of c channels, c_out outputs; channel counts in multiples of 8."""
+class GatedBlocks:
+    """`blocks` gated blocks of c channels between two ends that a subclass adds: parameters (those of
+    `first` and `last`, [(name, shape, weight decay)], before and behind the blocks'), activations, the
+    loss scaler and the solver.  c is a multiple of 8."""
 
-    def __init__(self, n, t, c_in, c, c_out, blocks, dtype=nc.NNCONV_BF16, seed=0, loss_scale=1024.0, weight_decay=0.01,
-                 device="cuda"):
+    def __init__(self, n, t, c, blocks, first, last, dtype, seed, loss_scale, weight_decay, device):
         import torch
-        self.n, self.t, self.c_in, self.c, self.c_out, self.blocks = n, t, c_in, c, c_out, blocks
+        self.n, self.t, self.c, self.blocks = n, t, c, blocks
         self.code, self.device = dtype, device
         self.dtype = torch.float16 if dtype == nc.NNCONV_F16 else torch.bfloat16
-        self.layout = [("embed", (c, 1, 1, c_in), weight_decay)]
+        self.layout = list(first)
         for b in range(blocks):
             self.layout += [("gain%d" % b, (c,), 0.0), ("in%d" % b, (3 * c, 1, 1, c), weight_decay),
                             ("bias%d" % b, (c,), 0.0), ("out%d" % b, (c, 1, 1, c), weight_decay)]
-        self.layout += [("gain", (c,), 0.0), ("head", (c_out, 1, 1, c), weight_decay)]
+        self.layout += [("gain", (c,), 0.0)] + list(last)
         self._parameters(torch.Generator().manual_seed(seed))
         self.scaler = torch.zeros(6, dtype=torch.int32, device=device)
         nc.check(nc.nnconv_loss_scaler_init(self.scaler.data_ptr(), loss_scale, 2.0, 2000, nc.current_stream()))
@@ -44,18 +46,22 @@ class SequenceModel:
         self.flag = torch.zeros(1, dtype=torch.int32, device=device)
         self.step_count = torch.zeros(1, dtype=torch.int32, device=device)
 
-        conv = lambda k, cc: nc.Conv2d(n, cc, 1, t, k, 1, 1, layout=nc.NNCONV_NHWC, dtype=dtype)  # noqa: E731
-        self.embed, self.head = conv(c, c_in), conv(c_out, c)
-        self.into, self.back = [conv(3 * c, c) for _ in range(blocks)], [conv(c, c) for _ in range(blocks)]
+        self.into, self.back = [self._conv(3 * c, c) for _ in range(blocks)], [self._conv(c, c) for _ in range(blocks)]
         self.norm = nc.RMSNorm(n * t, c, dtype=dtype)
         self.rec = nc.GatedRecurrence(n, t, c, ld=3 * c, dtype=dtype)
-        new = lambda k: torch.empty((n, t, k), dtype=self.dtype, device=device)  # noqa: E731
-        f32 = lambda *s: torch.empty(s, dtype=torch.float32, device=device)  # noqa: E731
+        new, f32 = self._new, lambda *s: torch.empty(s, dtype=torch.float32, device=device)
         # activations that the backward pass reads, one set a block
         self.acts = [dict(r=new(c), u=new(c), rstd=f32(n * t), p=new(3 * c), y=new(c), x=new(c), saved=self.rec.saved(device))
                      for _ in range(blocks)]
-        self.x0, self.r, self.u, self.rstd, self.out = new(c), new(c), new(c), f32(n * t), new(c_out)
-        self.grad = dict(out=new(c_out), u=new(c), r=new(c), y=new(c), p=new(3 * c))
+        self.x0, self.r, self.u, self.rstd = new(c), new(c), new(c), f32(n * t)
+        self.grad = dict(u=new(c), r=new(c), y=new(c), p=new(3 * c))
+
+    def _conv(self, k, c):
+        return nc.Conv2d(self.n, c, 1, self.t, k, 1, 1, layout=nc.NNCONV_NHWC, dtype=self.code)
+
+    def _new(self, k):
+        import torch
+        return torch.empty((self.n, self.t, k), dtype=self.dtype, device=self.device)
 
     def _parameters(self, g):
         import torch
@@ -83,7 +89,7 @@ class SequenceModel:
             else:
                 m.copy_(torch.randn(shape, generator=g) / math.sqrt(shape[-1]))
             entry = dict(master=m, grad=self.dw[name], weight_decay=decay)
-            if len(shape) == 4:
+            if len(shape) > 1:
                 w = self.w16[name] = part("w16", name, shape)
                 w.copy_(m)
                 blocks = slice(starts[name] // ALIGN, -(-(starts[name] + m.numel()) // ALIGN))
@@ -94,11 +100,9 @@ class SequenceModel:
             tensors.append(entry)
         self.solver = nc.AdamW(tensors, seed=1)
 
-    def forward(self, x):
-        """Outputs [n][t][c_out] of inputs [n][t][c_in]."""
-        c = self.c
-        self.embed.fwd(x, self.w16["embed"], self.x0)
-        h, r = self.x0, None
+    def run(self, h):
+        """The last norm's output [n][t][c], from the first block's input."""
+        c, r = self.c, None
         for b, a in enumerate(self.acts):
             self.norm.fwd(h, self.master["gain%d" % b], a["u"], residual=r, sum=a["r"], rstd=a["rstd"])
             self.into[b].fwd(a["u"], self.w16["in%d" % b], a["p"])
@@ -107,42 +111,34 @@ class SequenceModel:
             self.back[b].fwd(a["y"], self.w16["out%d" % b], a["x"])
             h, r = a["x"], a["r"]
         self.norm.fwd(h, self.master["gain"], self.u, residual=r, sum=self.r, rstd=self.rstd)
-        self.head.fwd(self.u, self.w16["head"], self.out)
-        return self.out
+        return self.u
 
-    def backward(self, x, dout):
-        """Parameter gradients, loss-scaled as dout is, into the flat gradient array."""
+    def _weights(self, conv, inp, dy, name):
+        conv.wgrad(inp, dy, self.dw[name], overflow_flag=self.flag)
+
+    def run_back(self):
+        """From the gradient of the last norm's output, grad["u"], that of the first block's input,
+        grad["r"]; the parameters' into the flat array."""
         c, d, flag = self.c, self.grad, self.flag
-
-        def weights(conv, inp, dy, name):
-            conv.wgrad(inp, dy, self.dw[name], overflow_flag=flag)
-
-        weights(self.head, self.u, dout, "head")
-        self.head.dgrad(dout, self.w16["head"], d["u"])
         self.norm.bwd(self.r, d["u"], self.master["gain"], self.rstd, d["r"], dgain=self.dw["gain"], overflow_flag=flag)
         for b in range(self.blocks - 1, -1, -1):
             a = self.acts[b]
-            weights(self.back[b], a["y"], d["r"], "out%d" % b)
+            self._weights(self.back[b], a["y"], d["r"], "out%d" % b)
             self.back[b].dgrad(d["r"], self.w16["out%d" % b], d["y"])
             v, f, g = (a["p"][..., i * c:(i + 1) * c] for i in range(3))
             dv, df, dg = (d["p"][..., i * c:(i + 1) * c] for i in range(3))
             self.rec.bwd(v, f, self.master["bias%d" % b], a["saved"], d["y"], dv, df, g=g, dg=dg, dbias=self.dw["bias%d" % b],
                          overflow_flag=flag)
-            weights(self.into[b], a["u"], d["p"], "in%d" % b)
+            self._weights(self.into[b], a["u"], d["p"], "in%d" % b)
             self.into[b].dgrad(d["p"], self.w16["in%d" % b], d["u"])
             # the stream's own gradient joins in place
             self.norm.bwd(a["r"], d["u"], self.master["gain%d" % b], a["rstd"], d["r"], dgain=self.dw["gain%d" % b], dsum=d["r"],
                           overflow_flag=flag)
-        weights(self.embed, x, d["r"], "embed")
+        return d["r"]
 
-    def train_step(self, x, target, lr, beta1=0.9, beta2=0.99):
-        """One step on the mean squared error; returns the loss as a device scalar."""
-        err = self.forward(x).float() - target
-        self.grad["out"].copy_(err * (2.0 / err.numel()) * self.loss_scale)
-        self.backward(x, self.grad["out"])
+    def update(self, lr, beta1, beta2):
         self.solver.step(self.step_count, lr, beta1, beta2, state=self.scaler, overflow_flag=self.flag)
         nc.check(nc.nnconv_loss_scaler_update(self.scaler.data_ptr(), self.flag.data_ptr(), nc.current_stream()))
-        return (err * err).mean()
 
     def features_q8(self, group=128):
         """The last forward's features (the last norm's output) in 8 bits: (codes, scales)."""
@@ -154,27 +150,64 @@ class SequenceModel:
         return q, scales
 
 
-class Server:
-    """One token of each of `n` sequences a call, from the model's present weights."""
+class SequenceModel(GatedBlocks):
+    """c_in input channels, `blocks` blocks of c channels, c_out outputs; channel counts in multiples of 8."""
+
+    def __init__(self, n, t, c_in, c, c_out, blocks, dtype=nc.NNCONV_BF16, seed=0, loss_scale=1024.0, weight_decay=0.01,
+                 device="cuda"):
+        self.c_in, self.c_out = c_in, c_out
+        super().__init__(n, t, c, blocks, [("embed", (c, 1, 1, c_in), weight_decay)], [("head", (c_out, 1, 1, c), weight_decay)],
+                         dtype, seed, loss_scale, weight_decay, device)
+        self.embed, self.head = self._conv(c, c_in), self._conv(c_out, c)
+        self.out, self.grad["out"] = self._new(c_out), self._new(c_out)
+
+    def forward(self, x):
+        """Outputs [n][t][c_out] of inputs [n][t][c_in]."""
+        self.embed.fwd(x, self.w16["embed"], self.x0)
+        self.head.fwd(self.run(self.x0), self.w16["head"], self.out)
+        return self.out
+
+    def backward(self, x, dout):
+        """Parameter gradients, loss-scaled as dout is, into the flat gradient array."""
+        self._weights(self.head, self.u, dout, "head")
+        self.head.dgrad(dout, self.w16["head"], self.grad["u"])
+        self._weights(self.embed, x, self.run_back(), "embed")
+
+    def train_step(self, x, target, lr, beta1=0.9, beta2=0.99):
+        """One step on the mean squared error; returns the loss as a device scalar."""
+        err = self.forward(x).float() - target
+        self.grad["out"].copy_(err * (2.0 / err.numel()) * self.loss_scale)
+        self.backward(x, self.grad["out"])
+        self.update(lr, beta1, beta2)
+        return (err * err).mean()
+
+
+class BlockSteps:
+    """The blocks of a model for one token of each of `n` sequences a call, from its present weights."""
 
     def __init__(self, model, n):
         import torch
-        self.model, c = model, model.c
-        conv = lambda k, cc: nc.Conv2d(n, cc, 1, 1, k, 1, 1, layout=nc.NNCONV_NHWC, dtype=model.code)  # noqa: E731
-        self.embed, self.into, self.back, self.head = conv(c, model.c_in), conv(3 * c, c), conv(c, c), conv(model.c_out, c)
+        self.model, self.n, c = model, n, model.c
+        self.into, self.back = self._conv(3 * c, c), self._conv(c, c)
         self.norm = nc.RMSNorm(n, c, dtype=model.code)
         self.rec = nc.GatedRecurrence(n, 1, c, ld=3 * c, dtype=model.code)
-        new = lambda k: torch.empty((n, k), dtype=model.dtype, device=model.device)  # noqa: E731
-        self.h, self.r, self.u, self.p, self.y, self.out = new(c), new(c), new(c), new(3 * c), new(c), new(model.c_out)
+        new = self._new
+        self.h, self.r, self.u, self.p, self.y = new(c), new(c), new(c), new(3 * c), new(c)
         self.states = torch.zeros((model.blocks, n, c), dtype=torch.float32, device=model.device)
+
+    def _conv(self, k, c):
+        return nc.Conv2d(self.n, c, 1, 1, k, 1, 1, layout=nc.NNCONV_NHWC, dtype=self.model.code)
+
+    def _new(self, k):
+        import torch
+        return torch.empty((self.n, k), dtype=self.model.dtype, device=self.model.device)
 
     def reset(self):
         self.states.zero_()
 
-    def step(self, x):
-        """Outputs [n][c_out] of one token [n][c_in] of each sequence; the states go on."""
+    def run(self):
+        """The last norm's output [n][c], from the first block's input in `h`; the states go on."""
         m, c = self.model, self.model.c
-        self.embed.fwd(x, m.w16["embed"], self.h)
         r = None
         for b in range(m.blocks):
             self.norm.fwd(self.h, m.master["gain%d" % b], self.u, residual=r, sum=self.r)
@@ -184,7 +217,21 @@ class Server:
             self.rec.fwd(v, f, m.master["bias%d" % b], self.y, g=g, h0=self.states[b], ht=self.states[b])
             self.back.fwd(self.y, m.w16["out%d" % b], self.h)
         self.norm.fwd(self.h, m.master["gain"], self.u, residual=r, sum=self.r)
-        self.head.fwd(self.u, m.w16["head"], self.out)
+        return self.u
+
+
+class Server(BlockSteps):
+    """One token of each of `n` sequences a call, from the model's present weights."""
+
+    def __init__(self, model, n):
+        super().__init__(model, n)
+        self.embed, self.head = self._conv(model.c, model.c_in), self._conv(model.c_out, model.c)
+        self.out = self._new(model.c_out)
+
+    def step(self, x):
+        """Outputs [n][c_out] of one token [n][c_in] of each sequence; the states go on."""
+        self.embed.fwd(x, self.model.w16["embed"], self.h)
+        self.head.fwd(self.run(), self.model.w16["head"], self.out)
         return self.out
 
 

@@ -1,0 +1,121 @@
+"""Refusals and sizes of the calls at both ends of a model over a vocabulary: every call here fails its checks
+(or has nothing to do) before anything is queued."""
+import ctypes
+
+import pytest
+
+from paper_2102_06725_amd import nnconv as nc
+
+FAKE = 0x100000  # never dereferenced
+INV, UNS = nc.NNCONV_ERR_INVALID_ARG, nc.NNCONV_ERR_UNSUPPORTED
+MIS, WSP, OK = nc.NNCONV_ERR_MISALIGNED, nc.NNCONV_ERR_WORKSPACE, nc.NNCONV_OK
+
+
+def test_struct_sizes():
+    assert ctypes.sizeof(nc.nnconv_embedding_desc) == 24
+    assert ctypes.sizeof(nc.nnconv_xent_desc) == 32
+
+
+def emb(rows=4, c=16, v=9, dtype=nc.NNCONV_F16, scale=1.0):
+    return nc.nnconv_embedding_desc(rows, c, v, dtype, scale)
+
+
+def efwd(d, ids=FAKE, table=FAKE, y=FAKE):
+    return nc.nnconv_embedding_fwd(d, ids, table, y, None)
+
+
+def ebwd(d, ids=FAKE, dy=FAKE, dtable=FAKE, kind=nc.NNCONV_F32, acc=0, flag=None, ws=FAKE, nb=1 << 40):
+    return nc.nnconv_embedding_bwd(d, ids, dy, dtable, kind, 1.0, acc, flag, ws, nb, None)
+
+
+@pytest.mark.parametrize("kw", [dict(rows=-1), dict(c=0), dict(c=-3), dict(v=0), dict(dtype=9), dict(scale=float("nan")),
+                                dict(scale=float("inf")), dict(rows=1 << 40, c=2)])
+def test_embedding_descriptors(nnlib, kw):
+    d = emb(**kw)
+    assert efwd(d) == ebwd(d) == nc.nnconv_embedding_workspace_size(d)[0] == INV
+
+
+@pytest.mark.parametrize("kw", [dict(dtype=nc.NNCONV_F32), dict(dtype=nc.NNCONV_F8), dict(rows=(1 << 27) + 1), dict(c=(1 << 24) + 1),
+                                dict(v=(1 << 29) + 1)])
+def test_embedding_limits(nnlib, kw):
+    d = emb(**kw)
+    assert efwd(d) == ebwd(d, kind=nc.NNCONV_F32) == nc.nnconv_embedding_workspace_size(d)[0] == UNS
+
+
+def test_embedding_refusals(nnlib):
+    d = emb()
+    assert efwd(d, ids=None) == efwd(d, table=None) == efwd(d, y=None) == INV
+    assert efwd(d, ids=FAKE + 2) == efwd(d, table=FAKE + 1) == efwd(d, y=FAKE + 1) == MIS
+    assert ebwd(d, ids=None) == ebwd(d, dy=None) == ebwd(d, dtable=None) == ebwd(d, acc=2) == ebwd(d, acc=-1) == INV
+    assert ebwd(d, kind=nc.NNCONV_BF16) == ebwd(d, kind=nc.NNCONV_F8) == UNS and ebwd(d, kind=17) == INV
+    assert ebwd(d, ids=FAKE + 2) == ebwd(d, dy=FAKE + 1) == ebwd(d, dtable=FAKE + 2) == ebwd(d, flag=FAKE + 2) == MIS
+    assert ebwd(d, dtable=FAKE + 1, kind=nc.NNCONV_F16) == ebwd(d, ws=FAKE + 8) == MIS
+    st, need = nc.nnconv_embedding_workspace_size(d)
+    assert st == OK and need >= 4 * 8 and ebwd(d, nb=need - 1) == WSP and ebwd(d, ws=None) == INV
+    assert efwd(emb(rows=0)) == efwd(emb(rows=0), ids=None, table=None, y=None) == OK
+    assert nc.nnconv_embedding_workspace_size(emb(rows=0)) == (OK, 0)
+    assert ebwd(emb(rows=0), dtable=None) == INV
+    assert ebwd(emb(rows=0), ids=None, dy=None, acc=1, ws=None, nb=0) == OK
+
+
+def xent(rows=4, c=16, v=9, dtype=nc.NNCONV_F16, k=1, teacher_dtype=nc.NNCONV_F32, scale=1.0):
+    return nc.nnconv_xent_desc(rows, c, v, dtype, k, teacher_dtype, scale)
+
+
+def xfwd(d, x=FAKE, w=FAKE, targets=FAKE, teacher=None, loss=FAKE, lse=None, ws=FAKE, nb=1 << 50):
+    return nc.nnconv_xent_fwd(d, x, w, targets, teacher, loss, lse, ws, nb, None)
+
+
+def xtrain(d, x=FAKE, w=FAKE, targets=FAKE, teacher=None, scale=None, loss=FAKE, lse=None, dx=FAKE, dw=FAKE, kind=nc.NNCONV_F32, acc=0,
+           flag=None, ws=FAKE, nb=1 << 50):
+    return nc.nnconv_xent_train(d, x, w, targets, teacher, 1.0, scale, loss, lse, dx, dw, kind, 1.0, acc, flag, ws, nb, None)
+
+
+@pytest.mark.parametrize("kw", [dict(rows=-1), dict(c=0), dict(v=0), dict(v=-5), dict(k=0), dict(dtype=9), dict(teacher_dtype=8),
+                                dict(scale=float("nan")), dict(scale=float("-inf")), dict(scale=0.0), dict(rows=1 << 40, c=2),
+                                dict(rows=1 << 30, v=1 << 20)])
+def test_xent_descriptors(nnlib, kw):
+    d = xent(**kw)
+    assert xfwd(d) == xtrain(d) == nc.nnconv_xent_workspace_size(d, nc.NNCONV_FWD)[0] == INV
+
+
+@pytest.mark.parametrize("kw", [dict(dtype=nc.NNCONV_F32), dict(dtype=nc.NNCONV_F8), dict(teacher_dtype=nc.NNCONV_F8),
+                                dict(teacher_dtype=nc.NNCONV_BF16), dict(k=1025), dict(rows=(1 << 23) + 1), dict(c=(1 << 20) + 1),
+                                dict(v=(1 << 21) + 1)])
+def test_xent_limits(nnlib, kw):
+    d = xent(**kw)
+    assert xfwd(d) == xtrain(d) == nc.nnconv_xent_workspace_size(d, nc.NNCONV_DGRAD)[0] == UNS
+
+
+def test_xent_refusals(nnlib):
+    d = xent()
+    for call in (xfwd, xtrain):
+        assert call(d, x=None) == call(d, w=None) == call(d, targets=None) == call(d, loss=None) == INV
+        assert call(xent(k=2)) == INV  # labels are one a row
+        assert call(d, x=FAKE + 1) == call(d, w=FAKE + 2) == call(d, targets=FAKE + 2) == call(d, loss=FAKE + 2) == MIS
+        assert call(d, teacher=FAKE + 2) == call(d, lse=FAKE + 2) == call(d, ws=FAKE + 8) == MIS
+        assert call(xent(c=15), w=FAKE + 1) == MIS
+        for pass_ in (nc.NNCONV_FWD if call is xfwd else nc.NNCONV_DGRAD,):
+            for d2, more in ((d, {}), (xent(c=15), {}), (xent(k=3), dict(teacher=FAKE))):
+                st, need = nc.nnconv_xent_workspace_size(d2, pass_)
+                assert st == OK and need > 0
+                assert call(d2, nb=need - 1, **more) == WSP and call(d2, ws=None, **more) == INV
+    assert xtrain(d, dx=None) == xtrain(d, acc=2) == INV
+    assert xtrain(d, kind=nc.NNCONV_BF16) == xtrain(d, kind=nc.NNCONV_F8) == UNS and xtrain(d, kind=33) == INV
+    assert xtrain(d, scale=FAKE + 2) == xtrain(d, dx=FAKE + 1) == xtrain(d, dw=FAKE + 2) == xtrain(d, flag=FAKE + 1) == MIS
+    assert xtrain(d, dw=FAKE + 1, kind=nc.NNCONV_F16) == MIS
+    assert nc.nnconv_xent_workspace_size(d, nc.NNCONV_WGRAD)[0] == INV
+    none = xent(rows=0)
+    assert xfwd(none, x=None, w=None, targets=None, loss=None, ws=None, nb=0) == OK
+    assert xtrain(none, x=None, w=None, targets=None, loss=None, dx=None, acc=1, ws=None, nb=0) == OK
+    assert xtrain(none, dw=None, ws=None, nb=0) == OK
+
+
+def test_the_workspace_is_bounded(nnlib):
+    """It grows with the rows by what each row has, not by its logits."""
+    size = lambda **kw: nc.nnconv_xent_workspace_size(xent(**kw), nc.NNCONV_DGRAD)[1]  # noqa: E731
+    a, b = size(rows=20000, c=64, v=100000), size(rows=40000, c=64, v=100000)
+    assert a < (1 << 30) + 3 * (1 << 28) and b - a < 20000 * 1000
+    assert size(rows=4, c=64, v=100) < 1 << 20
+    # several pieces have fp32 sums of dw beside them
+    assert size(rows=6000, c=512, v=100000) - size(rows=5000, c=512, v=100000) >= 4 * 512 * 100000
