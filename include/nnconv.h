@@ -622,7 +622,7 @@ nnconv_status nnconv_embedding_bwd(const nnconv_embedding_desc *desc, const int3
  * its x is not read. */
 typedef struct {
     int64_t rows;          /* 0 to 2^23 */
-    int32_t c;             /* channels, 1 to 2^20 */
+    int32_t c;             /* channels, 1 to 2^20; rows * c and v * c up to 2^35 */
     int32_t v;             /* vocabulary, 1 to 2^21 */
     int32_t dtype;         /* F16 or BF16: x, w, dx */
     int32_t k;             /* targets of a row, 1 to 1024; 1 with labels */

@@ -16,17 +16,22 @@ constexpr int MOST_TARGETS = 1024;
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;  // 16 bytes at any element
+
 struct Rows {
     int64_t rows;
     int32_t c, ldx, v, k;
     const uint16_t *x, *w;
-    int64_t ldw;
     const int32_t *targets;
     const void *teacher;  // or null: labels
     float scale;
     uint16_t *xc;    // [rows][ldx]: x with zeros behind its channels and in rows that do not count
-    float *zt, *qt;  // [rows][k]: the targets' logits, in units of log 2; what is taken from their softmax
-    float *base;     // [rows]: sum q (log q - z); the bits NOT_COUNTED in rows that do not count
+    uint16_t *wc;    // [v][ldx]: w with zeros behind its channels, or null
+    int32_t first_w; // workgroups before those that copy w
+    // of a teacher's targets, [rows][k]: logits in units of log 2; shares; what is taken from their
+    // softmax
+    float *zt, *qi, *qt;
+    float *base;     // [rows]: sum q log q; the bits NOT_COUNTED in rows that do not count
 };
 
 // What stands for a row that does not count.  Arithmetic makes no NaN with these bits.
@@ -40,26 +45,46 @@ __device__ __forceinline__ float wave_sum(float v) {
 }
 
 // 8 channels from `c` on of a row of n, zeros behind it.
-template <bool VEC>
 __device__ __forceinline__ u32x4 channels(const uint16_t *row, int c, int n) {
-    if constexpr (VEC) return *(const u32x4 *)(row + c);
+    if (c + 8 <= n) return *(const u32x4_any *)(row + c);
     u32x4 v = {};
 #pragma unroll
-    for (int d = 0; d < 8; ++d)
+    for (int d = 0; d < 7; ++d)
         if (c + d < n) v[d >> 1] |= (uint32_t)row[c + d] << (16 * (d & 1));
     return v;
 }
 
-// Labels: the copy of x, a thread 8 channels.
-template <bool VEC>
+// Whether this workgroup copies w, 1024 vectors of 8 channels each.
+constexpr int COPY_VECTORS = 1024;
+__device__ __forceinline__ bool copied_w(const Rows &P) {
+    if (blockIdx.x < (uint32_t)P.first_w) return false;
+    if (blockIdx.y > 0) return true;
+    const uint32_t per = (uint32_t)P.ldx / 8;
+    const int64_t first = (int64_t)(blockIdx.x - P.first_w) * COPY_VECTORS, count = (int64_t)P.v * per;
+    u32x4 v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const int64_t i = first + u * 256 + threadIdx.x, r = i / per;
+        if (i < count) v[u] = channels(P.w + r * P.c, (int)(i - r * per) * 8, P.c);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const int64_t i = first + u * 256 + threadIdx.x;
+        if (i < count) *(u32x4 *)(P.wc + i * 8) = v[u];
+    }
+    return true;
+}
+
+// Labels: the copies of x, a thread 8 channels, and of w.
 __global__ __launch_bounds__(256) void copy_kernel(const Rows P) {
+    if (copied_w(P)) return;
     const uint32_t per = (uint32_t)P.ldx / 8;
     const int64_t count = P.rows * per;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)P.first_w * 256) {
         const int64_t r = i / per;
         const int c = (int)(i - r * per) * 8;
         const bool in = (uint32_t)P.targets[r] < (uint32_t)P.v;
-        *(u32x4 *)(P.xc + r * P.ldx + c) = in ? channels<VEC>(P.x + r * P.c, c, P.c) : u32x4{};
+        *(u32x4 *)(P.xc + r * P.ldx + c) = in ? channels(P.x + r * P.c, c, P.c) : u32x4{};
     }
 }
 
@@ -81,58 +106,69 @@ __device__ __forceinline__ float teacher_logit(const void *p, int64_t i) {
         return from16<T>(((const uint16_t *)p)[i]);
 }
 
-// A teacher: a workgroup a row.  The row's copy, the logits of its targets in fp32 (their own sums:
-// the products' tiles have them in many places), and the teacher's softmax.  A quarter wave has a
-// target: 16 lanes of 8 channels each.
-template <class T, class S, bool VEC>
+// A teacher: workgroups (row, share of its targets).  The logits of the targets in fp32 (their own
+// sums: the products' tiles have them in many places), a quarter wave each, 16 lanes of 8 channels,
+// four loads on their way; the first of a row makes its copy and the teacher's softmax.  Bound by
+// the gather of the targets' rows of w.
+template <class T, class S>
 __global__ __launch_bounds__(256) void rows_kernel(const Rows P) {
+    if (copied_w(P)) return;
     const int64_t r = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    __shared__ float q[MOST_TARGETS], z[MOST_TARGETS];
-    __shared__ float part[4];
     const int k = P.k;
     const int32_t *t = P.targets + r * k;
+    const uint16_t *x = P.x + r * P.c;
     // the largest of the teacher's logits that count
     float most = -INFINITY;
-    bool any = false, nan = false;
+    bool any = false;
     for (int i = lane; i < k; i += 64) {
         const float a = teacher_logit<T, S>(P.teacher, r * k + i) * P.scale;
         if ((uint32_t)t[i] >= (uint32_t)P.v || a == -INFINITY) continue;
         any = true;
-        nan |= !(a == a);
         most = fmaxf(most, a);
     }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
     any = __any(any);
-    nan = __any(nan);
-    uint16_t *xc = P.xc + r * P.ldx;
-    const uint16_t *x = P.x + r * P.c;
-    if (!any) {
-        for (int c = tid * 8; c < P.ldx; c += 2048) *(u32x4 *)(xc + c) = u32x4{};
-        for (int i = tid; i < k; i += 256) P.zt[r * k + i] = P.qt[r * k + i] = 0.f;
-        if (tid == 0) P.base[r] = __builtin_bit_cast(float, NOT_COUNTED);
-        return;
+    if (blockIdx.y == 0) {
+        uint16_t *xc = P.xc + r * P.ldx;
+        for (int c = tid * 8; c < P.ldx; c += 2048) *(u32x4 *)(xc + c) = any ? channels(x, c, P.c) : u32x4{};
     }
-    for (int c = tid * 8; c < P.ldx; c += 2048) *(u32x4 *)(xc + c) = channels<VEC>(x, c, P.c);
+    if (!any) {
+        if (blockIdx.y == 0 && tid == 0) P.base[r] = __builtin_bit_cast(float, NOT_COUNTED);
+        return;  // nothing is read of the rest
+    }
+    const int l16 = lane & 15;
+    for (int i = (int)blockIdx.y * 16 + (tid >> 4); i < k; i += 16 * (int)gridDim.y) {
+        const int32_t j = t[i];
+        float dot = 0.f;
+        if ((uint32_t)j < (uint32_t)P.v) {
+            const uint16_t *w = P.w + (int64_t)j * P.c;
+            for (int c0 = l16 * 8; c0 < P.c; c0 += 512) {
+                u32x4 a[4], b[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int c = c0 + u * 128;
+                    b[u] = c < P.c ? channels(w, c, P.c) : u32x4{};
+                    a[u] = c < P.c ? channels(x, c, P.c) : u32x4{};
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u) dot = dot8<T>(a[u], b[u], dot);
+            }
+        }
+#pragma unroll
+        for (int d = 8; d > 0; d >>= 1) dot += __shfl_xor(dot, d);
+        if (l16 == 0) P.zt[r * k + i] = dot * P.scale * LOG2E;
+    }
+    if (blockIdx.y > 0) return;
+    __shared__ float q[MOST_TARGETS];
+    __shared__ float part[4];
     float sum = 0.f;
     for (int i = tid; i < k; i += 256) {
         const float a = teacher_logit<T, S>(P.teacher, r * k + i) * P.scale;
         const float e = (uint32_t)t[i] >= (uint32_t)P.v || a == -INFINITY ? 0.f : expf(a - most);
         q[i] = e;
         sum += e;
-    }
-    const int l16 = lane & 15;
-    for (int i = tid >> 4; i < k; i += 16) {
-        const int32_t j = t[i];
-        float dot = 0.f;
-        if ((uint32_t)j < (uint32_t)P.v) {
-            const uint16_t *w = P.w + (int64_t)j * P.ldw;  // whole vectors, zeros behind the channels
-            for (int c = l16 * 8; c < P.ldx; c += 128) dot = dot8<T>(channels<VEC>(x, c, P.c), *(const u32x4 *)(w + c), dot);
-        }
-#pragma unroll
-        for (int d = 8; d > 0; d >>= 1) dot += __shfl_xor(dot, d);
-        if (l16 == 0) z[i] = dot * P.scale;
     }
     sum = wave_sum(sum);
     if (lane == 0) part[wave] = sum;
@@ -144,28 +180,25 @@ __global__ __launch_bounds__(256) void rows_kernel(const Rows P) {
         const float e = q[i];
         float taken = 0.f;  // a target that is named twice is taken from once, with both shares
         for (int j = 0; j < k; ++j) taken += t[j] == t[i] ? q[j] : 0.f;
-        P.zt[r * k + i] = z[i] * LOG2E;
+        P.qi[r * k + i] = e / sum;
         P.qt[r * k + i] = taken / sum;
-        if (e != 0.f) base += e / sum * (teacher_logit<T, S>(P.teacher, r * k + i) * P.scale - most - log_sum - z[i]);
+        if (e != 0.f) base += e / sum * (teacher_logit<T, S>(P.teacher, r * k + i) * P.scale - most - log_sum);
     }
     __syncthreads();
     base = wave_sum(base);
     if (lane == 0) part[wave] = base;
     __syncthreads();
-    if (tid == 0) {
-        base = part[0] + part[1] + part[2] + part[3];
-        P.base[r] = nan ? __builtin_nanf("") : base;
-    }
+    if (tid == 0) P.base[r] = part[0] + part[1] + part[2] + part[3];
 }
 
 // The tiles' statistics of rows, and what becomes of them.
 struct Join {
     int64_t rows;
-    int32_t tiles, tile, v, k;  // tile: columns
+    int32_t tiles, shift, v, k;  // shift: of a column to its tile
     const float2 *stats;
     const int32_t *targets;     // [rows][k]
     const float *zt;            // the targets' logits, in units of log 2
-    const float *qt, *base;     // a teacher's shares and sums; null with labels
+    const float *qi, *qt, *base;  // a teacher's shares and sums (see Rows); null with labels
     float *loss, *lse;          // lse may be null
     uint16_t *e;                // training: [rows][lde]
     int64_t lde, stretch;       // elements of a workgroup
@@ -191,10 +224,22 @@ __device__ __forceinline__ bool row_counts(const Join &P, int64_t r) {
     return P.base ? counted(P.base[r]) : (uint32_t)P.targets[r] < (uint32_t)P.v;
 }
 
+// By one wave.
 __device__ __forceinline__ void put_loss(const Join &P, int64_t r, bool counts, float most, float log_sum) {
-    // a label's logit is subtracted before the logarithm joins: near 0 both are small
-    const float loss = P.base ? P.base[r] + (most + log_sum) * LN2 : (most - P.zt[r] + log_sum) * LN2;
-    P.loss[r] = counts ? loss : 0.f;
+    const int lane = threadIdx.x & 63;
+    float loss = 0.f;
+    if (P.base && counts) {
+        // sum q (log q + lse - z), the terms z - most first
+        float z = 0.f;
+        for (int i = lane; i < P.k; i += 64) {
+            const float q = P.qi[r * P.k + i];
+            if (q != 0.f) z += q * (most - P.zt[r * P.k + i]);
+        }
+        loss = P.base[r] + (wave_sum(z) + log_sum) * LN2;
+    } else if (counts)
+        loss = (most - P.zt[r] + log_sum) * LN2;  // near 0 both are small
+    if (lane != 0) return;
+    P.loss[r] = loss;
     if (P.lse) P.lse[r] = counts ? (most + log_sum) * LN2 : 0.f;
 }
 
@@ -205,7 +250,7 @@ __global__ __launch_bounds__(256) void join_kernel(const Join P) {
     float most, sum;
     join_row(P.stats + r * P.tiles, P.tiles, most, sum);
     const bool counts = row_counts(P, r);
-    if ((threadIdx.x & 63) == 0) put_loss(P, r, counts, most, log2f(sum));
+    put_loss(P, r, counts, most, log2f(sum));
 }
 
 // A workgroup a stretch of a row, one or at most SHARE of them: each joins the row's statistics
@@ -233,13 +278,13 @@ __global__ __launch_bounds__(256) void scale_kernel(const Join P) {
     float most, sum;
     join_row(s, P.tiles, most, sum);
     const float log_sum = log2f(sum), over = GRAD_UNIT / sum;
-    if (part == 0 && threadIdx.x == 0) put_loss(P, r, counts, most, log_sum);
+    if (part == 0 && threadIdx.x < 64) put_loss(P, r, counts, most, log_sum);
     for (;;) {
         float f[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const int64_t n = i + u * 2048;
-            const float m = n < n1 ? s[n / P.tile].x : most;
+            const float m = n < n1 ? s[n >> P.shift].x : most;
             f[u] = over * exp2f(m == most ? 0.f : m - most);
         }
 #pragma unroll
@@ -268,8 +313,9 @@ __global__ __launch_bounds__(256) void scale_kernel(const Join P) {
 
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 
-// Bytes of the exponentials of a piece of rows at most.
-constexpr int64_t PIECE_BYTES = (int64_t)1 << 30;
+// Bytes of the exponentials of a piece of rows at most, and in a forward call of the statistics.
+constexpr int64_t PIECE_BYTES = (int64_t)1 << 30, STATS_BYTES = (int64_t)1 << 27;
+constexpr int64_t MOST_OPERAND = (int64_t)1 << 35;  // elements of x and of w
 constexpr int CUS = 256;
 
 // A product's tile and, for the gradients, how often its reduction is split.
@@ -312,7 +358,7 @@ struct Plan {
     Shape logits, dx, dw;
     int32_t tiles;  // stats a row
     bool copy_w, copy_x;
-    size_t xc, wc, zt, qt, base, stats, e, part, acc, bytes;
+    size_t xc, wc, zt, qi, qt, base, stats, e, part, part_w, acc, bytes;
 };
 
 static Plan plan_of(const XentParams &p, bool train) {
@@ -323,12 +369,10 @@ static Plan plan_of(const XentParams &p, bool train) {
     // copied beside its softmax
     q.copy_x = q.copy_w || p.sizes_only || p.teacher || (train && p.dw) || ((uintptr_t)p.x & 15) != 0;
     q.lde = ((int64_t)p.v + 63) / 64 * 64;
+    const int64_t most = (train ? PIECE_BYTES / (2 * q.lde) : STATS_BYTES / (8 * (((int64_t)p.v + 127) / 128))) / 256 * 256;
     q.piece = p.rows;
-    if (train) {
-        const int64_t most = PIECE_BYTES / (2 * q.lde) / 256 * 256;
-        if (q.piece > most) q.piece = most > 256 ? most : 256;
-        if (q.piece > p.rows) q.piece = p.rows;
-    }
+    if (q.piece > most) q.piece = most > 256 ? most : 256;
+    if (q.piece > p.rows) q.piece = p.rows;
     q.logits = shape_of(q.piece, p.v, p.c, false);
     q.dx = shape_of(q.piece, p.c, q.lde, true);
     q.dw = shape_of(p.v, p.c, q.piece, true);
@@ -343,46 +387,43 @@ static Plan plan_of(const XentParams &p, bool train) {
     q.xc = take(q.copy_x ? (size_t)p.rows * q.ldx * 2 : 0);
     q.wc = take(q.copy_w ? (size_t)p.v * q.ldw * 2 : 0);
     q.zt = take((size_t)p.rows * p.k * 4);
+    q.qi = take((size_t)p.rows * p.k * 4);
     q.qt = take((size_t)p.rows * p.k * 4);
     q.base = take((size_t)p.rows * 4);
     q.stats = take((size_t)q.piece * q.tiles * 8);
-    q.e = q.part = q.acc = at;
+    q.e = q.part = q.part_w = q.acc = at;
     if (train) {
         q.e = take((size_t)q.piece * q.lde * 2);
-        size_t part = q.dx.splits > 1 ? (size_t)q.dx.splits * q.piece * p.c : 0;
-        const size_t w = q.dw.splits > 1 ? (size_t)q.dw.splits * p.v * p.c : 0;
-        if (p.dw || p.sizes_only) part = part > w ? part : w;
-        q.part = take(part * 4);
+        q.part = take(q.dx.splits > 1 ? (size_t)q.dx.splits * q.piece * p.c * 4 : 0);
+        q.part_w = take(q.dw.splits > 1 ? (size_t)q.dw.splits * p.v * p.c * 4 : 0);
         q.acc = take(q.piece < p.rows ? (size_t)p.v * p.c * 4 : 0);
     }
     q.bytes = at;
     return q;
 }
 
-template <class T, class S>
-static void launch_rows(const Rows &r, bool vec, hipStream_t st) {
-    if (vec)
-        hipLaunchKernelGGL((rows_kernel<T, S, true>), dim3((uint32_t)r.rows), dim3(256), 0, st, r);
-    else
-        hipLaunchKernelGGL((rows_kernel<T, S, false>), dim3((uint32_t)r.rows), dim3(256), 0, st, r);
-}
-
-static void launch_rows(int dtype, int teacher_dtype, const Rows &r, hipStream_t st) {
-    const bool vec = r.c % 8 == 0 && ((uintptr_t)r.x & 15) == 0;
+static void launch_rows(int dtype, int teacher_dtype, Rows r, hipStream_t st) {
+    const int64_t vectors = r.wc ? (int64_t)r.v * (r.ldx / 8) : 0;
+    const uint32_t more = (uint32_t)((vectors + COPY_VECTORS - 1) / COPY_VECTORS);
     if (!r.teacher) {
         const int64_t n = (r.rows * (r.ldx / 8) + 255) / 256;
-        const dim3 grid((uint32_t)(n < (1 << 20) ? n : (1 << 20)));
-        if (vec)
-            hipLaunchKernelGGL((copy_kernel<true>), grid, dim3(256), 0, st, r);
-        else
-            hipLaunchKernelGGL((copy_kernel<false>), grid, dim3(256), 0, st, r);
+        r.first_w = (int32_t)(n < (1 << 20) ? n : (1 << 20));
+        hipLaunchKernelGGL(copy_kernel, dim3((uint32_t)r.first_w + more), dim3(256), 0, st, r);
         return;
     }
+    r.first_w = (int32_t)r.rows;
+    // few rows: their targets are shared out
+    const int64_t most = (r.k + 15) / 16, want = 1024 / r.rows;
+    const dim3 grid((uint32_t)r.first_w + more, (uint32_t)(want < 1 ? 1 : want < most ? want : most));
     const bool wide = teacher_dtype == NNCONV_F32;
-    if (dtype == Half::id)
-        wide ? launch_rows<Half, float>(r, vec, st) : launch_rows<Half, uint16_t>(r, vec, st);
+    if (dtype == Half::id && wide)
+        hipLaunchKernelGGL((rows_kernel<Half, float>), grid, dim3(256), 0, st, r);
+    else if (dtype == Half::id)
+        hipLaunchKernelGGL((rows_kernel<Half, uint16_t>), grid, dim3(256), 0, st, r);
+    else if (wide)
+        hipLaunchKernelGGL((rows_kernel<BFloat, float>), grid, dim3(256), 0, st, r);
     else
-        wide ? launch_rows<BFloat, float>(r, vec, st) : launch_rows<BFloat, uint16_t>(r, vec, st);
+        hipLaunchKernelGGL((rows_kernel<BFloat, uint16_t>), grid, dim3(256), 0, st, r);
 }
 
 }  // namespace xent
@@ -391,8 +432,9 @@ using namespace xent;
 
 bool xent_fits(const XentParams &p) {
     if (p.k > MOST_TARGETS) return false;
-    // a tile's rows are addressed with 31 bits, workgroups with 30
-    return p.c <= (1 << 20) && p.v <= (1 << 21) && p.rows <= (1 << 23);
+    // a tile's rows are addressed with 31 bits, the threads of a launch with 32
+    return p.c <= (1 << 20) && p.v <= (1 << 21) && p.rows <= (1 << 23) && p.rows * p.c <= MOST_OPERAND &&
+           (int64_t)p.v * p.c <= MOST_OPERAND;
 }
 
 size_t xent_ws(const XentParams &p, bool train) {
@@ -408,17 +450,12 @@ hipError_t launch_xent(const XentParams &p, bool train, hipStream_t st) {
         g.splits = 1;
         g.k_split = 64;
         g.o = {p.dw, p.dw_dtype, p.c, p.v, 1.0f, nullptr, 0, nullptr, nullptr, nullptr};
-        return launch_grad(p.dtype, TILE_128, true, g, st);
+        return launch_grad_w(p.dtype, TILE_128, g, st);
     }
     const Plan q = plan_of(p, train);
     char *ws = (char *)p.ws;
     auto at = [&](size_t o) { return (float *)(ws + o); };
     const uint16_t *w = (const uint16_t *)p.w;
-    if (q.copy_w) {
-        hipError_t e = launch_pad_channels16(p.w, ws + q.wc, p.v, p.c, (int32_t)q.ldw, st);
-        if (e != hipSuccess) return e;
-        w = (const uint16_t *)(ws + q.wc);
-    }
     Rows r;
     r.rows = p.rows;
     r.c = p.c;
@@ -427,18 +464,20 @@ hipError_t launch_xent(const XentParams &p, bool train, hipStream_t st) {
     r.k = p.k;
     r.x = (const uint16_t *)p.x;
     r.w = w;
-    r.ldw = q.ldw;
+    r.wc = q.copy_w ? (uint16_t *)(ws + q.wc) : nullptr;
     r.targets = p.targets;
     r.teacher = p.teacher;
     r.scale = p.logit_scale;
     r.xc = (uint16_t *)(ws + q.xc);
     r.zt = at(q.zt);
+    r.qi = at(q.qi);
     r.qt = at(q.qt);
     r.base = at(q.base);
     const uint16_t *x = (const uint16_t *)p.x;
     if (q.copy_x) {
         launch_rows(p.dtype, p.teacher_dtype, r, st);
         x = r.xc;
+        if (q.copy_w) w = r.wc;
     }
 
     const int tile = tile_cols(q.logits.cfg);
@@ -462,12 +501,13 @@ hipError_t launch_xent(const XentParams &p, bool train, hipStream_t st) {
         Join j;
         j.rows = n;
         j.tiles = q.tiles;
-        j.tile = tile;
+        j.shift = tile == 256 ? 8 : 7;
         j.v = p.v;
         j.k = p.k;
         j.stats = l.stats;
         j.targets = p.targets + r0 * p.k;
         j.zt = r.zt + r0 * p.k;
+        j.qi = p.teacher ? r.qi + r0 * p.k : nullptr;
         j.qt = p.teacher ? r.qt + r0 * p.k : nullptr;
         j.base = p.teacher ? r.base + r0 : nullptr;
         j.loss = p.loss + r0;
@@ -487,7 +527,7 @@ hipError_t launch_xent(const XentParams &p, bool train, hipStream_t st) {
         else
             hipLaunchKernelGGL((scale_kernel<BFloat>), grid, dim3(256), 0, st, j);
         const float alpha = p.alpha * p.logit_scale / GRAD_UNIT;
-        Grad g;
+        Grad g, d;
         g.a = {l.e, q.lde, (int32_t)n};
         g.b = {w, q.ldw, (int32_t)q.ldw};
         g.k = p.v;
@@ -495,17 +535,15 @@ hipError_t launch_xent(const XentParams &p, bool train, hipStream_t st) {
         g.splits = q.dx.splits;
         g.part = at(q.part);
         g.o = {(uint16_t *)p.dx + r0 * p.c, p.dtype, p.c, n, alpha, p.grad_scale, 0, p.flag, nullptr, nullptr};
-        e = launch_grad(p.dtype, q.dx.cfg, false, g, st);
-        if (e != hipSuccess) return e;
-        if (!p.dw) continue;
-        g.a = {l.e, q.lde, (int32_t)q.lde};
-        g.b = {l.x.p, q.ldx, (int32_t)q.ldx};
-        g.k = n;
-        g.k_split = q.dw.k_split;
-        g.splits = q.dw.splits;
-        g.o = {p.dw, p.dw_dtype, p.c, p.v, alpha * p.inv_loss_scale, p.grad_scale, p.accumulate, p.flag,
+        d.a = {l.e, q.lde, (int32_t)q.lde};
+        d.b = {l.x.p, q.ldx, (int32_t)q.ldx};
+        d.k = n;
+        d.k_split = q.dw.k_split;
+        d.splits = q.dw.splits;
+        d.part = at(q.part_w);
+        d.o = {p.dw, p.dw_dtype, p.c, p.v, alpha * p.inv_loss_scale, p.grad_scale, p.accumulate, p.flag,
                r0 > 0 ? at(q.acc) : nullptr, r0 + n < p.rows ? at(q.acc) : nullptr};
-        e = launch_grad(p.dtype, q.dw.cfg, true, g, st);
+        e = launch_grads(p.dtype, q.dx.cfg, g, q.dw.cfg, p.dw ? &d : nullptr, st);
         if (e != hipSuccess) return e;
     }
     return hipGetLastError();

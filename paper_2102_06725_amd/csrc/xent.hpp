@@ -77,8 +77,9 @@ inline int tile_rows(Config c) { return c == TILE_256 ? 256 : c == TILE_128 ? 12
 inline int tile_cols(Config c) { return c == TILE_256 ? 256 : 128; }
 
 hipError_t launch_logits(int dtype, Config cfg, Logits p, hipStream_t st);
-// atr: a is read along its rows (the reduction's elements are p[k * ld + m]).
-hipError_t launch_grad(int dtype, Config cfg, bool atr, Grad p, hipStream_t st);
+// dx = d w and, with dw, dw = d^T x: one launch where both take tiles of one kind.
+hipError_t launch_grads(int dtype, Config cfg, const Grad &dx, Config cfg_w, const Grad *dw, hipStream_t st);
+hipError_t launch_grad_w(int dtype, Config cfg, const Grad &dw, hipStream_t st);
 
 // Tiles in an order that keeps a group of GROUP_M tile rows together.
 constexpr int GROUP_M = 8;

@@ -83,15 +83,14 @@ __device__ __forceinline__ void put4(const GradOut &o, float factor, int64_t m, 
 
 __device__ __forceinline__ float factor_of(const GradOut &o) { return o.scale ? o.alpha * *o.scale : o.alpha; }
 
-template <class T, int BM, int BN, int WM, int WN, int BK, int STAGES, int OCC, bool ATR>
-__global__ __launch_bounds__(WM * WN * 64, OCC) void grad_kernel(const Grad P) {
+// Workgroup `block` of a product.  ATR: a is read along its rows (the reduction's elements are
+// p[k * ld + m]).
+template <class T, int BM, int BN, int WM, int WN, int BK, int STAGES, bool ATR>
+__device__ __forceinline__ void grad_tile(const Grad &P, uint32_t block, char *lds) {
     typedef gemm::Tile<T, BM, BN, WM, WN, BK, STAGES, ATR, true> G;
     constexpr int FM = G::FM, FN = G::FN;
-    constexpr int LDS = G::LDS_BYTES < BM * BN * 2 ? BM * BN * 2 : G::LDS_BYTES;
-    __shared__ __attribute__((aligned(16))) char lds[LDS];
-
     const int per = P.tiles_m * P.tiles_n;
-    const int id = (int)xcd_remap(blockIdx.x, gridDim.x);
+    const int id = (int)xcd_remap(block, (uint32_t)(per * P.splits));
     const int split = id / per;
     int tm, tn;
     tile_of(id - split * per, P.tiles_m, P.tiles_n, tm, tn);
@@ -172,58 +171,106 @@ __global__ __launch_bounds__(WM * WN * 64, OCC) void grad_kernel(const Grad P) {
     if (o.flag && bad) *o.flag = 1;
 }
 
+// The two products, the first `blocks` workgroups one's: FIRST says which.
+template <class T, int BM, int BN, int WM, int WN, int BK, int STAGES, int OCC>
+__global__ __launch_bounds__(WM * WN * 64, OCC) void grads_kernel(const Grad dx, const Grad dw, int32_t blocks, bool dw_first) {
+    typedef gemm::Tile<T, BM, BN, WM, WN, BK, STAGES, true, true> G;
+    constexpr int LDS = G::LDS_BYTES < BM * BN * 2 ? BM * BN * 2 : G::LDS_BYTES;
+    __shared__ __attribute__((aligned(16))) char lds[LDS];
+    const bool first = (int)blockIdx.x < blocks;
+    const uint32_t block = first ? blockIdx.x : blockIdx.x - blocks;
+    if (first == dw_first)
+        grad_tile<T, BM, BN, WM, WN, BK, STAGES, true>(dw, block, lds);
+    else
+        grad_tile<T, BM, BN, WM, WN, BK, STAGES, false>(dx, block, lds);
+}
+
 // Sums of the splits, in order, a thread 4 columns.
-__global__ __launch_bounds__(256) void grad_join_kernel(const float *part, int32_t splits, GradOut o) {
+__device__ __forceinline__ void join(const Grad &P, int64_t first, int64_t step) {
+    const GradOut &o = P.o;
     const uint32_t per = ((uint32_t)o.n + 3) / 4;
     const int64_t count = o.m * per, size = o.m * o.n;
     const float factor = factor_of(o);
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
+    for (int64_t i = first; i < count; i += step) {
         const int64_t m = i / per;
         const int n = (int)(i - m * per) * 4;
-        const float *p = part + m * o.n + n;
+        const float *p = P.part + m * o.n + n;
         f32x4 v = {};
         if (n + 4 <= o.n) {
             v = *(const f32x4_any *)p;
 #pragma unroll 4
-            for (int s = 1; s < splits; ++s) v += *(const f32x4_any *)(p + s * size);
+            for (int s = 1; s < P.splits; ++s) v += *(const f32x4_any *)(p + s * size);
         } else
 #pragma unroll
             for (int d = 0; d < 3; ++d)
                 if (n + d < o.n)
-                    for (int s = 0; s < splits; ++s) v[d] += p[s * size + d];
+                    for (int s = 0; s < P.splits; ++s) v[d] += p[s * size + d];
         put4(o, factor, m, n, v);
     }
 }
 
-template <class T, int BM, int BN, int WM, int WN, int BK, int STAGES, int OCC>
-static hipError_t launch(bool atr, Grad p, hipStream_t st) {
-    p.tiles_m = (int32_t)((p.o.m + BM - 1) / BM);
-    p.tiles_n = (p.o.n + BN - 1) / BN;
-    const int64_t nb = (int64_t)p.tiles_m * p.tiles_n * p.splits;
-    if (nb <= 0) return hipSuccess;
-    if (nb > 0x3FFFFFFF) return hipErrorInvalidValue;
-    if (atr)
-        hipLaunchKernelGGL((grad_kernel<T, BM, BN, WM, WN, BK, STAGES, OCC, true>), dim3((uint32_t)nb),
-                           dim3(WM * WN * 64), 0, st, p);
+__global__ __launch_bounds__(256) void grads_join_kernel(const Grad a, const Grad b, int32_t blocks) {
+    if ((int)blockIdx.x < blocks)
+        join(a, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)blocks * 256);
     else
-        hipLaunchKernelGGL((grad_kernel<T, BM, BN, WM, WN, BK, STAGES, OCC, false>), dim3((uint32_t)nb),
-                           dim3(WM * WN * 64), 0, st, p);
-    if (p.splits > 1) {
-        const int64_t blocks = (p.o.m * ((p.o.n + 3) / 4) + 255) / 256;
-        hipLaunchKernelGGL(grad_join_kernel, dim3((uint32_t)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, st, p.part,
-                           p.splits, p.o);
+        join(b, (int64_t)(blockIdx.x - blocks) * 256 + threadIdx.x, (int64_t)(gridDim.x - blocks) * 256);
+}
+
+static int32_t join_blocks(const Grad &p) {
+    if (p.splits <= 1) return 0;
+    const int64_t blocks = (p.o.m * ((p.o.n + 3) / 4) + 255) / 256;
+    return (int32_t)(blocks < 65536 ? blocks : 65536);
+}
+
+// Either may be null.
+template <class T, int BM, int BN, int WM, int WN, int BK, int STAGES, int OCC>
+static hipError_t launch(const Grad *dx, const Grad *dw, hipStream_t st) {
+    Grad x = {}, w = {};
+    int64_t nx = 0, nw = 0;
+    auto tiles = [](Grad &p) {
+        p.tiles_m = (int32_t)((p.o.m + BM - 1) / BM);
+        p.tiles_n = (p.o.n + BN - 1) / BN;
+        return (int64_t)p.tiles_m * p.tiles_n * p.splits;
+    };
+    if (dx) {
+        x = *dx;
+        nx = tiles(x);
     }
+    if (dw) {
+        w = *dw;
+        nw = tiles(w);
+    }
+    if (nx + nw <= 0) return hipSuccess;
+    // a workgroup has up to 512 threads, a launch 2^32
+    if (nx + nw > 0x7FFFFF) return hipErrorInvalidValue;
+    // the longer reductions first
+    const bool dw_first = nx == 0 || (nw > 0 && w.k_split > x.k_split);
+    hipLaunchKernelGGL((grads_kernel<T, BM, BN, WM, WN, BK, STAGES, OCC>), dim3((uint32_t)(nx + nw)), dim3(WM * WN * 64), 0, st,
+                       x, w, (int32_t)(dw_first ? nw : nx), dw_first);
+    const int32_t jx = nx > 0 ? join_blocks(x) : 0, jw = nw > 0 ? join_blocks(w) : 0;
+    if (jx + jw > 0)
+        hipLaunchKernelGGL(grads_join_kernel, dim3((uint32_t)(jx + jw)), dim3(256), 0, st, x, w, jx);
     return hipGetLastError();
 }
 
 template <class T>
-static hipError_t launch_t(Config cfg, bool atr, const Grad &p, hipStream_t st) {
-    if (cfg == TILE_256) return launch<T, 256, 256, 2, 4, 64, 2, 2>(atr, p, st);
-    return launch<T, 128, 128, 2, 2, 64, 2, 2>(atr, p, st);
+static hipError_t launch_t(Config cfg, const Grad *dx, const Grad *dw, hipStream_t st) {
+    if (cfg == TILE_256) return launch<T, 256, 256, 2, 4, 64, 2, 2>(dx, dw, st);
+    return launch<T, 128, 128, 2, 2, 64, 2, 2>(dx, dw, st);
 }
 
-hipError_t launch_grad(int dtype, Config cfg, bool atr, Grad p, hipStream_t st) {
-    return dtype == Half::id ? launch_t<Half>(cfg, atr, p, st) : launch_t<BFloat>(cfg, atr, p, st);
+static hipError_t launch_pair(int dtype, Config cfg, const Grad *dx, const Grad *dw, hipStream_t st) {
+    return dtype == Half::id ? launch_t<Half>(cfg, dx, dw, st) : launch_t<BFloat>(cfg, dx, dw, st);
+}
+
+hipError_t launch_grads(int dtype, Config cfg, const Grad &dx, Config cfg_w, const Grad *dw, hipStream_t st) {
+    if (!dw || cfg == cfg_w) return launch_pair(dtype, cfg, &dx, dw, st);
+    const hipError_t e = launch_pair(dtype, cfg, &dx, nullptr, st);
+    return e == hipSuccess ? launch_pair(dtype, cfg_w, nullptr, dw, st) : e;
+}
+
+hipError_t launch_grad_w(int dtype, Config cfg, const Grad &dw, hipStream_t st) {
+    return launch_pair(dtype, cfg, nullptr, &dw, st);
 }
 
 }  // namespace xent

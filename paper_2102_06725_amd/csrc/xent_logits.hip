@@ -154,7 +154,7 @@ static hipError_t launch(Logits p, hipStream_t st) {
     p.tiles_n = (int32_t)(((int64_t)p.w.extent + BN - 1) / BN);
     const int64_t nb = (int64_t)p.tiles_m * p.tiles_n;
     if (nb <= 0) return hipSuccess;
-    if (nb > 0x3FFFFFFF) return hipErrorInvalidValue;
+    if (nb > 0x7FFFFF) return hipErrorInvalidValue;  // a launch has 2^32 threads at most
     if (p.e)
         hipLaunchKernelGGL((logits_kernel<T, BM, BN, WM, WN, BK, STAGES, OCC, true>), dim3((uint32_t)nb),
                            dim3(WM * WN * 64), 0, st, p);

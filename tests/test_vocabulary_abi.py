@@ -81,7 +81,7 @@ def test_xent_descriptors(nnlib, kw):
 
 @pytest.mark.parametrize("kw", [dict(dtype=nc.NNCONV_F32), dict(dtype=nc.NNCONV_F8), dict(teacher_dtype=nc.NNCONV_F8),
                                 dict(teacher_dtype=nc.NNCONV_BF16), dict(k=1025), dict(rows=(1 << 23) + 1), dict(c=(1 << 20) + 1),
-                                dict(v=(1 << 21) + 1)])
+                                dict(v=(1 << 21) + 1), dict(v=1 << 20, c=(1 << 15) + 8), dict(rows=1 << 23, c=(1 << 12) + 8)])
 def test_xent_limits(nnlib, kw):
     d = xent(**kw)
     assert xfwd(d) == xtrain(d) == nc.nnconv_xent_workspace_size(d, nc.NNCONV_DGRAD)[0] == UNS
