@@ -41,8 +41,8 @@ struct Stage {
     int32_t k[LOADS];        // its reduction index within a slice
 
     // 16-byte chunk swizzle of a row of KCH chunks: a fragment read has 16 rows at one chunk.
-    static __device__ __forceinline__ int swz(int r) { return KCH == 16 ? r & 15 : KCH == 8 ? (r >> 1) & 7 : (r >> 2) & 3; }
-    static_assert(KCH == 4 || KCH == 8 || KCH == 16, "swizzle");
+    static __device__ __forceinline__ int swz(int r) { return KCH == 8 ? (r >> 1) & 7 : (r >> 2) & 3; }
+    static_assert(KCH == 4 || KCH == 8, "swizzle");
     // 64-byte segments of rows across the reduction: the 4 rows of a transposing read fall in
     // four segments of the banks.
     static __device__ __forceinline__ int seg(int p) { return ROWB >= 256 ? p & 3 : (p >> 1) & 1; }

@@ -203,6 +203,10 @@ struct Join {
     uint16_t *e;                // training: [rows][lde]
     int64_t lde, stretch;       // elements of a workgroup
     int32_t parts;              // workgroups of a row
+    // [rows][c], or null: x, to be copied with zeros in rows that do not count, in 16-byte vectors
+    const uint16_t *x;
+    uint16_t *xc;
+    int32_t c;
 };
 
 // The largest logit of a row, and the sum of the exponentials against it, by one wave.
@@ -279,6 +283,9 @@ __global__ __launch_bounds__(256) void scale_kernel(const Join P) {
     join_row(s, P.tiles, most, sum);
     const float log_sum = log2f(sum), over = GRAD_UNIT / sum;
     if (part == 0 && threadIdx.x < 64) put_loss(P, r, counts, most, log_sum);
+    if (P.xc && part == P.parts - 1)
+        for (int c = threadIdx.x * 8; c < P.c; c += 2048)
+            *(u32x4 *)(P.xc + r * P.c + c) = counts ? *(const u32x4 *)(P.x + r * P.c + c) : u32x4{};
     for (;;) {
         float f[4];
 #pragma unroll
@@ -357,7 +364,7 @@ struct Plan {
     int64_t ldx, ldw, lde, piece;
     Shape logits, dx, dw;
     int32_t tiles;  // stats a row
-    bool copy_w, copy_x;
+    bool copy_w, copy_x, late_x;
     size_t xc, wc, zt, qi, qt, base, stats, e, part, part_w, acc, bytes;
 };
 
@@ -365,9 +372,10 @@ static Plan plan_of(const XentParams &p, bool train) {
     Plan q;
     q.ldx = q.ldw = (p.c + 7) / 8 * 8;
     q.copy_w = p.c % 8 != 0;
-    // rows that do not count may hold NaN, which the product for dw would meet; a teacher's rows are
-    // copied beside its softmax
-    q.copy_x = q.copy_w || p.sizes_only || p.teacher || (train && p.dw) || ((uintptr_t)p.x & 15) != 0;
+    // rows that do not count may hold NaN, which the product for dw would meet: it reads a copy, made
+    // beside a teacher's softmax or, where x is read as it is before, by scale_kernel
+    q.copy_x = q.copy_w || p.teacher || ((uintptr_t)p.x & 15) != 0;
+    q.late_x = !q.copy_x && train && p.dw;
     q.lde = ((int64_t)p.v + 63) / 64 * 64;
     const int64_t most = (train ? PIECE_BYTES / (2 * q.lde) : STATS_BYTES / (8 * (((int64_t)p.v + 127) / 128))) / 256 * 256;
     q.piece = p.rows;
@@ -384,7 +392,7 @@ static Plan plan_of(const XentParams &p, bool train) {
         at += align256(bytes);
         return was;
     };
-    q.xc = take(q.copy_x ? (size_t)p.rows * q.ldx * 2 : 0);
+    q.xc = take(q.copy_x || q.late_x || p.sizes_only ? (size_t)p.rows * q.ldx * 2 : 0);
     q.wc = take(q.copy_w ? (size_t)p.v * q.ldw * 2 : 0);
     q.zt = take((size_t)p.rows * p.k * 4);
     q.qi = take((size_t)p.rows * p.k * 4);
@@ -514,6 +522,9 @@ hipError_t launch_xent(const XentParams &p, bool train, hipStream_t st) {
         j.lse = p.lse ? p.lse + r0 : nullptr;
         j.e = l.e;
         j.lde = q.lde;
+        j.x = q.late_x ? x + r0 * p.c : nullptr;
+        j.xc = q.late_x ? r.xc + r0 * p.c : nullptr;
+        j.c = p.c;
         if (!train) {
             hipLaunchKernelGGL(join_kernel, dim3((uint32_t)((n + 3) / 4)), dim3(256), 0, st, j);
             continue;
@@ -536,7 +547,7 @@ hipError_t launch_xent(const XentParams &p, bool train, hipStream_t st) {
         g.part = at(q.part);
         g.o = {(uint16_t *)p.dx + r0 * p.c, p.dtype, p.c, n, alpha, p.grad_scale, 0, p.flag, nullptr, nullptr};
         d.a = {l.e, q.lde, (int32_t)q.lde};
-        d.b = {l.x.p, q.ldx, (int32_t)q.ldx};
+        d.b = {q.late_x ? j.xc : l.x.p, q.ldx, (int32_t)q.ldx};
         d.k = n;
         d.k_split = q.dw.k_split;
         d.splits = q.dw.splits;

@@ -593,6 +593,17 @@ class _Handle:
                 self._refuse(name, t, "%d%s dense elements of %s on device %d" % (count, " or more" if more else "", dtype, gpu))
 
 
+    @staticmethod
+    def _all_fit(gpu, *kinds):
+        """Whether dense tensors of (type, elements, tensors) are these."""
+        try:
+            for dtype, count, tensors in kinds:
+                if not _all_dense(tensors, dtype, count, gpu):
+                    return False
+        except AttributeError:  # an object that is no tensor
+            return False
+        return True
+
     def _gradient(self, name, t, count, gpu):
         """The type code of a parameter's gradient: fp32, or as the operands."""
         if not isinstance(t, self._tensor):
@@ -600,7 +611,8 @@ class _Handle:
                 raise ValueError("%s: %s is needed" % (type(self).__name__, name))
             return NNCONV_F32
         wide = t.dtype is self._f32
-        self._dense(self._f32 if wide else self._dtype, count, gpu, **{name: t})
+        if not _all_dense((t,), self._f32 if wide else self._dtype, count, gpu):
+            self._dense(self._f32 if wide else self._dtype, count, gpu, **{name: t})
         return NNCONV_F32 if wide else self.desc.dtype
 
 
@@ -888,37 +900,40 @@ class Embedding(_Handle):
 
     def __init__(self, rows, c, v, dtype=NNCONV_F16, scale=1.0):
         super().__init__(nnconv_embedding_desc(rows, c, v, dtype, scale), dtype)
+        self._rows, self._c, self._v = rows, c, v
         self._ws = _Workspaces()
         self._nbytes = None
 
     @property
     def rows(self):
-        return self.desc.rows
+        return self._rows
 
     @rows.setter
     def rows(self, rows):
-        self.desc.rows = rows
+        self.desc.rows = self._rows = rows
         self._nbytes = None
 
     def fwd(self, ids, table, y, stream=None):
-        d, gpu = self.desc, self._gpu("ids", ids)
-        self._dense(self._i32, d.rows, gpu, ids=ids)
-        self._dense(self._dtype, d.v * d.c, gpu, table=table)
-        self._dense(self._dtype, d.rows * d.c, gpu, y=y)
+        rows, c, gpu = self._rows, self._c, self._gpu("ids", ids)
+        if not self._all_fit(gpu, (self._i32, rows, (ids,)), (self._dtype, self._v * c, (table,)), (self._dtype, rows * c, (y,))):
+            self._dense(self._i32, rows, gpu, ids=ids)
+            self._dense(self._dtype, self._v * c, gpu, table=table)
+            self._dense(self._dtype, rows * c, gpu, y=y)
         check(self._lib.nnconv_embedding_fwd(self._ref, ids.data_ptr(), _ptr(table), _ptr(y), self._stream(stream, gpu)),
               "nnconv_embedding_fwd")
 
     def bwd(self, ids, dy, dtable, inv_loss_scale=1.0, accumulate=0, overflow_flag=None, stream=None):
         """dtable: fp32 or of the table's type."""
-        d, gpu = self.desc, self._gpu("ids", ids)
-        self._dense(self._i32, d.rows, gpu, ids=ids)
-        self._dense(self._dtype, d.rows * d.c, gpu, dy=dy)
-        kind = self._gradient("dtable", dtable, d.v * d.c, gpu)
+        rows, c, gpu = self._rows, self._c, self._gpu("ids", ids)
+        if not self._all_fit(gpu, (self._i32, rows, (ids,)), (self._dtype, rows * c, (dy,))):
+            self._dense(self._i32, rows, gpu, ids=ids)
+            self._dense(self._dtype, rows * c, gpu, dy=dy)
+        kind = self._gradient("dtable", dtable, self._v * c, gpu)
         if overflow_flag is not None:
             self._dense(self._i32, 1, gpu, more=True, overflow_flag=overflow_flag)
         stream = self._stream(stream, gpu)
         if self._nbytes is None:
-            st, self._nbytes = nnconv_embedding_workspace_size(d)
+            st, self._nbytes = nnconv_embedding_workspace_size(self.desc)
             check(st, "nnconv_embedding_workspace_size")
         ws = self._ws.get("bwd", stream, self._nbytes, ids.device)
         check(self._lib.nnconv_embedding_bwd(
@@ -935,7 +950,8 @@ class CrossEntropy(_Handle):
 
     def __init__(self, rows, c, v, dtype=NNCONV_F16, logit_scale=1.0, k=None, teacher_dtype=NNCONV_F32):
         import torch
-        super().__init__(nnconv_xent_desc(rows, c, v, dtype, 1 if k is None else k, teacher_dtype, logit_scale), dtype)
+        self._rows, self._c, self._v, self._k = rows, c, v, 1 if k is None else k
+        super().__init__(nnconv_xent_desc(rows, c, v, dtype, self._k, teacher_dtype, logit_scale), dtype)
         self._teacher = None if k is None else {
             NNCONV_F16: torch.float16, NNCONV_BF16: torch.bfloat16}.get(teacher_dtype, torch.float32)
         self._ws = _Workspaces()
@@ -943,11 +959,11 @@ class CrossEntropy(_Handle):
 
     @property
     def rows(self):
-        return self.desc.rows
+        return self._rows
 
     @rows.setter
     def rows(self, rows):
-        self.desc.rows = rows
+        self.desc.rows = self._rows = rows
         self._sizes.clear()
 
     def _workspace(self, pass_, stream, x):
@@ -958,16 +974,20 @@ class CrossEntropy(_Handle):
             self._sizes[pass_] = nb
         return self._ws.get(pass_, stream, nb, x.device), nb
 
-    def _operands(self, gpu, x, w, targets, teacher, loss, lse):
-        d = self.desc
+    def _operands(self, gpu, x, w, targets, teacher, loss, lse, dx=None):
+        rows, wide, pairs = self._rows, self._rows * self._c, self._rows * self._k
         if (teacher is None) != (self._teacher is None):
             raise ValueError("CrossEntropy: teacher: %s" % ("made with labels" if self._teacher is None else "is needed"))
-        self._dense(self._dtype, d.rows * d.c, gpu, x=x)
-        self._dense(self._dtype, d.v * d.c, gpu, w=w)
-        self._dense(self._i32, d.rows * d.k, gpu, targets=targets)
+        if self._all_fit(gpu, (self._dtype, wide, (x, dx)), (self._dtype, self._v * self._c, (w,)), (self._i32, pairs, (targets,)),
+                         (self._f32, rows, (loss, lse)), (self._teacher, pairs, (teacher,))):
+            return
+        self._dense(self._dtype, wide, gpu, x=x)
+        self._dense(self._dtype, self._v * self._c, gpu, w=w)
+        self._dense(self._i32, pairs, gpu, targets=targets)
         if teacher is not None:
-            self._dense(self._teacher, d.rows * d.k, gpu, teacher=teacher)
-        self._dense(self._f32, d.rows, gpu, loss=loss, lse=lse)
+            self._dense(self._teacher, pairs, gpu, teacher=teacher)
+        self._dense(self._f32, rows, gpu, loss=loss, lse=lse)
+        self._dense(self._dtype, wide, gpu, dx=dx)
 
     def fwd(self, x, w, targets, loss, lse=None, teacher=None, stream=None):
         gpu = self._gpu("x", x)
@@ -981,10 +1001,9 @@ class CrossEntropy(_Handle):
     def train(self, x, w, targets, loss, dx, dw=None, lse=None, teacher=None, alpha=1.0, grad_scale=None, inv_loss_scale=1.0,
               accumulate=0, overflow_flag=None, stream=None):
         """dw: fp32 or of w's type; grad_scale: an fp32 tensor of one element."""
-        d, gpu = self.desc, self._gpu("x", x)
-        self._operands(gpu, x, w, targets, teacher, loss, lse)
-        self._dense(self._dtype, d.rows * d.c, gpu, dx=dx)
-        kind = NNCONV_F32 if dw is None else self._gradient("dw", dw, d.v * d.c, gpu)
+        gpu = self._gpu("x", x)
+        self._operands(gpu, x, w, targets, teacher, loss, lse, dx)
+        kind = NNCONV_F32 if dw is None else self._gradient("dw", dw, self._v * self._c, gpu)
         if grad_scale is not None:
             self._dense(self._f32, 1, gpu, more=True, grad_scale=grad_scale)
         if overflow_flag is not None:
