@@ -231,6 +231,32 @@ __device__ __forceinline__ void dma16(uint32_t lds_addr, uint32_t voff, i32x4 de
         : "memory");
 }
 
+// 8 of a row's n 16-bit elements from c < n on, zeros behind the last, at any alignment: a row's end
+// is read as its last 8 elements and moved (an element at a time a wave would wait for each load).
+// SHORT: rows of fewer than 8.
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+template <bool SHORT>
+__device__ __forceinline__ u32x4 row_vector(const uint16_t *row, int c, int n) {
+    if constexpr (SHORT) {
+        u32x4 v = {};
+#pragma unroll
+        for (int d = 0; d < 7; ++d)
+            if (c + d < n) v[d >> 1] |= (uint32_t)row[c + d] << (16 * (d & 1));
+        return v;
+    }
+    const int at = c + 8 <= n ? c : n - 8;
+    u32x4 v = *(const u32x4_any *)(row + at);
+    if (n % 8 == 0) return v;
+    const int by = (c - at) * 16;
+    const uint64_t lo = v[0] | (uint64_t)v[1] << 32, hi = v[2] | (uint64_t)v[3] << 32;
+    const uint64_t a = by >= 64 ? hi >> (by - 64) : by > 0 ? lo >> by | hi << (64 - by) : lo;
+    const uint64_t b = by >= 64 ? 0 : hi >> by;
+    return u32x4{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
+}
+__device__ __forceinline__ u32x4 row_vector(const uint16_t *row, int c, int n) {
+    return n < 8 ? row_vector<true>(row, c, n) : row_vector<false>(row, c, n);
+}
+
 // A 16-bit tensor of any layout, read where it lies: element (n, c, h, w) at
 // p[n * sn + c * sc + h * sh + w * sw]; channels from `c` on are zero.
 struct StridedTensor {

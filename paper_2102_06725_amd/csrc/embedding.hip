@@ -5,14 +5,15 @@
 // every time), spans of sorted tokens are summed by a team of threads each, and rows whose tokens
 // reach over several spans are joined from their parts.  The launches that sort wait for their own
 // loads and barriers mostly; further workgroups of theirs clear the table meanwhile, the rows that
-// tokens name too (32768 tokens of 1152 channels, 32768 rows in fp32: 75 us a backward pass, 84 with rows looked up and cleared beside the sums).
+// tokens name too (32768 tokens of 1152 channels, 32768 rows in fp32: 74 us a
+// backward pass, 84 with rows looked up and cleared beside the sums).
 #include "launch.hpp"
 
 namespace nnconv {
 
 namespace embedding {
 
-typedef u32x4 __attribute__((aligned(2))) u32x4_any;  // 16 bytes at any element
+typedef u32x4 __attribute__((aligned(4))) u32x4_any4;
 typedef f32x4 __attribute__((aligned(4))) f32x4_any;
 
 template <class T>
@@ -288,9 +289,9 @@ __global__ __launch_bounds__(64 * WAVES) void sort_kernel(const Sort P) {
 
 // --- sums ------------------------------------------------------------------------------
 
-// Sorted tokens of a team, a multiple of 8: 32, and 8 where there are few, since each row's end is a
-// round trip to memory where it is added to what is there (5003 tokens of 771 channels: 39 us a
-// backward pass with 8, 52 with 16, 81 with 32; 32768 of 1152: 95 with 8, 86 with 16, 84 with 32).
+// Sorted tokens of a team, a multiple of 8: 32, and 8 where there are few and their teams would leave
+// most of the chip idle (5003 tokens of 771 channels added to what is there: 33 us a backward pass
+// with 8, 40 with 16, 56 with 32; 32768 of 1152: 11 us more with 8 than with 32).
 constexpr int SPAN = 32, SMALL_SPAN = 8;
 constexpr int64_t FEW_TOKENS = 16384;
 constexpr int LEAST_TEAM = 4;   // threads of one, of 8 channels each
@@ -308,71 +309,95 @@ struct Sums {
     float *part;             // [2 * spans][cp]: of a span, what belongs to the row of the span before, and to the next's
 };
 
-// 8 values of row `j` from channel c on to the gradient.
-__device__ __forceinline__ void put8(const Sums &P, int64_t j, int c, const float (&s)[8]) {
-    const int64_t i = j * P.c + c;
-    const int n = P.c - c < 8 ? P.c - c : 8;
-    float v[8];
-    bool bad = false;
+// What is at 8 channels of a row of the gradient, fp32 in both or 16 bits in `lo`.
+struct Old {
+    u32x4 lo, hi;
+};
+
+template <bool WIDE, bool SHORT>
+__device__ __forceinline__ Old read8(const Sums &P, int64_t j, int c) {
+    Old o = {};
+    if constexpr (!WIDE) {
+        o.lo = row_vector<SHORT>((const uint16_t *)P.dtable + j * P.c, c, P.c);
+        return o;
+    }
+    const uint32_t *row = (const uint32_t *)P.dtable + j * P.c;
+    if constexpr (SHORT) {
 #pragma unroll
-    for (int d = 0; d < 8; ++d) v[d] = s[d] * P.factor;
-    if (P.kind == 2) {
-        float *o = (float *)P.dtable + i;
-        if (n == 8) {
-            f32x4 lo = {v[0], v[1], v[2], v[3]}, hi = {v[4], v[5], v[6], v[7]};
-            if (P.accumulate) {
-                lo += *(const f32x4_any *)o;
-                hi += *(const f32x4_any *)(o + 4);
-            }
-            *(f32x4_any *)o = lo;
-            *(f32x4_any *)(o + 4) = hi;
+        for (int d = 0; d < 7; ++d)
+            if (c + d < P.c) (d < 4 ? o.lo : o.hi)[d & 3] = row[c + d];
+        return o;
+    }
+    // a row's end as its last 8 elements, moved
+    const int at = c + 8 <= P.c ? c : P.c - 8;
+    o.lo = *(const u32x4_any4 *)(row + at);
+    o.hi = *(const u32x4_any4 *)(row + at + 4);
+    if (P.c % 8 == 0) return o;
+    const int by = c - at;
+    if (by & 4) {
+        o.lo = o.hi;
+        o.hi = u32x4{};
+    }
 #pragma unroll
-            for (int d = 0; d < 4; ++d) bad |= !__builtin_isfinite(lo[d]) || !__builtin_isfinite(hi[d]);
-        } else
-            for (int d = 0; d < n; ++d) {
-                float x = 0.f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x = e == d ? v[e] : x;
-                if (P.accumulate) x += o[d];
-                o[d] = x;
-                bad |= !__builtin_isfinite(x);
-            }
-    } else {
-        uint16_t *o = (uint16_t *)P.dtable + i;
-        const bool half = P.kind == Half::id;
-        u32x4 old = {}, out;
-        if (P.accumulate) {
-            if (n == 8)
-                old = *(const u32x4_any *)o;
-            else
-#pragma unroll
-                for (int d = 0; d < 8; ++d)
-                    if (d < n) old[d >> 1] |= (uint32_t)o[d] << (16 * (d & 1));
+    for (int u = 1; u <= 2; u *= 2)
+        if (by & u) {
+            const u32x4 l = o.lo, h = o.hi;
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
-                v[2 * d] += half ? from16<Half>(old[d]) : from16<BFloat>(old[d]);
-                v[2 * d + 1] += half ? from16<Half>(old[d] >> 16) : from16<BFloat>(old[d] >> 16);
+                o.lo[d] = d + u < 4 ? l[(d + u) & 3] : h[(d + u) & 3];
+                o.hi[d] = d + u < 4 ? h[(d + u) & 3] : 0u;
             }
         }
-        const uint32_t top = half ? 0x7C00u : 0x7F80u;
+    return o;
+}
+
+// 8 values of row `j` from channel c on to the gradient, added to `old` (zeros without accumulate).
+template <class T, bool WIDE>
+__device__ __forceinline__ void put8(const Sums &P, int64_t j, int c, const float (&s)[8], const Old &old) {
+    const int64_t i = j * P.c + c;
+    const int n = P.c - c;
+    bool bad = false;
+    if constexpr (WIDE) {
+        float *o = (float *)P.dtable + i;
+        f32x4 lo = __builtin_bit_cast(f32x4, old.lo), hi = __builtin_bit_cast(f32x4, old.hi);
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
-            out[d] = half ? pack16<Half>(v[2 * d], v[2 * d + 1]) : pack16<BFloat>(v[2 * d], v[2 * d + 1]);
-            bad |= (2 * d < n && (out[d] & top) == top) || (2 * d + 1 < n && ((out[d] >> 16) & top) == top);
+            lo[d] += s[d] * P.factor;
+            hi[d] += s[d + 4] * P.factor;
+            // zeros behind the row's end are finite
+            bad |= !__builtin_isfinite(lo[d]) | !__builtin_isfinite(hi[d]);
         }
-        if (n == 8)
+        if (n >= 8) {
+            *(f32x4_any *)o = lo;
+            *(f32x4_any *)(o + 4) = hi;
+        } else
+#pragma unroll
+            for (int d = 0; d < 7; ++d)
+                if (d < n) o[d] = d < 4 ? lo[d & 3] : hi[d & 3];
+    } else {
+        uint16_t *o = (uint16_t *)P.dtable + i;
+        constexpr uint32_t TOP = T::id == Half::id ? 0x7C00u : 0x7F80u;
+        u32x4 out;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+            out[d] = pack16<T>(from16<T>(old.lo[d]) + s[2 * d] * P.factor, from16<T>(old.lo[d] >> 16) + s[2 * d + 1] * P.factor);
+            bad |= ((out[d] & TOP) == TOP) | (((out[d] >> 16) & TOP) == TOP);
+        }
+        if (n >= 8)
             *(u32x4_any *)o = out;
         else
 #pragma unroll
-            for (int d = 0; d < 8; ++d)
+            for (int d = 0; d < 7; ++d)
                 if (d < n) o[d] = (uint16_t)(out[d >> 1] >> (16 * (d & 1)));
     }
     if (bad && P.flag) *P.flag = 1;
 }
 
 // Workgroups of teams, a span each: runs of equal numbers.  A run that begins and ends in its span
-// is a row's whole sum.  Loads of 8 tokens are on their way at once.
-template <class T>
+// is a row's whole sum.  Loads of 8 tokens are on their way at once, and with them of what their rows
+// are added to.  Types are compiled in: with them chosen at run time the code of 8 tokens passed the
+// instruction cache, 5 us of the 38 that a pass over 5003 tokens of 771 channels took.
+template <class T, bool WIDE, bool ACCUMULATE, bool SHORT>
 __global__ __launch_bounds__(256) void sum_kernel(const Sums P) {
     __shared__ uint32_t key[256 / LEAST_TEAM * SPAN + 2], row[256 / LEAST_TEAM * SPAN];  // key[0]: the one before
     const int teams = 256 / P.team;
@@ -393,22 +418,17 @@ __global__ __launch_bounds__(256) void sum_kernel(const Sums P) {
     if (n <= 0 || c >= P.c) return;
     const int64_t span = (int64_t)blockIdx.x * teams + team;
     const uint32_t *k = key + 1 + begin;
-    const bool whole = c + 8 <= P.c;
     float sum[8] = {};
     bool begun = k[-1] == k[0];  // the run reaches in from the span before
     for (int i0 = 0; i0 < n; i0 += 8) {
         u32x4 v[8];
+        Old old[8] = {};
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
             v[u] = u32x4{};
             if (i0 + u >= n || k[i0 + u] >= (uint32_t)P.v) continue;  // padding is not read
-            const uint16_t *src = P.dy + (int64_t)row[begin + i0 + u] * P.c + c;
-            if (whole)
-                v[u] = *(const u32x4_any *)src;
-            else
-#pragma unroll
-                for (int d = 0; d < 7; ++d)
-                    if (c + d < P.c) v[u][d >> 1] |= (uint32_t)src[d] << (16 * (d & 1));
+            if (ACCUMULATE && k[i0 + u + 1] != k[i0 + u]) old[u] = read8<WIDE, SHORT>(P, k[i0 + u], c);
+            v[u] = row_vector<SHORT>(P.dy + (int64_t)row[begin + i0 + u] * P.c, c, P.c);
         }
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
@@ -426,7 +446,7 @@ __global__ __launch_bounds__(256) void sum_kernel(const Sums P) {
                 *(f32x4 *)to = f32x4{sum[0], sum[1], sum[2], sum[3]};
                 *(f32x4 *)(to + 4) = f32x4{sum[4], sum[5], sum[6], sum[7]};
             } else
-                put8(P, k[i], c, sum);
+                put8<T, WIDE>(P, k[i], c, sum, old[u]);
 #pragma unroll
             for (int d = 0; d < 8; ++d) sum[d] = 0.f;
             begun = false;
@@ -435,6 +455,7 @@ __global__ __launch_bounds__(256) void sum_kernel(const Sums P) {
 }
 
 // A workgroup a span: the row whose run begins in it and goes on behind it.
+template <class T, bool WIDE, bool ACCUMULATE, bool SHORT>
 __global__ __launch_bounds__(256) void join_kernel(const Sums P) {
     const int64_t s = blockIdx.x, last = s * P.span + P.span - 1;
     if (last + 1 >= P.rows) return;
@@ -474,7 +495,7 @@ __global__ __launch_bounds__(256) void join_kernel(const Sums P) {
             hi += *(const f32x4 *)(next + 4);
         }
         const float sum[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        put8(P, k, c, sum);
+        put8<T, WIDE>(P, k, c, sum, ACCUMULATE ? read8<WIDE, SHORT>(P, k, c) : Old{});
     }
 }
 
@@ -558,6 +579,26 @@ static void sort_one(const Sort &q, Clear &all, const Layout &l, char *ws, int b
                        (uint32_t *)(ws + l.key[0]), (uint32_t *)(ws + l.row[0]), part);
 }
 
+template <class T, bool WIDE, bool ACCUMULATE, bool SHORT>
+static void launch_sums(const Sums &s, dim3 grid, uint32_t spans, hipStream_t st) {
+    hipLaunchKernelGGL((sum_kernel<T, WIDE, ACCUMULATE, SHORT>), grid, dim3(256), 0, st, s);
+    if (spans > 1)
+        hipLaunchKernelGGL((join_kernel<T, WIDE, ACCUMULATE, SHORT>), dim3(spans, grid.y < 64 ? grid.y : 64), dim3(256), 0, st, s);
+}
+
+template <class T, bool WIDE, bool ACCUMULATE>
+static void launch_sums(const Sums &s, dim3 grid, uint32_t spans, hipStream_t st) {
+    s.c < 8 ? launch_sums<T, WIDE, ACCUMULATE, true>(s, grid, spans, st) : launch_sums<T, WIDE, ACCUMULATE, false>(s, grid, spans, st);
+}
+
+template <class T>
+static void launch_sums(const Sums &s, dim3 grid, uint32_t spans, hipStream_t st) {
+    if (s.kind == 2)
+        s.accumulate ? launch_sums<T, true, true>(s, grid, spans, st) : launch_sums<T, true, false>(s, grid, spans, st);
+    else
+        s.accumulate ? launch_sums<T, false, true>(s, grid, spans, st) : launch_sums<T, false, false>(s, grid, spans, st);
+}
+
 }  // namespace embedding
 
 using namespace embedding;
@@ -630,13 +671,9 @@ hipError_t launch_embedding_bwd(int dtype, const EmbeddingParams &p, hipStream_t
     const int64_t teams = 256 / s.team;
     const dim3 grid((uint32_t)((l.spans + teams - 1) / teams), (uint32_t)((vectors + 255) / 256));
     if (dtype == Half::id)
-        hipLaunchKernelGGL((sum_kernel<Half>), grid, dim3(256), 0, st, s);
+        launch_sums<Half>(s, grid, (uint32_t)l.spans, st);
     else
-        hipLaunchKernelGGL((sum_kernel<BFloat>), grid, dim3(256), 0, st, s);
-    if (l.spans > 1) {
-        const uint32_t cols = grid.y < 64 ? grid.y : 64;
-        hipLaunchKernelGGL(join_kernel, dim3((uint32_t)l.spans, cols), dim3(256), 0, st, s);
-    }
+        launch_sums<BFloat>(s, grid, (uint32_t)l.spans, st);
     return hipGetLastError();
 }
 

@@ -16,8 +16,6 @@ constexpr int MOST_TARGETS = 1024;
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
-typedef u32x4 __attribute__((aligned(2))) u32x4_any;  // 16 bytes at any element
-
 struct Rows {
     int64_t rows;
     int32_t c, ldx, v, k;
@@ -44,16 +42,6 @@ __device__ __forceinline__ float wave_sum(float v) {
     return v;
 }
 
-// 8 channels from `c` on of a row of n, zeros behind it.
-__device__ __forceinline__ u32x4 channels(const uint16_t *row, int c, int n) {
-    if (c + 8 <= n) return *(const u32x4_any *)(row + c);
-    u32x4 v = {};
-#pragma unroll
-    for (int d = 0; d < 7; ++d)
-        if (c + d < n) v[d >> 1] |= (uint32_t)row[c + d] << (16 * (d & 1));
-    return v;
-}
-
 // Whether this workgroup copies w, 1024 vectors of 8 channels each.
 constexpr int COPY_VECTORS = 1024;
 __device__ __forceinline__ bool copied_w(const Rows &P) {
@@ -65,7 +53,7 @@ __device__ __forceinline__ bool copied_w(const Rows &P) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
         const int64_t i = first + u * 256 + threadIdx.x, r = i / per;
-        if (i < count) v[u] = channels(P.w + r * P.c, (int)(i - r * per) * 8, P.c);
+        if (i < count) v[u] = row_vector(P.w + r * P.c, (int)(i - r * per) * 8, P.c);
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
@@ -84,7 +72,7 @@ __global__ __launch_bounds__(256) void copy_kernel(const Rows P) {
         const int64_t r = i / per;
         const int c = (int)(i - r * per) * 8;
         const bool in = (uint32_t)P.targets[r] < (uint32_t)P.v;
-        *(u32x4 *)(P.xc + r * P.ldx + c) = in ? channels(P.x + r * P.c, c, P.c) : u32x4{};
+        *(u32x4 *)(P.xc + r * P.ldx + c) = in ? row_vector(P.x + r * P.c, c, P.c) : u32x4{};
     }
 }
 
@@ -132,7 +120,7 @@ __global__ __launch_bounds__(256) void rows_kernel(const Rows P) {
     any = __any(any);
     if (blockIdx.y == 0) {
         uint16_t *xc = P.xc + r * P.ldx;
-        for (int c = tid * 8; c < P.ldx; c += 2048) *(u32x4 *)(xc + c) = any ? channels(x, c, P.c) : u32x4{};
+        for (int c = tid * 8; c < P.ldx; c += 2048) *(u32x4 *)(xc + c) = any ? row_vector(x, c, P.c) : u32x4{};
     }
     if (!any) {
         if (blockIdx.y == 0 && tid == 0) P.base[r] = __builtin_bit_cast(float, NOT_COUNTED);
@@ -149,8 +137,8 @@ __global__ __launch_bounds__(256) void rows_kernel(const Rows P) {
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
                     const int c = c0 + u * 128;
-                    b[u] = c < P.c ? channels(w, c, P.c) : u32x4{};
-                    a[u] = c < P.c ? channels(x, c, P.c) : u32x4{};
+                    b[u] = c < P.c ? row_vector(w, c, P.c) : u32x4{};
+                    a[u] = c < P.c ? row_vector(x, c, P.c) : u32x4{};
                 }
 #pragma unroll
                 for (int u = 0; u < 4; ++u) dot = dot8<T>(a[u], b[u], dot);
