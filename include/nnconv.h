@@ -582,8 +582,7 @@ typedef struct {
 } nnconv_embedding_desc;
 
 /* y[r] = scale * table[ids[r]], zeros for padding.  ids: [rows], table: [v][c],
- * y: [rows][c], dense.  16-byte aligned tables and outputs with c a multiple
- * of 8 are the fast ones.
+ * y: [rows][c], dense, any alignment of at least an element.
  * INVALID_ARG: rows < 0, c < 1, v < 1, scale not finite, bad dtype, null
  * pointers; UNSUPPORTED: dtype F32, larger sizes; MISALIGNED:
  * pointers below their element size. */

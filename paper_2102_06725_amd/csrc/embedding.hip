@@ -21,27 +21,27 @@ __device__ __forceinline__ uint32_t scaled(uint32_t two, float f) {
     return pack16<T>(from16<T>(two) * f, from16<T>(two >> 16) * f);
 }
 
-// VEC: rows of whole 16-byte vectors; a thread a vector.  Else a thread an element.
-template <class T, bool VEC>
+// A thread 8 channels of a row, at any alignment.
+template <class T, bool SHORT>
 __global__ __launch_bounds__(256) void fwd_kernel(const EmbeddingParams P) {
-    const uint32_t per = VEC ? (uint32_t)P.c / 8 : (uint32_t)P.c;
+    const uint32_t per = ((uint32_t)P.c + 7) / 8;
     const int64_t count = P.rows * per;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / per;
-        const uint32_t at = (uint32_t)(i - r * per);
+        const int c = (int)(i - r * per) * 8, n = P.c - c;
         const int32_t id = P.ids[r];
         const bool in = (uint32_t)id < (uint32_t)P.v;
-        if constexpr (VEC) {
-            u32x4 v = {};
-            if (in) v = *(const u32x4 *)((const uint16_t *)P.table + (int64_t)id * P.c + at * 8);
+        u32x4 v = {};
+        if (in) v = row_vector<SHORT>((const uint16_t *)P.table + (int64_t)id * P.c, c, P.c);
 #pragma unroll
-            for (int d = 0; d < 4; ++d) v[d] = in ? scaled<T>(v[d], P.scale) : 0u;
-            *(u32x4 *)((uint16_t *)P.y + r * P.c + at * 8) = v;
-        } else {
-            float v = 0.f;
-            if (in) v = from16<T>(((const uint16_t *)P.table)[(int64_t)id * P.c + at]) * P.scale;
-            ((uint16_t *)P.y)[i] = in ? (uint16_t)to16<T>(v) : (uint16_t)0;
-        }
+        for (int d = 0; d < 4; ++d) v[d] = in ? scaled<T>(v[d], P.scale) : 0u;
+        uint16_t *y = (uint16_t *)P.y + r * P.c + c;
+        if (n >= 8)
+            *(u32x4_any *)y = v;
+        else
+#pragma unroll
+            for (int d = 0; d < 7; ++d)
+                if (d < n) y[d] = (uint16_t)(v[d >> 1] >> (16 * (d & 1)));
     }
 }
 
@@ -606,15 +606,13 @@ using namespace embedding;
 size_t embedding_ws(int64_t rows, int32_t c) { return rows > 0 ? layout_of(rows, c).bytes : 0; }
 
 hipError_t launch_embedding_fwd(int dtype, const EmbeddingParams &p, hipStream_t st) {
-    const bool vec = p.c % 8 == 0 && ((uintptr_t)p.table & 15) == 0 && ((uintptr_t)p.y & 15) == 0;
-    const int64_t n = (p.rows * (vec ? p.c / 8 : p.c) + 255) / 256;
+    const int64_t n = (p.rows * ((p.c + 7) / 8) + 255) / 256;
     const dim3 grid((uint32_t)(n < (1 << 20) ? n : (1 << 20)));
-    if (dtype == Half::id) {
-        if (vec)
-            hipLaunchKernelGGL((fwd_kernel<Half, true>), grid, dim3(256), 0, st, p);
-        else
-            hipLaunchKernelGGL((fwd_kernel<Half, false>), grid, dim3(256), 0, st, p);
-    } else if (vec)
+    if (dtype == Half::id && p.c < 8)
+        hipLaunchKernelGGL((fwd_kernel<Half, true>), grid, dim3(256), 0, st, p);
+    else if (dtype == Half::id)
+        hipLaunchKernelGGL((fwd_kernel<Half, false>), grid, dim3(256), 0, st, p);
+    else if (p.c < 8)
         hipLaunchKernelGGL((fwd_kernel<BFloat, true>), grid, dim3(256), 0, st, p);
     else
         hipLaunchKernelGGL((fwd_kernel<BFloat, false>), grid, dim3(256), 0, st, p);
