@@ -576,7 +576,7 @@ nnconv_status nnconv_adamw_update(const nnconv_adamw_plan *plan, int32_t *step, 
 typedef struct {
     int64_t rows;   /* tokens, 0 to 2^27 */
     int32_t c;      /* channels, 1 to 2^24 */
-    int32_t v;      /* rows of the table, 1 to 2^29 */
+    int32_t v;      /* rows of the table, 1 to 2^29; v * c up to 2^35 */
     int32_t dtype;  /* F16 or BF16: table, y, dy */
     float scale;    /* finite: what a row is multiplied by */
 } nnconv_embedding_desc;
@@ -625,7 +625,7 @@ typedef struct {
     int32_t v;             /* vocabulary, 1 to 2^21 */
     int32_t dtype;         /* F16 or BF16: x, w, dx */
     int32_t k;             /* targets of a row, 1 to 1024; 1 with labels */
-    int32_t teacher_dtype; /* F32 or dtype (ignored without a teacher) */
+    int32_t teacher_dtype; /* F32 or dtype; F32 with labels */
     float logit_scale;     /* finite, not 0: 1 / temperature */
 } nnconv_xent_desc;
 

@@ -2254,7 +2254,8 @@ static nnconv_status embedding_check(const nnconv_embedding_desc *d) {
     if (!d || d->rows < 0 || d->c < 1 || d->v < 1 || !__builtin_isfinite(d->scale))
         return NNCONV_ERR_INVALID_ARG;
     if (d->rows > MAX_ELEMS / d->c || d->v > MAX_ELEMS / d->c) return NNCONV_ERR_INVALID_ARG;
-    if (d->c > MOST_ID_CHANNELS || d->v > MOST_TABLE_ROWS || d->rows > MOST_IDS)
+    if (d->c > MOST_ID_CHANNELS || d->v > MOST_TABLE_ROWS || d->rows > MOST_IDS ||
+        (int64_t)d->v * d->c > MOST_TABLE)
         return NNCONV_ERR_UNSUPPORTED;
     return half_dtype(d->dtype);
 }

@@ -176,7 +176,10 @@ __global__ __launch_bounds__(256) void rows_kernel(const Rows P) {
     base = wave_sum(base);
     if (lane == 0) part[wave] = base;
     __syncthreads();
-    if (tid == 0) P.base[r] = part[0] + part[1] + part[2] + part[3];
+    if (tid == 0) {
+        base = part[0] + part[1] + part[2] + part[3];
+        P.base[r] = base == base ? base : __builtin_nanf("");  // a teacher's NaN may have any bits
+    }
 }
 
 // The tiles' statistics of rows, and what becomes of them.

@@ -255,3 +255,68 @@ def test_pieces(nnlib):
                           (dw32 - 0.25, ref_dw, p.abs().t() @ x.double().abs() + 2.0 ** -12)):
         bound = (2.0 ** -11 + 2.0 ** -12 + 2.0 ** -15) * mag + 2.0 ** -11 * ref.abs() + 2.0 ** -23 + 2.0 ** 12 * 2.0 ** -28
         assert bool(((got.double() - ref).abs() <= bound).all())
+
+
+def test_a_teachers_nan(nnlib):
+    """A NaN among a teacher's logits, with any bits, is the row's and no other's."""
+    t = U.torch()
+    rng = np.random.default_rng(15)
+    x, w, targets, teacher = W.loss_inputs(rng, 20, 24, 100, "bf16", k=4)
+    X, Wt = (t.from_numpy(a).bfloat16().cuda() for a in (x, w))
+    T = t.from_numpy(targets.astype(np.int32)).cuda()
+    op = nc.CrossEntropy(20, 24, 100, dtype=nc.NNCONV_BF16, k=4)
+    got = []
+    for bits in (None, 0x7FC0DEAD, 0x7FC00000, 0x7F800001):
+        Q = t.from_numpy(teacher).float()
+        if bits is not None:
+            Q.view(t.int32)[6, 2] = bits
+        loss, dx = t.empty(20, device="cuda"), t.empty_like(X)
+        op.train(X, Wt, T, loss, dx, teacher=Q.cuda())
+        got.append((loss.cpu(), dx.cpu()))
+    rest = t.arange(20) != 6
+    for loss, dx in got[1:]:
+        assert bool(loss[6].isnan()) and bool(dx[6].isnan().all())
+        assert t.equal(loss[rest], got[0][0][rest]) and t.equal(dx[rest], got[0][1][rest])
+
+
+@pytest.mark.parametrize("train", [False, True])
+def test_many_short_rows(nnlib, train):
+    """More rows than one launch's tiles of a small vocabulary, and forward calls of several pieces."""
+    t = U.torch()
+    rows, c, v = 70001, 8, 70
+    g = t.Generator(device="cuda").manual_seed(1)
+    x, w = t.randn((rows, c), generator=g, device="cuda").half(), t.randn((v, c), generator=g, device="cuda").half()
+    target = t.randint(-1, v, (rows,), generator=g, device="cuda", dtype=t.int32)
+    op = nc.CrossEntropy(rows, c, v)
+    loss, dx, dw = t.empty(rows, device="cuda"), t.empty_like(x), t.empty(v, c, device="cuda")
+    if train:
+        op.train(x, w, target, loss, dx, dw)
+    else:
+        op.fwd(x, w, target, loss)
+    live = target >= 0
+    z = t.log_softmax(x.double() @ w.double().t(), 1)
+    want = -z.gather(1, target.clamp(min=0).long()[:, None])[:, 0] * live
+    assert float((loss - want).abs().max()) < 2.0 ** -18
+    if train:
+        dz = z.exp() * live[:, None]
+        dz[t.arange(rows, device="cuda"), target.clamp(min=0).long()] -= live.double()
+        # one rounding of dz, its storage before, one of the result
+        assert bool(((dx.double() - dz @ w.double()).abs() <= 2.0 ** -9.5 * (dz.abs() @ w.double().abs()) + 2.0 ** -20).all())
+        mag = dz.abs().t() @ x.double().abs()
+        assert bool(((dw.double() - dz.t() @ x.double()).abs() <= 2.0 ** -10 * mag).all())
+
+
+def test_forward_in_pieces(nnlib):
+    """A vocabulary whose statistics of all rows pass the workspace's share: pieces of 256 rows and more."""
+    t = U.torch()
+    rows, c, v = 9000, 8, 400000  # 1024 rows a piece
+    g = t.Generator(device="cuda").manual_seed(2)
+    x, w = t.randn((rows, c), generator=g, device="cuda").bfloat16(), t.randn((v, c), generator=g, device="cuda").bfloat16()
+    target = t.randint(0, v, (rows,), generator=g, device="cuda", dtype=t.int32)
+    op = nc.CrossEntropy(rows, c, v, dtype=nc.NNCONV_BF16)
+    loss, lse = t.empty(rows, device="cuda"), t.empty(rows, device="cuda")
+    op.fwd(x, w, target, loss, lse=lse)
+    for r in range(0, rows, 499):
+        z = x[r].double() @ w.double().t()
+        assert abs(float(lse[r] - t.logsumexp(z, 0))) < 2.0 ** -17
+        assert abs(float(loss[r] - t.logsumexp(z, 0) + z[target[r]])) < 2.0 ** -16
