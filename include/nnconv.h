@@ -574,7 +574,7 @@ nnconv_status nnconv_adamw_update(const nnconv_adamw_plan *plan, int32_t *step, 
  * null pointers for what has none. */
 
 typedef struct {
-    int64_t rows;   /* tokens, 0 to 2^27 */
+    int64_t rows;   /* tokens, 0 to 2^26 */
     int32_t c;      /* channels, 1 to 2^24 */
     int32_t v;      /* rows of the table, 1 to 2^29; v * c up to 2^35 */
     int32_t dtype;  /* F16 or BF16: table, y, dy */

@@ -454,14 +454,18 @@ __global__ __launch_bounds__(256) void sum_kernel(const Sums P) {
     }
 }
 
-// A workgroup a span: the row whose run begins in it and goes on behind it.
+// A workgroup a span: the row whose run begins in it and goes on behind it.  Its teams take a share
+// of the spans behind each (a token that pads a batch may be most of it), added up in order.
+constexpr int JOIN_THREADS = 1024;
+
 template <class T, bool WIDE, bool ACCUMULATE, bool SHORT>
-__global__ __launch_bounds__(256) void join_kernel(const Sums P) {
+__global__ __launch_bounds__(JOIN_THREADS) void join_kernel(const Sums P) {
     const int64_t s = blockIdx.x, last = s * P.span + P.span - 1;
     if (last + 1 >= P.rows) return;
     const uint32_t k = P.key[last];
     if (k >= (uint32_t)P.v || P.key[last + 1] != k) return;
     if (s > 0 && P.key[s * P.span] == k && P.key[s * P.span - 1] == k) return;  // begins before
+    __shared__ f32x4 sums[2][JOIN_THREADS];
     int64_t more = 0;  // spans behind this one that it reaches into
     for (;; more += 64) {
         const int64_t i = (s + 1 + more + (threadIdx.x & 63)) * P.span;
@@ -471,13 +475,21 @@ __global__ __launch_bounds__(256) void join_kernel(const Sums P) {
             break;
         }
     }
-    for (int c = ((int)blockIdx.y * 256 + threadIdx.x) * 8; c < P.c; c += (int)gridDim.y * 256 * 8) {
+    const int team = threadIdx.x / P.team, teams = JOIN_THREADS / P.team, at = threadIdx.x & (P.team - 1);
+    const int64_t share = (more + teams - 1) / teams, step = 2 * (int64_t)P.cp;
+    const int busy = (int)((more + share - 1) / share);
+    int64_t i = team * share;
+    const int64_t end = i + share < more ? i + share : more;
+    const int c = ((int)blockIdx.y * 256 + at) * 8;
+    f32x4 lo = {}, hi = {};
+    if (c < P.c) {
         const float *from = P.part + (2 * s + 1) * P.cp + c;
-        f32x4 lo = *(const f32x4 *)from, hi = *(const f32x4 *)(from + 4);
-        const float *next = P.part + 2 * (s + 1) * P.cp + c;
-        const int64_t step = 2 * (int64_t)P.cp;
-        int64_t i = 0;
-        for (; i + 8 <= more; i += 8, next += 8 * step) {
+        if (team == 0) {
+            lo = *(const f32x4 *)from;
+            hi = *(const f32x4 *)(from + 4);
+        }
+        const float *next = P.part + 2 * (s + 1 + i) * P.cp + c;
+        for (; i + 8 <= end; i += 8, next += 8 * step) {
             f32x4 a[8], b[8];
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
@@ -490,13 +502,23 @@ __global__ __launch_bounds__(256) void join_kernel(const Sums P) {
                 hi += b[u];
             }
         }
-        for (; i < more; ++i, next += step) {
+        for (; i < end; ++i, next += step) {
             lo += *(const f32x4 *)next;
             hi += *(const f32x4 *)(next + 4);
         }
-        const float sum[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        put8<T, WIDE>(P, k, c, sum, ACCUMULATE ? read8<WIDE, SHORT>(P, k, c) : Old{});
     }
+    if (busy > 1) {
+        sums[0][threadIdx.x] = lo;
+        sums[1][threadIdx.x] = hi;
+        __syncthreads();
+    }
+    if (team > 0 || c >= P.c) return;
+    for (int t = 1; t < busy; ++t) {
+        lo += sums[0][t * P.team + at];
+        hi += sums[1][t * P.team + at];
+    }
+    const float sum[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    put8<T, WIDE>(P, k, c, sum, ACCUMULATE ? read8<WIDE, SHORT>(P, k, c) : Old{});
 }
 
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
@@ -583,7 +605,7 @@ template <class T, bool WIDE, bool ACCUMULATE, bool SHORT>
 static void launch_sums(const Sums &s, dim3 grid, uint32_t spans, hipStream_t st) {
     hipLaunchKernelGGL((sum_kernel<T, WIDE, ACCUMULATE, SHORT>), grid, dim3(256), 0, st, s);
     if (spans > 1)
-        hipLaunchKernelGGL((join_kernel<T, WIDE, ACCUMULATE, SHORT>), dim3(spans, grid.y < 64 ? grid.y : 64), dim3(256), 0, st, s);
+        hipLaunchKernelGGL((join_kernel<T, WIDE, ACCUMULATE, SHORT>), dim3(spans, grid.y), dim3(JOIN_THREADS), 0, st, s);
 }
 
 template <class T, bool WIDE, bool ACCUMULATE>

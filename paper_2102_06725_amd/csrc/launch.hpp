@@ -502,8 +502,8 @@ hipError_t launch_adamw(const AdamwTable &tab, int64_t chunks, int32_t *step, fl
 // --- both ends of a model over a vocabulary ------------------------------------
 
 // Tokens of a lookup, its channels and rows of its table at most, so that launches stay within
-// 2^31 threads and 2^16 workgroups along their second axis.
-constexpr int64_t MOST_IDS = 1 << 27;
+// 2^32 threads and 2^16 workgroups along their second axis.
+constexpr int64_t MOST_IDS = 1 << 26;
 constexpr int32_t MOST_ID_CHANNELS = 1 << 24, MOST_TABLE_ROWS = 1 << 29;
 constexpr int64_t MOST_TABLE = (int64_t)1 << 35;  // elements
 

@@ -35,7 +35,7 @@ def test_embedding_descriptors(nnlib, kw):
     assert efwd(d) == ebwd(d) == nc.nnconv_embedding_workspace_size(d)[0] == INV
 
 
-@pytest.mark.parametrize("kw", [dict(dtype=nc.NNCONV_F32), dict(dtype=nc.NNCONV_F8), dict(rows=(1 << 27) + 1), dict(c=(1 << 24) + 1),
+@pytest.mark.parametrize("kw", [dict(dtype=nc.NNCONV_F32), dict(dtype=nc.NNCONV_F8), dict(rows=(1 << 26) + 1), dict(c=(1 << 24) + 1),
                                 dict(v=(1 << 29) + 1), dict(v=1 << 20, c=(1 << 15) + 8)])
 def test_embedding_limits(nnlib, kw):
     d = emb(**kw)
