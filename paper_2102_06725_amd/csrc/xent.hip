@@ -95,10 +95,11 @@ __device__ __forceinline__ float teacher_logit(const void *p, int64_t i) {
 }
 
 // A teacher: workgroups (row, share of its targets).  The logits of the targets in fp32 (their own
-// sums: the products' tiles have them in many places), a quarter wave each, 16 lanes of 8 channels,
-// four loads on their way; the first of a row makes its copy and the teacher's softmax.  Bound by
-// the gather of the targets' rows of w.
-template <class T, class S>
+// sums: the products' tiles have them in many places), LANES lanes each; the first of a row makes
+// its copy and the teacher's softmax.  Bound by the gather of the targets' rows of w (4096 x 32 of
+// 1152 channels: 302 MB in 58 us); few targets have a wave each, for the latency.  SHORT: fewer than 8
+// channels.
+template <class T, class S, int LANES, bool SHORT>
 __global__ __launch_bounds__(256) void rows_kernel(const Rows P) {
     if (copied_w(P)) return;
     const int64_t r = blockIdx.x;
@@ -120,33 +121,25 @@ __global__ __launch_bounds__(256) void rows_kernel(const Rows P) {
     any = __any(any);
     if (blockIdx.y == 0) {
         uint16_t *xc = P.xc + r * P.ldx;
-        for (int c = tid * 8; c < P.ldx; c += 2048) *(u32x4 *)(xc + c) = any ? row_vector(x, c, P.c) : u32x4{};
+        for (int c = tid * 8; c < P.ldx; c += 2048) *(u32x4 *)(xc + c) = any ? row_vector<SHORT>(x, c, P.c) : u32x4{};
     }
     if (!any) {
         if (blockIdx.y == 0 && tid == 0) P.base[r] = __builtin_bit_cast(float, NOT_COUNTED);
         return;  // nothing is read of the rest
     }
-    const int l16 = lane & 15;
-    for (int i = (int)blockIdx.y * 16 + (tid >> 4); i < k; i += 16 * (int)gridDim.y) {
+    constexpr int TEAMS = 256 / LANES;
+    const int at = tid & (LANES - 1);
+    for (int i = (int)blockIdx.y * TEAMS + tid / LANES; i < k; i += TEAMS * (int)gridDim.y) {
         const int32_t j = t[i];
         float dot = 0.f;
         if ((uint32_t)j < (uint32_t)P.v) {
             const uint16_t *w = P.w + (int64_t)j * P.c;
-            for (int c0 = l16 * 8; c0 < P.c; c0 += 512) {
-                u32x4 a[4], b[4];
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int c = c0 + u * 128;
-                    b[u] = c < P.c ? row_vector(w, c, P.c) : u32x4{};
-                    a[u] = c < P.c ? row_vector(x, c, P.c) : u32x4{};
-                }
-#pragma unroll
-                for (int u = 0; u < 4; ++u) dot = dot8<T>(a[u], b[u], dot);
-            }
+            for (int c = at * 8; c < P.c; c += LANES * 8)
+                dot = dot8<T>(row_vector<SHORT>(x, c, P.c), row_vector<SHORT>(w, c, P.c), dot);
         }
 #pragma unroll
-        for (int d = 8; d > 0; d >>= 1) dot += __shfl_xor(dot, d);
-        if (l16 == 0) P.zt[r * k + i] = dot * P.scale * LOG2E;
+        for (int d = LANES / 2; d > 0; d >>= 1) dot += __shfl_xor(dot, d);
+        if (at == 0) P.zt[r * k + i] = dot * P.scale * LOG2E;
     }
     if (blockIdx.y > 0) return;
     __shared__ float q[MOST_TARGETS];
@@ -401,6 +394,26 @@ static Plan plan_of(const XentParams &p, bool train) {
     return q;
 }
 
+template <class T, class S, int LANES>
+static void launch_teacher(const Rows &r, uint32_t blocks, hipStream_t st) {
+    // few rows: their targets are shared out
+    const int64_t most = (r.k + 256 / LANES - 1) / (256 / LANES), want = 1024 / r.rows;
+    const dim3 grid(blocks, (uint32_t)(want < 1 ? 1 : want < most ? want : most));
+    if (r.c < 8)
+        hipLaunchKernelGGL((rows_kernel<T, S, LANES, true>), grid, dim3(256), 0, st, r);
+    else
+        hipLaunchKernelGGL((rows_kernel<T, S, LANES, false>), grid, dim3(256), 0, st, r);
+}
+
+template <class T, class S>
+static void launch_teacher(const Rows &r, uint32_t blocks, hipStream_t st) {
+    // a wave a target while that fills the chip no more than twice
+    if (r.rows * r.k <= 2 * CUS * 32)
+        launch_teacher<T, S, 64>(r, blocks, st);
+    else
+        launch_teacher<T, S, 16>(r, blocks, st);
+}
+
 static void launch_rows(int dtype, int teacher_dtype, Rows r, hipStream_t st) {
     const int64_t vectors = r.wc ? (int64_t)r.v * (r.ldx / 8) : 0;
     const uint32_t more = (uint32_t)((vectors + COPY_VECTORS - 1) / COPY_VECTORS);
@@ -411,18 +424,15 @@ static void launch_rows(int dtype, int teacher_dtype, Rows r, hipStream_t st) {
         return;
     }
     r.first_w = (int32_t)r.rows;
-    // few rows: their targets are shared out
-    const int64_t most = (r.k + 15) / 16, want = 1024 / r.rows;
-    const dim3 grid((uint32_t)r.first_w + more, (uint32_t)(want < 1 ? 1 : want < most ? want : most));
     const bool wide = teacher_dtype == NNCONV_F32;
     if (dtype == Half::id && wide)
-        hipLaunchKernelGGL((rows_kernel<Half, float>), grid, dim3(256), 0, st, r);
+        launch_teacher<Half, float>(r, (uint32_t)r.first_w + more, st);
     else if (dtype == Half::id)
-        hipLaunchKernelGGL((rows_kernel<Half, uint16_t>), grid, dim3(256), 0, st, r);
+        launch_teacher<Half, uint16_t>(r, (uint32_t)r.first_w + more, st);
     else if (wide)
-        hipLaunchKernelGGL((rows_kernel<BFloat, float>), grid, dim3(256), 0, st, r);
+        launch_teacher<BFloat, float>(r, (uint32_t)r.first_w + more, st);
     else
-        hipLaunchKernelGGL((rows_kernel<BFloat, uint16_t>), grid, dim3(256), 0, st, r);
+        launch_teacher<BFloat, uint16_t>(r, (uint32_t)r.first_w + more, st);
 }
 
 }  // namespace xent
