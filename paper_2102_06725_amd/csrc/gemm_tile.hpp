@@ -9,6 +9,21 @@
 // The reduction goes through an LDS ring of STAGES slices of BK elements; a wave reads the
 // fragments of a 16-deep step while it multiplies those of the step before, and issues the loads
 // of a slice between matrix instructions.
+//
+// Tiles and rates, one product of 8192 x 2048 x 65536 bf16 in its three forms (both along the
+// reduction; one across it; both across it), normal values, on a card whose library does 1187, 1134
+// and 990 TFLOP/s of them (1270 to 1400 of an 8192^3 one):
+//   256 x 256, 4 waves, 32-element slices, 4 of them    -, 1131, 1116
+//   the same, 64-element slices, 2 of them              -, 1132, 1083
+//   8 waves of 128 x 64, 32-element slices, 4           -, 1198, 1144
+//   8 waves of 128 x 64, 64-element slices, 2           -, 1222, 1185     (taken)
+//   16 waves of 64 x 64, 64-element slices, 2           -, 1260, 1139     (spills registers)
+//   256 x 128, 4 waves, two workgroups a compute unit   -, 891, 1105
+//   128 x 128, 4 waves, 64-element slices, 2            -, 968, 984
+// (the first form ends in another way, see xent_logits.hip).  The matrix units are busy in 59 % of
+// the cycles at 1.94 GHz: the rest is waits at the slices' ends, and a faster tile lowers the clock.
+// 128 x 128 tiles run with 8 waves: on short reductions, which are bound by latency, a step of 777 x
+// 331 x 5003 takes 50 us with 8 and 52.5 with 4.  64 x 64 ones were not faster anywhere.
 #pragma once
 
 #include "launch.hpp"
