@@ -321,7 +321,11 @@ struct Shape {
 // rates are those of long products, 1200 and 960 TFLOP/s over all units.
 static Shape shape_of(int64_t m, int64_t n, int64_t k, bool split) {
     Shape best = {TILE_256, 1, (k + 63) / 64 * 64};
-    if (!split && m <= 32) return {TILE_32, 1, best.k_split};
+    // Logits that 128 x 128 tiles would keep no more than half the units busy with (300 x 512 of 4096
+    // channels: 22 us with 32 x 128 tiles, 31 with 128 x 128; 128 x 16384 of 2048: 28 and 30), and
+    // those of up to 32 rows; beyond, the smaller tiles lose (64 x 65536 of 2048: 54 and 49; 512 x 8192
+    // of 512: 21 and 12).
+    if (!split && (m <= 32 || (m + 127) / 128 * ((n + 127) / 128) <= CUS / 2)) return {TILE_32, 1, best.k_split};
     double least = 1e300;
     for (int c = TILE_256; c <= TILE_128; ++c) {
         const int64_t b = tile_rows((Config)c), slots = c == TILE_256 ? CUS : 2 * CUS;

@@ -71,7 +71,7 @@ struct Grad {
     int32_t tiles_m, tiles_n;
 };
 
-// Tiles of a product: 256 x 256, 128 x 128, and for the logits of a few rows 32 x 128.
+// Tiles of a product: 256 x 256, 128 x 128, and for few logits 32 x 128.
 enum Config { TILE_256 = 0, TILE_128 = 1, TILE_32 = 2 };
 inline int tile_rows(Config c) { return c == TILE_256 ? 256 : c == TILE_128 ? 128 : 32; }
 inline int tile_cols(Config c) { return c == TILE_256 ? 256 : 128; }

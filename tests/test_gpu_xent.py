@@ -205,9 +205,10 @@ def test_handle(nnlib, rows, c, v):
     assert t.allclose(loss.cpu(), ref["loss"].host(), rtol=1e-5, atol=1e-5)
 
 
-@pytest.mark.parametrize("rows,c,v,dtype,k", [(600, 520, 20000, "bf16", None), (2100, 1100, 8300, "f16", None), (1500, 300, 3000, "f16", 9)])
+@pytest.mark.parametrize("rows,c,v,dtype,k", [(600, 520, 20000, "bf16", None), (2100, 1100, 8300, "f16", None), (1500, 300, 3000, "f16", 9),
+                                              (1100, 64, 2001, "bf16", None), (1409, 77, 1500, "f16", None)])
 def test_large_tiles(nnlib, rows, c, v, dtype, k):
-    """Sizes whose products take 256 x 256 tiles, one and several a compute unit, and split reductions."""
+    """Sizes whose products take 256 x 256 and 128 x 128 tiles, one and several a compute unit, and split reductions."""
     rng = np.random.default_rng(rows)
     x, w, targets, teacher = W.loss_inputs(rng, rows, c, v, dtype, k=k, pad=0.1)
     got = W.loss_call(x, w, targets, teacher, dtype, 1.0)
