@@ -618,7 +618,8 @@ nnconv_status nnconv_embedding_bwd(const nnconv_embedding_desc *desc, const int3
  * of the student from it; entries whose target is padding or whose logit is
  * -inf are left out, and a target that is named twice counts with both shares.
  * A row without an entry does not count: its loss, lse and gradients are 0, and
- * its x is not read. */
+ * its x is not read.  Logits may be of any size whose products and their
+ * differences fp32 holds: a row's largest product is taken off before the scale. */
 typedef struct {
     int64_t rows;          /* 0 to 2^23 */
     int32_t c;             /* channels, 1 to 2^20; rows * c and v * c up to 2^35 */

@@ -26,8 +26,8 @@ struct Rows {
     uint16_t *xc;    // [rows][ldx]: x with zeros behind its channels and in rows that do not count
     uint16_t *wc;    // [v][ldx]: w with zeros behind its channels, or null
     int32_t first_w; // workgroups before those that copy w
-    // of a teacher's targets, [rows][k]: logits in units of log 2; shares; what is taken from their
-    // softmax
+    // of a teacher's targets, [rows][k]: products with x, turned where scale is negative; shares; what
+    // is taken from their softmax
     float *zt, *qi, *qt;
     float *base;     // [rows]: sum q log q; the bits NOT_COUNTED in rows that do not count
 };
@@ -139,7 +139,7 @@ __global__ __launch_bounds__(256) void rows_kernel(const Rows P) {
         }
 #pragma unroll
         for (int d = LANES / 2; d > 0; d >>= 1) dot += __shfl_xor(dot, d);
-        if (at == 0) P.zt[r * k + i] = dot * P.scale * LOG2E;
+        if (at == 0) P.zt[r * k + i] = P.scale < 0.f ? -dot : dot;
     }
     if (blockIdx.y > 0) return;
     __shared__ float q[MOST_TARGETS];
@@ -179,9 +179,10 @@ __global__ __launch_bounds__(256) void rows_kernel(const Rows P) {
 struct Join {
     int64_t rows;
     int32_t tiles, shift, v, k;  // shift: of a column to its tile
+    float scale, unit;          // |logit_scale|, and over log 2: what products count
     const float2 *stats;
     const int32_t *targets;     // [rows][k]
-    const float *zt;            // the targets' logits, in units of log 2
+    const float *zt;            // the targets' products
     const float *qi, *qt, *base;  // a teacher's shares and sums (see Rows); null with labels
     float *loss, *lse;          // lse may be null
     uint16_t *e;                // training: [rows][lde]
@@ -193,8 +194,8 @@ struct Join {
     int32_t c;
 };
 
-// The largest logit of a row, and the sum of the exponentials against it, by one wave.
-__device__ __forceinline__ void join_row(const float2 *s, int tiles, float &most, float &sum) {
+// The largest product of a row, and the sum of the exponentials against it, by one wave.
+__device__ __forceinline__ void join_row(const float2 *s, int tiles, float unit, float &most, float &sum) {
     const int lane = threadIdx.x & 63;
     most = -INFINITY;
     for (int i = lane; i < tiles; i += 64) most = fmaxf(most, s[i].x);
@@ -203,7 +204,7 @@ __device__ __forceinline__ void join_row(const float2 *s, int tiles, float &most
     sum = 0.f;
     for (int i = lane; i < tiles; i += 64) {
         const float2 v = s[i];
-        sum += v.y * exp2f(v.x == most ? 0.f : v.x - most);
+        sum += v.y * exp2f(v.x == most ? 0.f : (v.x - most) * unit);
     }
     sum = wave_sum(sum);
 }
@@ -212,23 +213,27 @@ __device__ __forceinline__ bool row_counts(const Join &P, int64_t r) {
     return P.base ? counted(P.base[r]) : (uint32_t)P.targets[r] < (uint32_t)P.v;
 }
 
+// How far a target's product lies below the largest, 0 at least: a teacher's targets have their own
+// sums, whose rounding may pass it.
+__device__ __forceinline__ float below(float most, float zt) { return zt > most ? 0.f : most - zt; }
+
 // By one wave.
 __device__ __forceinline__ void put_loss(const Join &P, int64_t r, bool counts, float most, float log_sum) {
     const int lane = threadIdx.x & 63;
     float loss = 0.f;
     if (P.base && counts) {
-        // sum q (log q + lse - z), the terms z - most first
+        // sum q (log q + lse - z), the terms most - z first
         float z = 0.f;
         for (int i = lane; i < P.k; i += 64) {
             const float q = P.qi[r * P.k + i];
-            if (q != 0.f) z += q * (most - P.zt[r * P.k + i]);
+            if (q != 0.f) z += q * below(most, P.zt[r * P.k + i]);
         }
-        loss = P.base[r] + (wave_sum(z) + log_sum) * LN2;
+        loss = P.base[r] + wave_sum(z) * P.scale + log_sum * LN2;
     } else if (counts)
-        loss = (most - P.zt[r] + log_sum) * LN2;  // near 0 both are small
+        loss = below(most, P.zt[r]) * P.scale + log_sum * LN2;  // near 0 both are small
     if (lane != 0) return;
     P.loss[r] = loss;
-    if (P.lse) P.lse[r] = counts ? (most + log_sum) * LN2 : 0.f;
+    if (P.lse) P.lse[r] = counts ? most * P.scale + log_sum * LN2 : 0.f;
 }
 
 // A wave a row.
@@ -236,7 +241,7 @@ __global__ __launch_bounds__(256) void join_kernel(const Join P) {
     const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (r >= P.rows) return;
     float most, sum;
-    join_row(P.stats + r * P.tiles, P.tiles, most, sum);
+    join_row(P.stats + r * P.tiles, P.tiles, P.unit, most, sum);
     const bool counts = row_counts(P, r);
     put_loss(P, r, counts, most, log2f(sum));
 }
@@ -264,7 +269,7 @@ __global__ __launch_bounds__(256) void scale_kernel(const Join P) {
     load(i);  // on their way meanwhile
     const bool counts = row_counts(P, r);
     float most, sum;
-    join_row(s, P.tiles, most, sum);
+    join_row(s, P.tiles, P.unit, most, sum);
     const float log_sum = log2f(sum), over = GRAD_UNIT / sum;
     if (part == 0 && threadIdx.x < 64) put_loss(P, r, counts, most, log_sum);
     if (P.xc && part == P.parts - 1)
@@ -276,7 +281,7 @@ __global__ __launch_bounds__(256) void scale_kernel(const Join P) {
         for (int u = 0; u < 4; ++u) {
             const int64_t n = i + u * 2048;
             const float m = n < n1 ? s[n >> P.shift].x : most;
-            f[u] = over * exp2f(m == most ? 0.f : m - most);
+            f[u] = over * exp2f(m == most ? 0.f : (m - most) * P.unit);
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
@@ -298,7 +303,7 @@ __global__ __launch_bounds__(256) void scale_kernel(const Join P) {
         const int32_t j = P.targets[r * P.k + i];
         if ((uint32_t)j >= (uint32_t)P.v || j < n0 || j >= n1) continue;
         const float q = P.qt ? P.qt[r * P.k + i] : 1.f;
-        e[j] = (uint16_t)to16<T>(GRAD_UNIT * (exp2f(P.zt[r * P.k + i] - most - log_sum) - q));
+        e[j] = (uint16_t)to16<T>(GRAD_UNIT * (exp2f(-below(most, P.zt[r * P.k + i]) * P.unit - log_sum) - q));
     }
 }
 
@@ -517,6 +522,8 @@ hipError_t launch_xent(const XentParams &p, bool train, hipStream_t st) {
         j.shift = tile == 256 ? 8 : 7;
         j.v = p.v;
         j.k = p.k;
+        j.scale = fabsf(p.logit_scale);
+        j.unit = fabsf(l.unit);
         j.stats = l.stats;
         j.targets = p.targets + r0 * p.k;
         j.zt = r.zt + r0 * p.k;

@@ -2,7 +2,7 @@
 // (xent_logits.hip, xent_grad.hip).
 //
 //   logits   z = scale * x w^T by tiles; of each tile's rows the largest z and the sum of
-//            exp(z - largest), and in training e = exp(z - largest) in fp16
+//            e = exp(z - largest), and in training e in 16 bits
 //   join     lse and loss of the tiles' statistics
 //   scale    the same, and e -> 2^15 (softmax(z) - q) in the operand type, in place
 //   grad     dx = d w, dw = d^T x
@@ -17,7 +17,8 @@ namespace xent {
 // 2^15: the gradient of a logit lies in [-1, 1]; in fp16 it keeps 11 bits down to 2^-29 then.
 constexpr float GRAD_UNIT = 32768.0f;
 
-// How the exponentials, which lie in [0, 1], are kept in 16 bits.  For bf16 operands fp16's 11 bits
+// How the exponentials, at most 1 since the largest product is taken off before the scale, are kept
+// in 16 bits.  For bf16 operands fp16's 11 bits
 // are three more than what they are rounded to later.  fp16 operands hold 11 themselves, and two
 // such roundings would add to the product's error: without a sign and with 4 exponent bits there
 // are 13, down to 2^-14 of the tile's largest, and an absolute error of 2^-28 of it below.
@@ -39,8 +40,9 @@ struct Logits {
     int32_t k;           // reduction elements
     float unit;          // logit_scale / log 2: what a product counts in units of log 2
     const int32_t *labels;  // [rows] or null
-    float *zt;           // [rows]: the labels' logits, in units of log 2
-    float2 *stats;       // [rows][tiles_n]: largest, in units of log 2, and sum
+    // products here and in the statistics are turned where logit_scale is negative
+    float *zt;           // [rows]: the labels' products
+    float2 *stats;       // [rows][tiles_n]: largest product, and sum of the exponentials
     uint16_t *e;         // [rows][lde] or null
     int64_t lde;         // a multiple of 64, >= v
     bool stream;         // e past the caches

@@ -3,12 +3,13 @@
 // A tile's logits stay in registers: of each row the largest (in the lane's 16 values of each
 // block, then its other half's, then the other waves' through LDS) and the sum of the exponentials
 // against it go to memory, and in training the exponentials themselves, at most 1, in 16 bits.
-// Logits are counted in units of log 2, as the exponential instruction takes them: the largest is
-// rounded to fp32 in these units, and each exponential's argument is one fused step from it, so
-// that the sums belong to the very number that is stored.  The label's logit is taken from the
-// same product, so that a loss near 0 is the difference of equal numbers.
+// The largest product is taken off before a product is scaled (to units of log 2, as the exponential
+// instruction takes them): the largest token's exponential is 1, whatever its logit (taken off after the
+// scaling, in one fused step, it would be 2 to the power of that logit's rounding, which passes any
+// format from 2^24 on).  Statistics are products, and the label's product is one of the same: a row
+// that is sure of its label has loss 0.
 //
-// What bounds it: the matrix units, and behind each tile about 9 vector instructions a logit, the
+// What bounds it: the matrix units, and behind each tile about 10 vector instructions a logit, the
 // exponential a half of their time, that no other tile of the compute unit covers (256 x 256 tiles
 // fill it): 8192 x 65536 logits of 2048 channels with their exponentials in 2.0 ms, 1.10 PFLOP/s, against
 // 1.68 for the product dx of the same size.  Smaller tiles, two a compute unit, cover it and lose
@@ -89,7 +90,7 @@ __global__ __launch_bounds__(WM * WN * 64, OCC) void logits_kernel(const Logits 
                     z = g.acc[j][i][u];
                 }
         // another padding than -1 may lie in the tile's empty columns
-        if (mine && label[i] < P.w.extent && m0 + r < P.x.extent) P.zt[m0 + r] = z * unit;
+        if (mine && label[i] < P.w.extent && m0 + r < P.x.extent) P.zt[m0 + r] = z;
     }
     barrier_lds();
 #pragma unroll
@@ -98,13 +99,13 @@ __global__ __launch_bounds__(WM * WN * 64, OCC) void logits_kernel(const Logits 
         float v = red[0][0][r];
 #pragma unroll
         for (int w = 1; w < WN; ++w) v = fmaxf(v, red[0][w][r]);
-        v = v == -INFINITY ? 0.f : v * unit;  // a row of infinitely low logits has sum 0
+        v = v == -INFINITY ? 0.f : v;  // a row of infinitely low logits has sum 0
         float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < FN; ++j)
 #pragma unroll
             for (int u = 0; u < 16; ++u) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(g.acc[j][i][u], unit, -v));
+                const float e = __builtin_amdgcn_exp2f((g.acc[j][i][u] - v) * unit);
                 g.acc[j][i][u] = e;
                 sum += e;
             }
@@ -120,7 +121,7 @@ __global__ __launch_bounds__(WM * WN * 64, OCC) void logits_kernel(const Logits 
             v = fmaxf(v, red[0][w][r]);
             s += red[1][w][r];
         }
-        P.stats[(m0 + r) * P.tiles_n + tn] = float2{v == -INFINITY ? v : v * unit, s};
+        P.stats[(m0 + r) * P.tiles_n + tn] = float2{v, s};
     }
     if constexpr (KEEP) {
         // through the wave's own part of LDS (behind the barriers above no wave reads operands there
