@@ -86,12 +86,18 @@ __device__ __forceinline__ float dot8(u32x4 a, u32x4 b, float s) {
     return s;
 }
 
+// A teacher's logit i, turned where the factor is negative, and whether the entry is left out, which
+// its own value says.  The factor comes behind the difference to the largest: before it, what is finite
+// may pass fp32.
 template <class T, class S>
-__device__ __forceinline__ float teacher_logit(const void *p, int64_t i) {
+__device__ __forceinline__ float teacher_logit(const Rows &P, int64_t i, bool &out) {
+    float a;
     if constexpr (sizeof(S) == 4)
-        return ((const float *)p)[i];
+        a = ((const float *)P.teacher)[i];
     else
-        return from16<T>(((const uint16_t *)p)[i]);
+        a = from16<T>(((const uint16_t *)P.teacher)[i]);
+    out = (uint32_t)P.targets[i] >= (uint32_t)P.v || a == -INFINITY;
+    return P.scale < 0.f ? -a : a;
 }
 
 // A teacher: workgroups (row, share of its targets).  The logits of the targets in fp32 (their own
@@ -111,8 +117,9 @@ __global__ __launch_bounds__(256) void rows_kernel(const Rows P) {
     float most = -INFINITY;
     bool any = false;
     for (int i = lane; i < k; i += 64) {
-        const float a = teacher_logit<T, S>(P.teacher, r * k + i) * P.scale;
-        if ((uint32_t)t[i] >= (uint32_t)P.v || a == -INFINITY) continue;
+        bool out;
+        const float a = teacher_logit<T, S>(P, r * k + i, out);
+        if (out) continue;
         any = true;
         most = fmaxf(most, a);
     }
@@ -144,10 +151,12 @@ __global__ __launch_bounds__(256) void rows_kernel(const Rows P) {
     if (blockIdx.y > 0) return;
     __shared__ float q[MOST_TARGETS];
     __shared__ float part[4];
+    const float scale = fabsf(P.scale);
     float sum = 0.f;
     for (int i = tid; i < k; i += 256) {
-        const float a = teacher_logit<T, S>(P.teacher, r * k + i) * P.scale;
-        const float e = (uint32_t)t[i] >= (uint32_t)P.v || a == -INFINITY ? 0.f : expf(a - most);
+        bool out;
+        const float a = teacher_logit<T, S>(P, r * k + i, out);
+        const float e = out ? 0.f : expf((a - most) * scale);
         q[i] = e;
         sum += e;
     }
@@ -163,7 +172,8 @@ __global__ __launch_bounds__(256) void rows_kernel(const Rows P) {
         for (int j = 0; j < k; ++j) taken += t[j] == t[i] ? q[j] : 0.f;
         P.qi[r * k + i] = e / sum;
         P.qt[r * k + i] = taken / sum;
-        if (e != 0.f) base += e / sum * (teacher_logit<T, S>(P.teacher, r * k + i) * P.scale - most - log_sum);
+        bool out;
+        if (e != 0.f) base += e / sum * ((teacher_logit<T, S>(P, r * k + i, out) - most) * scale - log_sum);
     }
     __syncthreads();
     base = wave_sum(base);
