@@ -655,8 +655,11 @@ nnconv_status nnconv_xent_fwd(const nnconv_xent_desc *desc, const void *x, const
  *   dx[r] = G * logit_scale * sum over j of dz[r][j] * w[j],   G = alpha * (*grad_scale)
  *   dw[j] = (accumulate ? dw[j] : 0)
  *           + inv_loss_scale * G * logit_scale * sum over r of dz[r][j] * x[r]
- * dz is rounded once to the operands' type, as an operand of both products
- * (2^15 dz, so that fp16 keeps its 11 bits down to a dz of 2^-29).  dx:
+ * dz is an operand of both products and rounded to the operands' type for them
+ * (2^15 dz, so that fp16 keeps its 11 bits down to a dz of 2^-29).  Where the
+ * token is no target it comes from an exponential that is kept in 12 bits (F16)
+ * or 11 (BF16); below 2^-30 (2^-62) of the row's largest among the 256 tokens
+ * around it, in steps of 2^-41 (2^-72) of that one.  dx:
  * [rows][c], it may be x itself; dw: [v][c] of dw_dtype, F32 or desc->dtype,
  * or NULL: then it is left out.  overflow_flag is set where an element of dx
  * or dw is inf or NaN.  16-byte aligned dx and dw with c a multiple of 8 are the

@@ -18,21 +18,29 @@ namespace xent {
 constexpr float GRAD_UNIT = 32768.0f;
 
 // How the exponentials, at most 1 since the largest product is taken off before the scale, are kept
-// in 16 bits.  For bf16 operands fp16's 11 bits
-// are three more than what they are rounded to later.  fp16 operands hold 11 themselves, and two
-// such roundings would add to the product's error: without a sign and with 4 exponent bits there
-// are 13, down to 2^-14 of the tile's largest, and an absolute error of 2^-28 of it below.
+// in 16 bits: without a sign and with the bits that they need.  What they are rounded to later has 11
+// bits down to 2^-29 (fp16 in units of 2^-15): 5 bits of exponent and 12 of a number go to 2^-30 of the
+// tile's largest, and on in steps of 2^-41.  bf16 has 8 bits and no such end: 6 bits of exponent, 11 of a
+// number, down to 2^-62.  With fewer bits of exponent, rare tokens beside a likely one had gradients
+// of 0.
+template <class T>
+struct Kept {
+    static constexpr int EXPONENT = T::id == BFloat::id ? 6 : 5;
+    static constexpr int SHIFT = 7 + EXPONENT;  // of an fp32 number's bits behind the exponent's are cut
+    // 2^(127 - the exponent of 1), which has all bits
+    static constexpr float UNIT = T::id == BFloat::id ? 0x1p64f : 0x1p96f;
+};
 template <class T>
 __device__ __forceinline__ uint32_t pack_exp(float lo, float hi) {
-    if constexpr (T::id == BFloat::id) return pack16<Half>(lo, hi);
-    const uint32_t a = __builtin_bit_cast(uint32_t, lo * 0x1p-112f) + 0x400u;  // 1 has exponent 15
-    const uint32_t b = __builtin_bit_cast(uint32_t, hi * 0x1p-112f) + 0x400u;
-    return ((a >> 11) & 0xFFFFu) | ((b >> 11) << 16);
+    typedef Kept<T> K;
+    const uint32_t a = (__builtin_bit_cast(uint32_t, lo * (1.0f / K::UNIT)) + (1u << (K::SHIFT - 1))) << (16 - K::SHIFT);
+    const uint32_t b = (__builtin_bit_cast(uint32_t, hi * (1.0f / K::UNIT)) + (1u << (K::SHIFT - 1))) << (16 - K::SHIFT);
+    return __builtin_amdgcn_perm(b, a, 0x07060302);  // the upper halves
 }
 template <class T>
 __device__ __forceinline__ float unpack_exp(uint32_t bits) {
-    if constexpr (T::id == BFloat::id) return from16<Half>(bits);
-    return __builtin_bit_cast(float, (bits & 0xFFFFu) << 11) * 0x1p112f;
+    typedef Kept<T> K;
+    return __builtin_bit_cast(float, (bits & 0xFFFFu) << K::SHIFT) * K::UNIT;
 }
 
 struct Logits {
