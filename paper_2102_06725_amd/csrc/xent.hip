@@ -32,10 +32,6 @@ struct Rows {
     float *base;     // [rows]: sum q log q; the bits NOT_COUNTED in rows that do not count
 };
 
-// What stands for a row that does not count.  Arithmetic makes no NaN with these bits.
-constexpr uint32_t NOT_COUNTED = 0x7FC0DEADu;
-__device__ __forceinline__ bool counted(float v) { return __builtin_bit_cast(uint32_t, v) != NOT_COUNTED; }
-
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
@@ -219,9 +215,7 @@ __device__ __forceinline__ void join_row(const float2 *s, int tiles, float unit,
     sum = wave_sum(sum);
 }
 
-__device__ __forceinline__ bool row_counts(const Join &P, int64_t r) {
-    return P.base ? counted(P.base[r]) : (uint32_t)P.targets[r] < (uint32_t)P.v;
-}
+__device__ __forceinline__ bool row_counts(const Join &P, int64_t r) { return Counts{P.targets, P.base, P.v}.of(r); }
 
 // How far a target's product lies below the largest, 0 at least: a teacher's targets have their own
 // sums, whose rounding may pass it.
@@ -477,7 +471,7 @@ hipError_t launch_xent(const XentParams &p, bool train, hipStream_t st) {
         Grad g = {};
         g.splits = 1;
         g.k_split = 64;
-        g.o = {p.dw, p.dw_dtype, p.c, p.v, 1.0f, nullptr, 0, nullptr, nullptr, nullptr};
+        g.o = {p.dw, p.dw_dtype, p.c, p.v, 1.0f, nullptr, 0, nullptr, nullptr, nullptr, false, {}};
         return launch_grad_w(p.dtype, TILE_128, g, st);
     }
     const Plan q = plan_of(p, train);
@@ -567,7 +561,8 @@ hipError_t launch_xent(const XentParams &p, bool train, hipStream_t st) {
         g.k_split = q.dx.k_split;
         g.splits = q.dx.splits;
         g.part = at(q.part);
-        g.o = {(uint16_t *)p.dx + r0 * p.c, p.dtype, p.c, n, alpha, p.grad_scale, 0, p.flag, nullptr, nullptr};
+        g.o = {(uint16_t *)p.dx + r0 * p.c, p.dtype, p.c, n, alpha, p.grad_scale, 0, p.flag, nullptr, nullptr, true,
+               {j.targets, j.base, p.v}};
         d.a = {l.e, q.lde, (int32_t)q.lde};
         d.b = {q.late_x ? j.xc : l.x.p, q.ldx, (int32_t)q.ldx};
         d.k = n;
@@ -575,7 +570,7 @@ hipError_t launch_xent(const XentParams &p, bool train, hipStream_t st) {
         d.splits = q.dw.splits;
         d.part = at(q.part_w);
         d.o = {p.dw, p.dw_dtype, p.c, p.v, alpha * p.inv_loss_scale, p.grad_scale, p.accumulate, p.flag,
-               r0 > 0 ? at(q.acc) : nullptr, r0 + n < p.rows ? at(q.acc) : nullptr};
+               r0 > 0 ? at(q.acc) : nullptr, r0 + n < p.rows ? at(q.acc) : nullptr, false, {}};
         e = launch_grads(p.dtype, q.dx.cfg, g, q.dw.cfg, p.dw ? &d : nullptr, st);
         if (e != hipSuccess) return e;
     }

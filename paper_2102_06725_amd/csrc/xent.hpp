@@ -57,6 +57,18 @@ struct Logits {
     int32_t tiles_m, tiles_n;
 };
 
+// What stands for a row that does not count.  Arithmetic makes no NaN with these bits.
+constexpr uint32_t NOT_COUNTED = 0x7FC0DEADu;
+__device__ __forceinline__ bool counted(float v) { return __builtin_bit_cast(uint32_t, v) != NOT_COUNTED; }
+
+// Which rows count: those whose label is a token, or with a teacher whose sum (see Rows in xent.hip) says so.
+struct Counts {
+    const int32_t *labels;
+    const float *base;
+    int32_t v;
+    __device__ __forceinline__ bool of(int64_t r) const { return base ? counted(base[r]) : (uint32_t)labels[r] < (uint32_t)v; }
+};
+
 // Where a gradient product goes: out = (accumulate ? out : 0) + alpha * *scale * (acc + prev).
 struct GradOut {
     void *out;
@@ -69,6 +81,9 @@ struct GradOut {
     int32_t *flag;       // set where a value is not finite, or null
     const float *prev;   // fp32 [m][n] sums of earlier pieces, or null
     float *keep;         // fp32 [m][n]: acc + prev goes here and nowhere else, or null
+    // rows of dx that do not count are 0, where an infinity in w or a factor makes them NaN; looked at only there
+    bool by_rows;
+    Counts counts;
 };
 
 struct Grad {

@@ -37,6 +37,7 @@ __device__ __forceinline__ void put4(const GradOut &o, float factor, int64_t m, 
         return;
     }
     v *= factor;
+    if (o.by_rows && !__builtin_isfinite(v[0] + v[1] + v[2] + v[3]) && !o.counts.of(m)) v = f32x4{};
     bool bad = false;
     if (o.kind == 2) {
         float *to = (float *)o.out + i;
@@ -118,7 +119,7 @@ __device__ __forceinline__ void grad_tile(const Grad &P, uint32_t block, char *l
         constexpr int ROWB = G::WTN * 4, CPR = G::WTN / 4;
         char *own = lds + wave * (32 * ROWB);
         float *part = P.splits > 1 ? P.part + (int64_t)split * o.m * o.n : nullptr;
-        const GradOut raw = {nullptr, 2, o.n, o.m, 1.f, nullptr, 0, nullptr, nullptr, part};
+        const GradOut raw = {nullptr, 2, o.n, o.m, 1.f, nullptr, 0, nullptr, nullptr, part, false, {}};
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
 #pragma unroll
@@ -164,11 +165,17 @@ __device__ __forceinline__ void grad_tile(const Grad &P, uint32_t block, char *l
 #pragma unroll 4
     for (int r = lane / CPR; r < G::WTM; r += 64 / CPR) {
         const int64_t m = m0 + wm * G::WTM + r;
-        const u32x4 v = *(const u32x4 *)(own + r * ROWB + (c ^ (r & (CPR - 1))) * 16);
+        u32x4 v = *(const u32x4 *)(own + r * ROWB + (c ^ (r & (CPR - 1))) * 16);
         if (m >= o.m || n >= o.n) continue;
+        bool here = false;
 #pragma unroll
         for (int d = 0; d < 4; ++d)
-            bad |= (v[d] & TOP) == TOP || ((v[d] >> 16) & TOP) == TOP;
+            here |= (v[d] & TOP) == TOP || ((v[d] >> 16) & TOP) == TOP;
+        if (here && o.by_rows && !o.counts.of(m)) {
+            v = u32x4{};
+            here = false;
+        }
+        bad |= here;
         __builtin_nontemporal_store(v, (u32x4 *)((uint16_t *)o.out + m * o.n + n));
     }
     if (o.flag && bad) *o.flag = 1;
