@@ -26,6 +26,7 @@ struct Rows {
     uint16_t *xc;    // [rows][ldx]: x with zeros behind its channels and in rows that do not count
     uint16_t *wc;    // [v][ldx]: w with zeros behind its channels, or null
     int32_t first_w; // workgroups before those that copy w
+    int32_t shares;  // workgroups of a row's targets
     // of a teacher's targets, [rows][k]: products with x, turned where scale is negative; shares; what
     // is taken from their softmax
     float *zt, *qi, *qt;
@@ -42,7 +43,6 @@ __device__ __forceinline__ float wave_sum(float v) {
 constexpr int COPY_VECTORS = 1024;
 __device__ __forceinline__ bool copied_w(const Rows &P) {
     if (blockIdx.x < (uint32_t)P.first_w) return false;
-    if (blockIdx.y > 0) return true;
     const uint32_t per = (uint32_t)P.ldx / 8;
     const int64_t first = (int64_t)(blockIdx.x - P.first_w) * COPY_VECTORS, count = (int64_t)P.v * per;
     u32x4 v[4];
@@ -96,7 +96,7 @@ __device__ __forceinline__ float teacher_logit(const Rows &P, int64_t i, bool &o
     return P.scale < 0.f ? -a : a;
 }
 
-// A teacher: workgroups (row, share of its targets).  The logits of the targets in fp32 (their own
+// A teacher: workgroups of a row and a share of its targets.  The logits of the targets in fp32 (their own
 // sums: the products' tiles have them in many places), LANES lanes each; the first of a row makes
 // its copy and the teacher's softmax.  Bound by the gather of the targets' rows of w (4096 x 32 of
 // 1152 channels: 302 MB in 58 us); few targets have a wave each, for the latency.  SHORT: fewer than 8
@@ -104,7 +104,9 @@ __device__ __forceinline__ float teacher_logit(const Rows &P, int64_t i, bool &o
 template <class T, class S, int LANES, bool SHORT>
 __global__ __launch_bounds__(256) void rows_kernel(const Rows P) {
     if (copied_w(P)) return;
-    const int64_t r = blockIdx.x;
+    // the rows' first shares, which have more to do, come first, on units of their own
+    const int share = (int)(blockIdx.x / (uint32_t)P.rows);
+    const int64_t r = blockIdx.x - (uint32_t)share * (uint32_t)P.rows;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int k = P.k;
     const int32_t *t = P.targets + r * k;
@@ -122,17 +124,17 @@ __global__ __launch_bounds__(256) void rows_kernel(const Rows P) {
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
     any = __any(any);
-    if (blockIdx.y == 0) {
+    if (share == 0) {
         uint16_t *xc = P.xc + r * P.ldx;
         for (int c = tid * 8; c < P.ldx; c += 2048) *(u32x4 *)(xc + c) = any ? row_vector<SHORT>(x, c, P.c) : u32x4{};
     }
     if (!any) {
-        if (blockIdx.y == 0 && tid == 0) P.base[r] = __builtin_bit_cast(float, NOT_COUNTED);
+        if (share == 0 && tid == 0) P.base[r] = __builtin_bit_cast(float, NOT_COUNTED);
         return;  // nothing is read of the rest
     }
     constexpr int TEAMS = 256 / LANES;
     const int at = tid & (LANES - 1);
-    for (int i = (int)blockIdx.y * TEAMS + tid / LANES; i < k; i += TEAMS * (int)gridDim.y) {
+    for (int i = share * TEAMS + tid / LANES; i < k; i += TEAMS * P.shares) {
         const int32_t j = t[i];
         float dot = 0.f;
         if ((uint32_t)j < (uint32_t)P.v) {
@@ -144,7 +146,7 @@ __global__ __launch_bounds__(256) void rows_kernel(const Rows P) {
         for (int d = LANES / 2; d > 0; d >>= 1) dot += __shfl_xor(dot, d);
         if (at == 0) P.zt[r * k + i] = P.scale < 0.f ? -dot : dot;
     }
-    if (blockIdx.y > 0) return;
+    if (share > 0) return;
     __shared__ float q[MOST_TARGETS];
     __shared__ float part[4];
     const float scale = fabsf(P.scale);
@@ -408,10 +410,12 @@ static Plan plan_of(const XentParams &p, bool train) {
 }
 
 template <class T, class S, int LANES>
-static void launch_teacher(const Rows &r, uint32_t blocks, hipStream_t st) {
+static void launch_teacher(Rows r, uint32_t more, hipStream_t st) {
     // few rows: their targets are shared out
     const int64_t most = (r.k + 256 / LANES - 1) / (256 / LANES), want = 1024 / r.rows;
-    const dim3 grid(blocks, (uint32_t)(want < 1 ? 1 : want < most ? want : most));
+    r.shares = (int32_t)(want < 1 ? 1 : want < most ? want : most);
+    r.first_w = (int32_t)r.rows * r.shares;
+    const dim3 grid((uint32_t)r.first_w + more);
     if (r.c < 8)
         hipLaunchKernelGGL((rows_kernel<T, S, LANES, true>), grid, dim3(256), 0, st, r);
     else
@@ -419,12 +423,12 @@ static void launch_teacher(const Rows &r, uint32_t blocks, hipStream_t st) {
 }
 
 template <class T, class S>
-static void launch_teacher(const Rows &r, uint32_t blocks, hipStream_t st) {
+static void launch_teacher(const Rows &r, uint32_t more, hipStream_t st) {
     // a wave a target while that fills the chip no more than twice
     if (r.rows * r.k <= 2 * CUS * 32)
-        launch_teacher<T, S, 64>(r, blocks, st);
+        launch_teacher<T, S, 64>(r, more, st);
     else
-        launch_teacher<T, S, 16>(r, blocks, st);
+        launch_teacher<T, S, 16>(r, more, st);
 }
 
 static void launch_rows(int dtype, int teacher_dtype, Rows r, hipStream_t st) {
@@ -436,16 +440,15 @@ static void launch_rows(int dtype, int teacher_dtype, Rows r, hipStream_t st) {
         hipLaunchKernelGGL(copy_kernel, dim3((uint32_t)r.first_w + more), dim3(256), 0, st, r);
         return;
     }
-    r.first_w = (int32_t)r.rows;
     const bool wide = teacher_dtype == NNCONV_F32;
     if (dtype == Half::id && wide)
-        launch_teacher<Half, float>(r, (uint32_t)r.first_w + more, st);
+        launch_teacher<Half, float>(r, more, st);
     else if (dtype == Half::id)
-        launch_teacher<Half, uint16_t>(r, (uint32_t)r.first_w + more, st);
+        launch_teacher<Half, uint16_t>(r, more, st);
     else if (wide)
-        launch_teacher<BFloat, float>(r, (uint32_t)r.first_w + more, st);
+        launch_teacher<BFloat, float>(r, more, st);
     else
-        launch_teacher<BFloat, uint16_t>(r, (uint32_t)r.first_w + more, st);
+        launch_teacher<BFloat, uint16_t>(r, more, st);
 }
 
 }  // namespace xent
