@@ -509,7 +509,10 @@ class _Workspaces:
     and each call that torch captures into a graph has one of the graph's memory, so that graphs
     of a handle may be replayed beside each other and beside its calls.  A workspace that became
     too small is kept until the handle goes: a graph that the caller captured by other means may
-    hold its address."""
+    hold its address.  From LARGE bytes on it is replaced, and kept only if such a graph was seen
+    to take it."""
+
+    LARGE = 64 << 20  # beside the calls that need it the look at the stream is nothing
 
     def __init__(self):
         import torch
@@ -522,11 +525,25 @@ class _Workspaces:
             return self._new(nbytes, stream, device)
         t = self._held.get((kind, stream, device))
         if t is None or t.numel() < nbytes:
-            if t is not None:  # doubled, so that all that is kept is no more than what is in use
+            if t is not None and t.numel() < self.LARGE:  # doubled, so that all that is kept is no more than what is in use
                 self._kept.append(t)
                 nbytes = max(nbytes, 2 * t.numel())
+            elif t is not None:
+                nbytes = max(nbytes, t.numel() * 9 // 8)  # not a new one for each batch that is a little larger
+                self._held.pop((kind, stream, device), None)
+                t = None  # its memory may be what the new one takes: both are used in the stream's order
             t = self._held[kind, stream, device] = self._new(nbytes, stream, device)
+        if t.numel() >= self.LARGE and device.type == "cuda" and self._captured(stream, device) and not any(k is t for k in self._kept):
+            self._kept.append(t)
         return t
+
+    def _captured(self, stream, device):
+        """Whether a graph is being captured on a stream that is not the current one."""
+        import torch
+        if not stream or stream == current_stream():
+            return False
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream, device)):
+            return self._capturing()
 
     @staticmethod
     def _new(nbytes, stream, device):
@@ -946,7 +963,8 @@ class CrossEntropy(_Handle):
     nnconv_xent_*.  With labels each row has one target; with `k` each row has k targets and a
     teacher's logits for them, fp32 or of x's type (teacher_dtype).  `rows` may be changed between
     calls.  Tensors are dense and on the current device, targets int32; others are refused with a
-    ValueError."""
+    ValueError.  The workspace of training, 1 GiB and more where there are many logits, is held for
+    each stream, and each captured graph has one of its own."""
 
     def __init__(self, rows, c, v, dtype=NNCONV_F16, logit_scale=1.0, k=None, teacher_dtype=NNCONV_F32):
         import torch

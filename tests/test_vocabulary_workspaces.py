@@ -1,0 +1,121 @@
+"""Large workspaces: a handle holds one a stream and pass, no more than a call needs and an eighth; a graph that was captured by
+other means than torch's keeps the memory that it was given."""
+import ctypes
+import weakref
+
+import numpy as np
+import pytest
+
+from paper_2102_06725_amd import nnconv as nc
+
+import sequence_util as U
+import vocabulary_util as W
+
+GIB = 1 << 30
+
+
+def test_large_ones_are_replaced():
+    """Tensors without memory stand for them."""
+    t = U.torch()
+    w, meta = nc._Workspaces(), t.device("meta")
+    seen = []
+    for step in range(40):
+        need = GIB + step * (GIB >> 4)
+        ws = w.get("train", 0, need, meta)
+        assert need <= ws.numel() <= need * 9 // 8
+        if not seen or seen[-1]() is not ws:
+            seen.append(weakref.ref(ws))
+        del ws
+        assert sum(r().numel() for r in seen if r() is not None) <= need * 9 // 8
+    assert len(seen) < 20  # not one for each size
+    # no call of a size that was there before takes new memory
+    last = seen[-1]()
+    assert all(w.get("train", 0, n, meta) is last for n in (1, 100, GIB, 2 * GIB))
+
+
+def test_growth_from_small_ones():
+    t = U.torch()
+    w, meta = nc._Workspaces(), t.device("meta")
+    held, n = [], 1
+    while n < 8 * GIB:
+        ws = w.get("train", 0, n, meta)
+        if not held or held[-1]() is not ws:
+            held.append(weakref.ref(ws))
+        assert ws.numel() <= max(2 * n, n * 9 // 8)
+        n = n * 5 // 4 + 1
+    assert sum(r().numel() for r in held if r() is not None) <= n * 9 // 8 + 4 * nc._Workspaces.LARGE
+
+
+class Graph:
+    """Calls on a stream captured with the runtime's own functions."""
+
+    def __init__(self, stream):
+        self.hip, self.stream = ctypes.CDLL("libamdhip64.so"), ctypes.c_void_p(stream.cuda_stream)
+        self.graph, self.exec = ctypes.c_void_p(), ctypes.c_void_p()
+
+    def __enter__(self):
+        assert self.hip.hipStreamBeginCapture(self.stream, 2) == 0  # hipStreamCaptureModeRelaxed
+
+    def __exit__(self, *_):
+        assert self.hip.hipStreamEndCapture(self.stream, ctypes.byref(self.graph)) == 0
+        assert self.hip.hipGraphInstantiate(ctypes.byref(self.exec), self.graph, None, None, 0) == 0
+
+    def launch(self):
+        assert self.hip.hipGraphLaunch(self.exec, self.stream) == 0
+
+
+@pytest.mark.gpu
+def test_a_graph_of_other_means(nnlib):
+    """Captured on a stream that is not the current one, then the handle grows: what the graph was given is nobody else's."""
+    t = U.torch()
+    v, c = 16000, 64
+    rng = np.random.default_rng(3)
+    rows = 3000
+    x, w, targets, _ = W.loss_inputs(rng, 2 * rows, c, v, "f16")
+    X, Wt, T = (t.from_numpy(a).cuda() for a in (x, w, targets[:, 0]))
+    X, Wt, T = X.half(), Wt.half(), T.to(t.int32)
+    op, side = nc.CrossEntropy(rows, c, v), t.cuda.Stream()
+    loss, dx, dw = t.empty(2 * rows, device="cuda"), t.empty_like(X), t.empty(v, c, device="cuda")
+
+    def run(n):
+        op.rows = n
+        op.train(X[:n], Wt, T[:n], loss[:n], dx[:n], dw, stream=side.cuda_stream)
+
+    run(rows)
+    t.cuda.synchronize()
+    want = [a.clone() for a in (loss[:rows], dx[:rows], dw)]
+    g = Graph(side)
+    with g:
+        run(rows)
+    for _ in range(3):
+        run(2 * rows)
+        t.cuda.synchronize()
+        with t.cuda.stream(side):
+            held = [t.full((n << 20,), 0x5A, dtype=t.uint8, device="cuda") for n in (80, 100, 120, 200, 20, 20)]
+        for a in (loss, dx, dw):
+            a.zero_()
+        t.cuda.synchronize()
+        g.launch()
+        t.cuda.synchronize()
+        assert all(t.equal(a, b) for a, b in zip((loss[:rows], dx[:rows], dw), want))
+        assert all(bool((h == 0x5A).all()) for h in held)
+
+
+@pytest.mark.gpu
+def test_what_a_growing_handle_holds(nnlib):
+    """Batches that grow past the limit of a piece: the memory in use is a call's own."""
+    t = U.torch()
+    v, c = 131072, 8
+    w, x = t.zeros((v, c), dtype=t.half, device="cuda"), t.zeros((12288, c), dtype=t.half, device="cuda")
+    targets, loss, dx = t.zeros(12288, dtype=t.int32, device="cuda"), t.empty(12288, device="cuda"), t.empty_like(x)
+    op = nc.CrossEntropy(1, c, v)
+    t.cuda.synchronize()
+    before = t.cuda.memory_allocated()
+    for n in (1000, 3000, 4000, 4096, 5000, 12288):
+        op.rows = n
+        op.train(x[:n], w, targets[:n], loss[:n], dx[:n])
+        need = nc.nnconv_xent_workspace_size(op.desc, nc.NNCONV_DGRAD)[1]
+        assert t.cuda.memory_allocated() - before <= need * 9 // 8 + (4 << 20)
+    t.cuda.synchronize()
+    # all tokens alike: each loss is log v
+    assert float((loss - np.log(v)).abs().max()) < 1e-4
