@@ -29,7 +29,10 @@ class TokenModel(GatedBlocks):
         rows = n * t
         self.embed = nc.Embedding(rows, c, v, dtype=dtype, scale=math.sqrt(c))
         self.loss = nc.CrossEntropy(rows, c, v, dtype=dtype)
-        self.distillation = None if k is None else nc.CrossEntropy(rows, c, v, dtype=dtype, k=k)
+        self.distillation = None
+        if k is not None:
+            self.distillation = nc.CrossEntropy(rows, c, v, dtype=dtype, k=k)
+            self.distillation._ws = self.loss._ws  # a step is of one kind or the other
         self.losses = torch.empty((n, t), dtype=torch.float32, device=device)
 
     def forward(self, ids):

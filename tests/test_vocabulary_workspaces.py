@@ -119,3 +119,40 @@ def test_what_a_growing_handle_holds(nnlib):
     t.cuda.synchronize()
     # all tokens alike: each loss is log v
     assert float((loss - np.log(v)).abs().max()) < 1e-4
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("v", [30000, 120000])
+def test_a_models_two_losses(nnlib, v):
+    """Steps against labels and against a teacher use the same memory, and give what a model of one kind alone gives."""
+    from paper_2102_06725_amd.token_model import TokenModel, counting
+    t = U.torch()
+    n, length, c, k = 4, 128, 64, 5
+
+    def make():
+        return TokenModel(n, length, v, c, blocks=1, k=k)
+
+    ids, targets = counting(n, length, v, seed=1)
+    g = t.Generator(device="cuda").manual_seed(2)
+    tops = t.randint(0, v, (n, length, k), generator=g, device="cuda", dtype=t.int32)
+    logits = t.randn((n, length, k), generator=g, device="cuda")
+    alone = make()
+    alone.forward(ids)
+    want = alone.backward(ids, tops, logits).clone(), alone.dw["table"].clone()
+    both = make()
+    both.forward(ids)
+    both.backward(ids, targets)
+    t.cuda.synchronize()
+    before = t.cuda.memory_allocated()
+    both.forward(ids)
+    got = both.backward(ids, tops, logits)
+    grown = t.cuda.memory_allocated() - before
+    need = nc.nnconv_xent_workspace_size(both.distillation.desc, nc.NNCONV_DGRAD)[1]
+    # a teacher's is a little larger than the one that is there.  Below LARGE it is kept and twice its size is taken; from there on
+    # it is replaced by one that is an eighth larger.  The allocator rounds up to 2 MiB.
+    small = need < nc._Workspaces.LARGE
+    assert need >= 2 * n * length * v and small == (v == 30000)
+    assert grown <= (2 * need if small else need // 8) + (4 << 20)
+    assert t.equal(got, want[0]) and t.equal(both.dw["table"], want[1])
+    held = sum(w.numel() for w in both.loss._ws._held.values()) + sum(w.numel() for w in both.loss._ws._kept)
+    assert both.distillation._ws is both.loss._ws and held <= (3 * need if small else need * 9 // 8)
