@@ -627,7 +627,7 @@ typedef struct {
     int32_t dtype;         /* F16 or BF16: x, w, dx */
     int32_t k;             /* targets of a row, 1 to 1024; 1 with labels */
     int32_t teacher_dtype; /* F32 or dtype; F32 with labels */
-    float logit_scale;     /* finite, not 0: 1 / temperature */
+    float logit_scale;     /* finite, not 0, up to 2^127: 1 / temperature */
 } nnconv_xent_desc;
 
 /* Bytes of workspace of nnconv_xent_fwd (NNCONV_FWD) or nnconv_xent_train
@@ -643,7 +643,7 @@ nnconv_status nnconv_xent_workspace_size(const nnconv_xent_desc *desc, nnconv_pa
  * workspace.  ws: 16-byte aligned.
  * INVALID_ARG: sizes below the limits above, logit_scale 0 or not finite, bad
  * dtypes, null x, w, targets or loss, k other than 1 without a teacher;
- * UNSUPPORTED: larger sizes, other types; WORKSPACE; MISALIGNED. */
+ * UNSUPPORTED: larger sizes and factors, other types; WORKSPACE; MISALIGNED. */
 nnconv_status nnconv_xent_fwd(const nnconv_xent_desc *desc, const void *x, const void *w,
                               const int32_t *targets, const void *teacher, float *loss, float *lse,
                               void *ws, size_t ws_bytes, void *hip_stream);

@@ -456,7 +456,7 @@ static void launch_rows(int dtype, int teacher_dtype, Rows r, hipStream_t st) {
 using namespace xent;
 
 bool xent_fits(const XentParams &p) {
-    if (p.k > MOST_TARGETS) return false;
+    if (p.k > MOST_TARGETS || fabsf(p.logit_scale) > 0x1p127f) return false;  // 1.44 times which fp32 holds
     // a tile's rows are addressed with 31 bits, the threads of a launch with 32
     return p.c <= (1 << 20) && p.v <= (1 << 21) && p.rows <= (1 << 23) && p.rows * p.c <= MOST_OPERAND &&
            (int64_t)p.v * p.c <= MOST_OPERAND;
