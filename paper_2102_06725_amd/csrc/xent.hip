@@ -255,7 +255,7 @@ __global__ __launch_bounds__(256) void join_kernel(const Join P) {
 // A workgroup a stretch of a row, one or at most SHARE of them: each joins the row's statistics
 // itself (a launch for it took 4 us of a small step's 58), all of the stretch is scaled by its
 // tiles' factors, then the targets are written from their own logits.  Bound by its 4 bytes an
-// element (5.2 TB/s on 1 GiB).
+// element (4.9 TB/s on 1 GiB).
 constexpr int64_t STRETCH = 8192, SHARE = 8;
 
 template <class T>
