@@ -616,7 +616,8 @@ nnconv_status nnconv_embedding_bwd(const nnconv_embedding_desc *desc, const int3
  * teacher q is the softmax of logit_scale * teacher[r][.] over the row's k
  * entries, the teacher's largest logits as a rule, and the loss the divergence
  * of the student from it; entries whose target is padding or whose logit
- * teacher[r][i] is -inf are left out (whatever logit_scale's sign), and a target that is named twice counts with both shares.
+ * teacher[r][i] is -inf are left out (whatever logit_scale's sign), and a
+ * target that is named twice counts with both shares.
  * A row without an entry does not count: its loss, lse and gradients are 0, and
  * its x is not read.  Logits may be of any size whose products and their
  * differences fp32 holds: a row's largest product is taken off before the scale. */
